@@ -148,6 +148,70 @@ sw_status sw_mixed_iteration_host(sw_ctx* ctx, void* kv_pool, const sw_batch* h_
                                   const void* h_k_new, const void* h_v_new, void* h_out, float* h_lse,
                                   void* stream);
 
+/* ---- beside the plain iteration: a window, an 8-bit pool, eviction (no counterparts in the paper) ------------- */
+
+/* Attention inside a sliding window, with sinks: the row at position t attends key k when k <= t and (k > t - window or k < sinks), that is
+ * the last `window` keys including its own and the first `sinks` of its sequence.  window >= 1, sinks >= 0; a window as long as
+ * the context is full attention.  Otherwise as sw_mixed_attn_run and sw_mixed_iteration_run.  A page without a key that its row (of a
+ * chunk: some row from the same 256 / group tokens on) attends is not read, and its id not looked at: it may have been given to another
+ * sequence.  The keys beside attended ones, in pages that are read, must be finite. */
+sw_status sw_mixed_attn_window_run(sw_ctx* ctx, const void* kv_pool, const sw_batch* batch, int32_t window, int32_t sinks, const void* q,
+                                   void* out, float* lse, void* stream);
+sw_status sw_mixed_iteration_window_run(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, int32_t window, int32_t sinks, const void* k_new,
+                                        const void* v_new, const void* q, void* out, float* lse, void* stream);
+
+/* The KV pool in 8 bits.  kv8_pool: e4m3 [num_pages][2 (K, V)][num_kv_heads][16][head_dim] (num_pages of the context's layout), scales: fp32
+ * [num_pages][2][num_kv_heads]; an element of a block (page, K|V, head) stands for its e4m3 value times the block's scale, a power of two.
+ * Neither has to be initialised.  Both start on a 16-byte boundary.
+ *
+ * sw_kv8_append writes the iteration's rows (bf16, as sw_kv_append's).  A block's scale is the smallest power of two, 2^-100 at least, that
+ * brings the largest magnitude of its rows to 448 or less; rows are divided by it and rounded to the nearest e4m3 value.  Rows that join
+ * others in a page may raise the scale (it never falls): the older rows are then rounded again at the new one, which changes only values that
+ * become subnormal.  A row at a page's first slot starts the page anew.  A non-finite element makes its block's scale NaN, and NaN of all that is read
+ * from the block.  Rows of different chunks or requests must lie on different pages, or the shared page holds anything afterwards
+ * (append such rows by calls of their own).  Slots behind the new rows are left as they are.
+ *
+ * sw_kv8_attn_run is sw_mixed_attn_run over such a pool: its products see the values that the pool stands for exactly.  The scales must be
+ * powers of two (between 2^-100 and 2^120) or NaN.  Iterations with chunks first copy the chunks' prompts to 16 bits, in `scratch` (256-byte aligned
+ * device memory of sw_kv8_scratch_bytes(layout, sum over the chunks of ceil((P + C) / 16)) bytes, of no use between calls); decode-only
+ * ones take no scratch (NULL, 0).  Both calls are asynchronous. */
+size_t sw_kv8_scratch_bytes(const sw_layout* layout, int64_t prompt_pages);
+sw_status sw_kv8_append(sw_ctx* ctx, void* kv8_pool, float* scales, const sw_batch* batch, const void* k_new, const void* v_new, void* stream);
+sw_status sw_kv8_attn_run(sw_ctx* ctx, const void* kv8_pool, const float* scales, const sw_batch* batch, const void* q, void* out, float* lse,
+                          void* scratch, size_t scratch_bytes, void* stream);
+
+/* Accumulated attention weights: fp32 [rows][num_kv_heads][capacity] (device), one row per sequence, one weight per KV head and position.
+ * Request i of a batch uses row row_of[i] (device int32 [num_decode]); the requests of a call use different rows. */
+typedef struct {
+    float* weights;
+    int64_t rows;
+    int32_t capacity; /* positions in a row; no request of a call may be longer */
+    const int32_t* row_of;
+} sw_key_weights;
+
+/* sw_mixed_attn_run of a decode-only iteration that also adds up what weight every key got: the weight of key k of request i and a KV head grows
+ * by the sum over the head's group of exp(score - log-sum-exp).  The request's last key is set instead (it is attended for the first time).
+ * lse must be given, on a 16-byte boundary.  scratch: 16-byte aligned device memory of sw_attn_weights_scratch_bytes(layout,
+ * decode_page_indptr[num_decode]) bytes, of no use between calls.  A request that does not fit (row outside the weights, context longer than a
+ * row, pages beyond the scratch) is reported by sw_check_status; its output is written, its weights are not (nor, beyond the scratch, those of
+ * the pages there).  The sums do not depend on any order.  SW_ERR_UNSUPPORTED for batches with chunks.  Asynchronous (two launches). */
+size_t sw_attn_weights_scratch_bytes(const sw_layout* layout, int64_t decode_pages);
+sw_status sw_decode_attn_weights_run(sw_ctx* ctx, const void* kv_pool, const sw_batch* batch, const void* q, void* out, float* lse,
+                                     const sw_key_weights* weights, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Eviction by those weights.  Of the decode_kv_len[i] keys of request i (all in the pool), every KV head keeps min(budget, decode_kv_len[i]): the first `sinks`,
+ * the last `recent`, and of those between them the heaviest; of equal weights the ones at the lowest positions; a NaN counts as the
+ * lightest.  (A head's kept keys differ from another's.)  They keep their order.  K and V rows go to slots 0, 1, ... of the pages
+ * new_pages[new_page_indptr[i] ..] (device, CSR like the batch's), their weights to the front of row new_row_of[i] (device int32 [num_decode]); the
+ * positions they came from to kept[i][head][0 ..] (device int32 [num_decode][num_kv_heads][budget]), their number to new_len[i] (device
+ * int32).  What lies behind these is left as it is.  The old pages and rows are left as they are too; no new page or row may be among those that the
+ * call reads, nor twice among the new ones.  1 <= budget <= capacity, sinks + recent <= budget.  A request that does not fit (page list too
+ * short, row outside the weights, context longer than a row) is reported by sw_check_status, gets new_len 0 and nothing else; a page id outside the
+ * pool is reported, and that page's rows of that head are not copied.  Asynchronous (two launches). */
+sw_status sw_kv_evict(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const sw_key_weights* weights, const int32_t* new_page_indptr,
+                      const int32_t* new_pages, const int32_t* new_row_of, int32_t budget, int32_t sinks, int32_t recent, int32_t* kept,
+                      int32_t* new_len, void* stream);
+
 /* Profiler step (Sec. 5.1; Sec. 6.4): time the attention of one iteration over a stack of `layers` pools
  * (kv_pools: HOST array of `layers` device pool pointers, used round-robin so that successive launches do
  * not hit the same cache lines).  Runs `warmup` untimed and `reps` timed iterations of `layers` launches

@@ -63,12 +63,17 @@ class sw_telemetry_totals(C.Structure):
                 ("max_residual_ns", C.c_int64)]
 
 
+class sw_key_weights(C.Structure):
+    _fields_ = [("weights", C.c_void_p), ("rows", C.c_int64), ("capacity", C.c_int32), ("row_of", C.c_void_p)]
+
+
 EXPORTS = ["sw_workspace_bytes", "sw_create", "sw_destroy", "sw_kv_append", "sw_mixed_attn_run", "sw_mixed_iteration_run",
            "sw_mixed_iteration_host", "sw_cost_probe", "sw_cost_probe_iteration", "sw_check_status", "sw_cost_table_create",
            "sw_cost_table_destroy", "sw_cost_table_lookup", "sw_choose_chunk", "sw_choose_chunks", "sw_last_error",
            "sw_decode_attn_static", "sw_selftest_wait_timeout", "sw_telemetry_create", "sw_telemetry_destroy",
            "sw_telemetry_record", "sw_telemetry_margin", "sw_telemetry_exceeds", "sw_telemetry_get_totals",
-           "sw_telemetry_reset"]
+           "sw_telemetry_reset", "sw_mixed_attn_window_run", "sw_mixed_iteration_window_run", "sw_kv8_scratch_bytes", "sw_kv8_append",
+           "sw_kv8_attn_run", "sw_attn_weights_scratch_bytes", "sw_decode_attn_weights_run", "sw_kv_evict"]
 
 _vp, _i32, _i64 = C.c_void_p, C.c_int32, C.c_int64
 _lib.sw_workspace_bytes.restype = C.c_size_t
@@ -80,6 +85,16 @@ _lib.sw_kv_append.argtypes = [_vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp]
 _lib.sw_mixed_attn_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, _vp]
 _lib.sw_mixed_iteration_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.sw_mixed_iteration_host.argtypes = [_vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.sw_mixed_attn_window_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _i32, _i32, _vp, _vp, _vp, _vp]
+_lib.sw_mixed_iteration_window_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.sw_kv8_scratch_bytes.restype = C.c_size_t
+_lib.sw_kv8_scratch_bytes.argtypes = [C.POINTER(sw_layout), _i64]
+_lib.sw_kv8_append.argtypes = [_vp, _vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp]
+_lib.sw_kv8_attn_run.argtypes = [_vp, _vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, _vp, C.c_size_t, _vp]
+_lib.sw_attn_weights_scratch_bytes.restype = C.c_size_t
+_lib.sw_attn_weights_scratch_bytes.argtypes = [C.POINTER(sw_layout), _i64]
+_lib.sw_decode_attn_weights_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, C.POINTER(sw_key_weights), _vp, C.c_size_t, _vp]
+_lib.sw_kv_evict.argtypes = [_vp, _vp, C.POINTER(sw_batch), C.POINTER(sw_key_weights), _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp]
 _lib.sw_cost_probe.argtypes = [_vp, C.POINTER(_vp), _i32, C.POINTER(sw_batch), _vp, _vp, _i32, _i32,
                                C.POINTER(_i64), C.POINTER(_i64), C.POINTER(_i64), _vp]
 _lib.sw_cost_probe_iteration.argtypes = [_vp, C.POINTER(_vp), _i32, C.POINTER(sw_batch), _vp, _vp, _vp, _vp, _i32, _i32,
@@ -227,6 +242,74 @@ def sw_mixed_iteration_host(ctx: Context, kv_pool, host_struct: sw_batch, h_q, h
     _check(_lib.sw_mixed_iteration_host(ctx.handle, _ptr(kv_pool), C.byref(host_struct), _ptr(h_q), _ptr(h_k_new),
                                         _ptr(h_v_new), _ptr(h_out), _ptr(h_lse), _stream_handle(stream)),
            "sw_mixed_iteration_host")
+
+
+# ---- a window, an 8-bit pool, eviction --------------------------------------------------------------------------------
+def sw_mixed_attn_window_run(ctx: Context, kv_pool, batch: DeviceBatch, window: int, sinks: int, q, out, lse=None, stream=None) -> None:
+    """As ``sw_mixed_attn_run``; every row attends its last ``window`` keys and the first ``sinks`` of its sequence."""
+    _check(_lib.sw_mixed_attn_window_run(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), window, sinks, _ptr(q), _ptr(out), _ptr(lse),
+                                         _stream_handle(stream)), "sw_mixed_attn_window_run")
+
+
+def sw_mixed_iteration_window_run(ctx: Context, kv_pool, batch: DeviceBatch, window: int, sinks: int, k_new, v_new, q, out, lse=None,
+                                  stream=None) -> None:
+    _check(_lib.sw_mixed_iteration_window_run(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), window, sinks, _ptr(k_new), _ptr(v_new),
+                                              _ptr(q), _ptr(out), _ptr(lse), _stream_handle(stream)), "sw_mixed_iteration_window_run")
+
+
+def _bytes_of(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def sw_kv8_scratch_bytes(layout: sw_layout, prompt_pages: int) -> int:
+    return int(_lib.sw_kv8_scratch_bytes(C.byref(layout), prompt_pages))
+
+
+def sw_kv8_append(ctx: Context, kv8_pool, scales, batch: DeviceBatch, k_new, v_new, stream=None) -> None:
+    """The iteration's new rows into an 8-bit pool (``torch.float8_e4m3fn`` or ``uint8``) with its fp32 ``scales``."""
+    _check(_lib.sw_kv8_append(ctx.handle, _ptr(kv8_pool), _ptr(scales), C.byref(batch.struct), _ptr(k_new), _ptr(v_new),
+                              _stream_handle(stream)), "sw_kv8_append")
+
+
+def sw_kv8_attn_run(ctx: Context, kv8_pool, scales, batch: DeviceBatch, q, out, lse=None, scratch=None, stream=None) -> None:
+    """``sw_mixed_attn_run`` over an 8-bit pool; ``scratch``: ``sw_kv8_scratch_bytes`` bytes, for iterations with chunks."""
+    _check(_lib.sw_kv8_attn_run(ctx.handle, _ptr(kv8_pool), _ptr(scales), C.byref(batch.struct), _ptr(q), _ptr(out), _ptr(lse),
+                                _ptr(scratch), _bytes_of(scratch), _stream_handle(stream)), "sw_kv8_attn_run")
+
+
+class KeyWeights:
+    """Accumulated attention weights (fp32 ``[rows][num_kv_heads][capacity]``) and the rows of a batch's requests (int32)."""
+
+    def __init__(self, weights, row_of):
+        import torch
+
+        if weights.dtype != torch.float32 or weights.dim() != 3 or not weights.is_contiguous():
+            raise ValueError("weights must be a contiguous fp32 tensor [rows][num_kv_heads][capacity]")
+        if row_of.dtype != torch.int32 or row_of.dim() != 1 or not row_of.is_contiguous():
+            raise ValueError("row_of must be a contiguous int32 tensor")
+        self.weights, self.row_of = weights, row_of
+        self.struct = sw_key_weights(weights.data_ptr(), weights.shape[0], weights.shape[2], row_of.data_ptr())
+
+
+def sw_attn_weights_scratch_bytes(layout: sw_layout, decode_pages: int) -> int:
+    return int(_lib.sw_attn_weights_scratch_bytes(C.byref(layout), decode_pages))
+
+
+def sw_decode_attn_weights_run(ctx: Context, kv_pool, batch: DeviceBatch, q, out, lse, weights: KeyWeights, scratch, stream=None) -> None:
+    """Decode attention that adds what weight every key got to ``weights``; ``scratch``: ``sw_attn_weights_scratch_bytes`` bytes."""
+    _check(_lib.sw_decode_attn_weights_run(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), _ptr(q), _ptr(out), _ptr(lse),
+                                           C.byref(weights.struct), _ptr(scratch), _bytes_of(scratch), _stream_handle(stream)),
+           "sw_decode_attn_weights_run")
+
+
+def sw_kv_evict(ctx: Context, kv_pool, batch: DeviceBatch, weights: KeyWeights, new_page_indptr, new_pages, new_weights: KeyWeights,
+                budget: int, sinks: int, recent: int, kept, new_len, stream=None) -> None:
+    """Keep ``budget`` keys of every (request, KV head) pair; ``new_weights``: the same tensor with the rows they go to."""
+    if new_weights.weights.data_ptr() != weights.weights.data_ptr():
+        raise ValueError("new_weights must be rows of the same tensor")
+    _check(_lib.sw_kv_evict(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), C.byref(weights.struct), _ptr(new_page_indptr),
+                            _ptr(new_pages), _ptr(new_weights.row_of), budget, sinks, recent, _ptr(kept), _ptr(new_len),
+                            _stream_handle(stream)), "sw_kv_evict")
 
 
 def sw_cost_probe_iteration(ctx: Context, kv_pools, batch: DeviceBatch, k_new, v_new, q, out, warmup: int = 3,

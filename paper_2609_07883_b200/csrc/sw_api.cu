@@ -79,6 +79,7 @@ constexpr size_t kHostPartBytes = 4u << 20;
 
 struct sw_ctx {
     sw_layout layout;
+    bool window_grid_resident = false;   // as grid_resident, of the kernels with a window
     int device = 0;
     int num_sms = 0;
     float stage_us = 0.f, step_us = 0.f;  // planning estimates from the device's clocks (sw::device_timing)
@@ -94,6 +95,12 @@ struct sw_ctx {
         sw::KvMaps maps;
     };
     std::vector<MapEntry> kv_maps;  // small cache: one entry per pool of a layer stack
+    struct Kv8MapEntry {
+        const void* pool;
+        CUtensorMap map;
+    };
+    Kv8MapEntry kv8_maps[128];   // likewise of 8-bit pools, the oldest replaced first
+    int kv8_map_count = 0, kv8_map_next = 0;
     cudaEvent_t ev0 = nullptr, ev1 = nullptr;
     // host-buffer iterations in parts: the copies' stream and events
     cudaStream_t copies = nullptr;
@@ -284,8 +291,14 @@ sw_status sw_create(const sw_layout* layout, int device, void* workspace, size_t
     ctx->encode = reinterpret_cast<EncodeTiledFn>(fn);
     e = cudaMemset(ctx->ws, 0, w.pf_ml);  // control words, tickets and split-KV scratch start at zero
     if (e == cudaSuccess) e = sw::configure_kernels(layout->head_dim);
-    int per_sm = 0;
+    if (e == cudaSuccess) e = sw::configure_window_kernels(layout->head_dim);
+    if (e == cudaSuccess) e = sw::configure_kv8_kernels(layout->head_dim);
+    if (e == cudaSuccess) e = sw::configure_scored_kernels(layout->head_dim);
+    if (e == cudaSuccess) e = sw::configure_evict_kernels();
+    int per_sm = 0, window_per_sm = 0;
     if (e == cudaSuccess) e = sw::mixed_attn_resident_ctas_per_sm(layout->head_dim, &per_sm);
+    if (e == cudaSuccess) e = sw::window_attn_resident_ctas_per_sm(layout->head_dim, &window_per_sm);
+    ctx->window_grid_resident = (int64_t)window_per_sm * prop.multiProcessorCount >= ctx->num_sms;
     // The fused launch lets CTAs wait for one another's share of the KV append, so the whole grid has to be resident.
     // Where it would not be (fewer SMs than the properties promise cannot be seen here, but a smaller shared-memory
     // or register budget can) sw_mixed_iteration_run issues the append as a launch of its own.
@@ -318,17 +331,8 @@ void sw_destroy(sw_ctx* ctx) {
     delete ctx;
 }
 
-sw_status sw_kv_append(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const void* k_new, const void* v_new,
-                       void* stream) {
-    Chunks ch;
-    sw_status st = check_batch(ctx, batch, "sw_kv_append", &ch);
-    if (st != SW_OK) return st;
-    if (ch.rows + batch->num_decode == 0) return SW_OK;
-    if (!kv_pool || !k_new || !v_new) return sw_fail(SW_ERR_INVALID_ARG, "sw_kv_append: null tensor");
-    st = check_current_device(ctx, "sw_kv_append");
-    if (st != SW_OK) return st;
-    if (((reinterpret_cast<uintptr_t>(kv_pool) | reinterpret_cast<uintptr_t>(k_new) | reinterpret_cast<uintptr_t>(v_new)) & 15) != 0)
-        return sw_fail(SW_ERR_INVALID_ARG, "sw_kv_append: tensors must be 16-byte aligned");
+namespace {
+sw::AppendParams append_params(const sw_ctx* ctx, const sw_batch* batch, const Chunks& ch, void* kv_pool, const void* k_new, const void* v_new) {
     sw::AppendParams p{};
     p.Hkv = ctx->layout.num_kv_heads;
     p.D = ctx->layout.head_dim;
@@ -348,27 +352,29 @@ sw_status sw_kv_append(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const 
     p.v_new = static_cast<const __nv_bfloat16*>(v_new);
     p.pool = static_cast<__nv_bfloat16*>(kv_pool);
     p.ctrl = reinterpret_cast<int32_t*>(ctx->ws + ctx->w.ctrl);
+    return p;
+}
+}  // namespace
+
+sw_status sw_kv_append(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const void* k_new, const void* v_new,
+                       void* stream) {
+    Chunks ch;
+    sw_status st = check_batch(ctx, batch, "sw_kv_append", &ch);
+    if (st != SW_OK) return st;
+    if (ch.rows + batch->num_decode == 0) return SW_OK;
+    if (!kv_pool || !k_new || !v_new) return sw_fail(SW_ERR_INVALID_ARG, "sw_kv_append: null tensor");
+    st = check_current_device(ctx, "sw_kv_append");
+    if (st != SW_OK) return st;
+    if (((reinterpret_cast<uintptr_t>(kv_pool) | reinterpret_cast<uintptr_t>(k_new) | reinterpret_cast<uintptr_t>(v_new)) & 15) != 0)
+        return sw_fail(SW_ERR_INVALID_ARG, "sw_kv_append: tensors must be 16-byte aligned");
+    const sw::AppendParams p = append_params(ctx, batch, ch, kv_pool, k_new, v_new);
     SW_CUDA(sw::launch_kv_append(p, ctx->num_sms, static_cast<cudaStream_t>(stream)));
     return SW_OK;
 }
 
 namespace {
-// The attention launch; with k_new / v_new non-null the same launch first writes those rows into the pool.
-sw_status run_mixed(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const void* k_new, const void* v_new, const void* q,
-                    void* out, float* lse, void* stream, const char* who) {
-    Chunks ch;
-    sw_status st = check_batch(ctx, batch, who, &ch);
-    if (st != SW_OK) return st;
-    if (ch.rows + batch->num_decode == 0) return SW_OK;
-    if (!kv_pool || !q || !out) return sw_fail(SW_ERR_INVALID_ARG, "%s: null tensor", who);
-    st = check_current_device(ctx, who);
-    if (st != SW_OK) return st;
-    if (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(k_new) |
-          reinterpret_cast<uintptr_t>(v_new)) & 15) != 0)
-        return sw_fail(SW_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
-    const sw::KvMaps* kv_maps = nullptr;
-    st = kv_map_for(ctx, kv_pool, &kv_maps);
-    if (st != SW_OK) return st;
+// The parameters of an attention launch that do not depend on what the pool holds.
+sw::MixedParams mixed_params(const sw_ctx* ctx, const sw_batch* batch, const Chunks& ch, const void* q, void* out, float* lse) {
     const sw_layout& l = ctx->layout;
     sw::MixedParams p{};
     p.Hq = l.num_q_heads;
@@ -397,13 +403,6 @@ sw_status run_mixed(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const voi
     p.q = static_cast<const __nv_bfloat16*>(q);
     p.out = static_cast<__nv_bfloat16*>(out);
     p.lse = lse;
-    if (k_new) {
-        p.k_new = static_cast<const __nv_bfloat16*>(k_new);
-        p.v_new = static_cast<const __nv_bfloat16*>(v_new);
-        p.pool = static_cast<__nv_bfloat16*>(kv_pool);
-        p.append_first = p.C > 0;
-        p.append_last = p.C == 0;
-    }
     p.ctrl = reinterpret_cast<int32_t*>(ctx->ws + ctx->w.ctrl);
     p.tickets = reinterpret_cast<int32_t*>(ctx->ws + ctx->w.tickets);
     p.ready = p.tickets + (size_t)std::max(1, ctx->max_decode) * l.num_kv_heads;
@@ -416,37 +415,90 @@ sw_status run_mixed(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const voi
     p.pf_o = reinterpret_cast<float*>(ctx->ws + ctx->w.pf_o);
     p.pf_slots = ctx->w.pf_slots;
     p.pf_tickets = reinterpret_cast<int32_t*>(ctx->ws + ctx->w.pf_tickets);
-    // q as [row][head][element] restricted to the chunk rows: one box = 128 tile rows (token-major, the g heads of a
-    // KV head minor) x 64 elements; rows past the chunk read as zero
-    CUtensorMap q_map = kv_maps->half, out_map = kv_maps->half;
-    if (p.C > 0) {
-        const cuuint64_t dims[3] = {(cuuint64_t)l.head_dim, (cuuint64_t)l.num_q_heads, (cuuint64_t)p.C};
-        const cuuint64_t strides[2] = {(cuuint64_t)l.head_dim * 2, (cuuint64_t)l.num_q_heads * l.head_dim * 2};
-        const cuuint32_t box[3] = {64, (cuuint32_t)p.group, (cuuint32_t)(128 / p.group)};
-        const cuuint32_t elem_strides[3] = {1, 1, 1};
-        CUresult r = ctx->encode(&q_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box,
-                                 elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-        if (r != CUDA_SUCCESS) return sw_fail(SW_ERR_CUDA, "cuTensorMapEncodeTiled(q) failed with CUresult %d", (int)r);
-        // out has the same shape: tiles whose 128 rows all lie inside a chunk are stored through this map
-        r = ctx->encode(&out_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, out, dims, strides, box, elem_strides,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-        if (r != CUDA_SUCCESS) return sw_fail(SW_ERR_CUDA, "cuTensorMapEncodeTiled(out) failed with CUresult %d", (int)r);
+    return p;
+}
+
+// q as [row][head][element] restricted to the chunk rows: one box = 128 tile rows (token-major, the g heads of a
+// KV head minor) x 64 elements; rows past the chunk read as zero.  out has the same shape: tiles whose 128 rows all lie inside a chunk
+// are stored through its map.  (Without chunk rows the maps are left as they are.)
+sw_status encode_row_maps(const sw_ctx* ctx, const sw::MixedParams& p, CUtensorMap* q_map, CUtensorMap* out_map) {
+    if (p.C == 0) return SW_OK;
+    const sw_layout& l = ctx->layout;
+    const cuuint64_t dims[3] = {(cuuint64_t)l.head_dim, (cuuint64_t)l.num_q_heads, (cuuint64_t)p.C};
+    const cuuint64_t strides[2] = {(cuuint64_t)l.head_dim * 2, (cuuint64_t)l.num_q_heads * l.head_dim * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)p.group, (cuuint32_t)(128 / p.group)};
+    const cuuint32_t elem_strides[3] = {1, 1, 1};
+    CUresult r = ctx->encode(q_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(p.q), dims, strides, box,
+                             elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return sw_fail(SW_ERR_CUDA, "cuTensorMapEncodeTiled(q) failed with CUresult %d", (int)r);
+    r = ctx->encode(out_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, p.out, dims, strides, box, elem_strides,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return sw_fail(SW_ERR_CUDA, "cuTensorMapEncodeTiled(out) failed with CUresult %d", (int)r);
+    return SW_OK;
+}
+
+bool aligned16(const void* a, const void* b = nullptr, const void* c = nullptr, const void* d = nullptr) {
+    return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c) | reinterpret_cast<uintptr_t>(d)) & 15) == 0;
+}
+
+// The last `keys` keys and the first `sinks` are attended; keys == 0: all.
+struct Window {
+    int keys = 0, sinks = 0;
+};
+sw_status check_window(int32_t window, int32_t sinks, const char* who, Window* out) {
+    if (window < 1 || sinks < 0) return sw_fail(SW_ERR_INVALID_ARG, "%s: window %d, sinks %d (at least 1 and 0)", who, window, sinks);
+    out->keys = std::min(window, 1 << 30);   // (longer than any context whose positions the kernels can add to it)
+    out->sinks = std::min(sinks, 1 << 30);
+    return SW_OK;
+}
+
+// The attention launch; with k_new / v_new non-null the same launch first writes those rows into the pool.
+sw_status run_mixed(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const void* k_new, const void* v_new, const void* q,
+                    void* out, float* lse, void* stream, const char* who, Window window = {}) {
+    Chunks ch;
+    sw_status st = check_batch(ctx, batch, who, &ch);
+    if (st != SW_OK) return st;
+    if (ch.rows + batch->num_decode == 0) return SW_OK;
+    if (!kv_pool || !q || !out) return sw_fail(SW_ERR_INVALID_ARG, "%s: null tensor", who);
+    st = check_current_device(ctx, who);
+    if (st != SW_OK) return st;
+    if (!aligned16(q, out, k_new, v_new)) return sw_fail(SW_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
+    const sw::KvMaps* kv_maps = nullptr;
+    st = kv_map_for(ctx, kv_pool, &kv_maps);
+    if (st != SW_OK) return st;
+    sw::MixedParams p = mixed_params(ctx, batch, ch, q, out, lse);
+    if (k_new) {
+        p.k_new = static_cast<const __nv_bfloat16*>(k_new);
+        p.v_new = static_cast<const __nv_bfloat16*>(v_new);
+        p.pool = static_cast<__nv_bfloat16*>(kv_pool);
+        p.append_first = p.C > 0;
+        p.append_last = p.C == 0;
     }
-    SW_CUDA(sw::launch_mixed_attn(l.head_dim, *kv_maps, q_map, out_map, p, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+    CUtensorMap q_map = kv_maps->half, out_map = kv_maps->half;
+    st = encode_row_maps(ctx, p, &q_map, &out_map);
+    if (st != SW_OK) return st;
+    if (window.keys > 0) {
+        p.window = window.keys;
+        p.sinks = window.sinks;
+        p.sink_pages = (window.sinks + sw::kPageSize - 1) / sw::kPageSize;
+        SW_CUDA(sw::launch_window_attn(ctx->layout.head_dim, *kv_maps, q_map, out_map, p, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+        return SW_OK;
+    }
+    SW_CUDA(sw::launch_mixed_attn(ctx->layout.head_dim, *kv_maps, q_map, out_map, p, ctx->num_sms, static_cast<cudaStream_t>(stream)));
     return SW_OK;
 }
 
 // Append + attention: one launch, or two where the persistent grid would not be resident at once.
 sw_status run_iteration(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const void* k_new, const void* v_new, const void* q,
-                        void* out, float* lse, void* stream, const char* who) {
-    if (ctx && !ctx->grid_resident) {
+                        void* out, float* lse, void* stream, const char* who, Window window = {}) {
+    if (ctx && !(window.keys > 0 ? ctx->window_grid_resident : ctx->grid_resident)) {
         sw_status st = sw_kv_append(ctx, kv_pool, batch, k_new, v_new, stream);
         if (st != SW_OK) return st;
-        return run_mixed(ctx, kv_pool, batch, nullptr, nullptr, q, out, lse, stream, who);
+        return run_mixed(ctx, kv_pool, batch, nullptr, nullptr, q, out, lse, stream, who, window);
     }
-    return run_mixed(ctx, kv_pool, batch, k_new, v_new, q, out, lse, stream, who);
+    return run_mixed(ctx, kv_pool, batch, k_new, v_new, q, out, lse, stream, who, window);
 }
 }  // namespace
 
@@ -459,6 +511,224 @@ sw_status sw_mixed_iteration_run(sw_ctx* ctx, void* kv_pool, const sw_batch* bat
                                  const void* q, void* out, float* lse, void* stream) {
     if (!k_new || !v_new) return sw_fail(SW_ERR_INVALID_ARG, "sw_mixed_iteration_run: null tensor");
     return run_iteration(ctx, kv_pool, batch, k_new, v_new, q, out, lse, stream, "sw_mixed_iteration_run");
+}
+
+// ---- sliding window with sinks ------------------------------------------------------------------------------------
+sw_status sw_mixed_attn_window_run(sw_ctx* ctx, const void* kv_pool, const sw_batch* batch, int32_t window, int32_t sinks, const void* q,
+                                   void* out, float* lse, void* stream) {
+    Window w;
+    sw_status st = check_window(window, sinks, "sw_mixed_attn_window_run", &w);
+    if (st != SW_OK) return st;
+    return run_mixed(ctx, const_cast<void*>(kv_pool), batch, nullptr, nullptr, q, out, lse, stream, "sw_mixed_attn_window_run", w);
+}
+
+sw_status sw_mixed_iteration_window_run(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, int32_t window, int32_t sinks, const void* k_new,
+                                        const void* v_new, const void* q, void* out, float* lse, void* stream) {
+    Window w;
+    sw_status st = check_window(window, sinks, "sw_mixed_iteration_window_run", &w);
+    if (st != SW_OK) return st;
+    if (!k_new || !v_new) return sw_fail(SW_ERR_INVALID_ARG, "sw_mixed_iteration_window_run: null tensor");
+    return run_iteration(ctx, kv_pool, batch, k_new, v_new, q, out, lse, stream, "sw_mixed_iteration_window_run", w);
+}
+
+// ---- the pool in 8 bits --------------------------------------------------------------------------------------------
+namespace {
+// Pages of 16 bits that the chunks' prompts take.
+int64_t prompt_pages(const Chunks& ch) {
+    int64_t pages = 0;
+    for (int j = 0; j < ch.n; ++j) pages += ((int64_t)ch.P[j] + ch.C[j] + sw::kPageSize - 1) / sw::kPageSize;
+    return pages;
+}
+size_t page_bytes(const sw_layout& l) { return (size_t)2 * l.num_kv_heads * sw::kPageSize * l.head_dim * 2; }
+size_t kv8_scratch(const sw_layout& l, int64_t pages) { return (size_t)pages * page_bytes(l) + align_up((size_t)pages * 4, 256); }
+
+sw_status kv8_map_for(sw_ctx* ctx, const void* pool, const CUtensorMap** out) {
+    for (int i = 0; i < ctx->kv8_map_count; ++i)
+        if (ctx->kv8_maps[i].pool == pool) {
+            *out = &ctx->kv8_maps[i].map;
+            return SW_OK;
+        }
+    sw_ctx::Kv8MapEntry& e = ctx->kv8_maps[ctx->kv8_map_next];
+    e.pool = nullptr;
+    CUresult r = sw::encode_kv8_page_map(ctx->encode, ctx->layout, pool, &e.map);
+    if (r != CUDA_SUCCESS) return sw_fail(SW_ERR_CUDA, "cuTensorMapEncodeTiled(8-bit pool) failed with CUresult %d", (int)r);
+    e.pool = pool;
+    constexpr int kMost = sizeof ctx->kv8_maps / sizeof ctx->kv8_maps[0];
+    ctx->kv8_map_next = (ctx->kv8_map_next + 1) % kMost;
+    ctx->kv8_map_count = std::min(ctx->kv8_map_count + 1, kMost);
+    *out = &e.map;
+    return SW_OK;
+}
+}  // namespace
+
+size_t sw_kv8_scratch_bytes(const sw_layout* layout, int64_t prompt_pages) {
+    if (!layout || !layout_supported(*layout) || prompt_pages < 0 || prompt_pages > (int64_t)1 << 30 ||
+        2 * prompt_pages * layout->num_kv_heads >= (int64_t)1 << 31)
+        return 0;
+    return kv8_scratch(*layout, prompt_pages);
+}
+
+sw_status sw_kv8_append(sw_ctx* ctx, void* kv8_pool, float* scales, const sw_batch* batch, const void* k_new, const void* v_new, void* stream) {
+    Chunks ch;
+    sw_status st = check_batch(ctx, batch, "sw_kv8_append", &ch);
+    if (st != SW_OK) return st;
+    if (ch.rows + batch->num_decode == 0) return SW_OK;
+    if (!kv8_pool || !scales || !k_new || !v_new) return sw_fail(SW_ERR_INVALID_ARG, "sw_kv8_append: null tensor");
+    st = check_current_device(ctx, "sw_kv8_append");
+    if (st != SW_OK) return st;
+    if (!aligned16(kv8_pool, k_new, v_new, scales)) return sw_fail(SW_ERR_INVALID_ARG, "sw_kv8_append: tensors must be 16-byte aligned");
+    const sw::AppendParams p = append_params(ctx, batch, ch, nullptr, k_new, v_new);
+    SW_CUDA(sw::launch_kv8_append(p, ch.C, static_cast<uint8_t*>(kv8_pool), scales, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+    return SW_OK;
+}
+
+sw_status sw_kv8_attn_run(sw_ctx* ctx, const void* kv8_pool, const float* scales, const sw_batch* batch, const void* q, void* out, float* lse,
+                          void* scratch, size_t scratch_bytes, void* stream) {
+    const char* who = "sw_kv8_attn_run";
+    Chunks ch;
+    sw_status st = check_batch(ctx, batch, who, &ch);
+    if (st != SW_OK) return st;
+    if (ch.rows + batch->num_decode == 0) return SW_OK;
+    if (!kv8_pool || !scales || !q || !out) return sw_fail(SW_ERR_INVALID_ARG, "%s: null tensor", who);
+    st = check_current_device(ctx, who);
+    if (st != SW_OK) return st;
+    if (!aligned16(kv8_pool, q, out, scales)) return sw_fail(SW_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
+    const sw_layout& l = ctx->layout;
+    const int64_t pages = prompt_pages(ch);
+    if (pages > (int64_t)1 << 30 || 2 * pages * l.num_kv_heads >= (int64_t)1 << 31)
+        return sw_fail(SW_ERR_UNSUPPORTED, "%s: the chunks' prompts have %lld pages", who, (long long)pages);
+    if (pages > 0 && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255) != 0 || scratch_bytes < kv8_scratch(l, pages)))
+        return sw_fail(SW_ERR_WORKSPACE, "%s: prompts of %lld pages take a 256-byte aligned scratch of %zu bytes", who, (long long)pages,
+                       kv8_scratch(l, pages));
+    const CUtensorMap* page_map = nullptr;
+    st = kv8_map_for(ctx, kv8_pool, &page_map);
+    if (st != SW_OK) return st;
+    sw::KvMaps maps{*page_map, *page_map};
+    sw::MixedParams p = mixed_params(ctx, batch, ch, q, out, lse);
+    p.kv8_scales = scales;
+    p.stage_us *= 0.5f;   // pages are half as long
+    p.stages_per_us *= 2.f;
+    p.steps_per_stage *= 0.5f;
+    CUtensorMap q_map = *page_map, out_map = *page_map;
+    if (pages > 0) {
+        __nv_bfloat16* copy = static_cast<__nv_bfloat16*>(scratch);
+        int32_t* list = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(scratch) + (size_t)pages * page_bytes(l));
+        const sw::AppendParams a = append_params(ctx, batch, ch, nullptr, nullptr, nullptr);
+        sw_layout copy_layout = l;
+        copy_layout.num_pages = pages;
+        sw::KvMaps copy_maps;
+        CUresult r = sw::encode_kv_maps(ctx->encode, copy_layout, copy, &copy_maps);
+        if (r != CUDA_SUCCESS) return sw_fail(SW_ERR_CUDA, "cuTensorMapEncodeTiled(scratch) failed with CUresult %d", (int)r);
+        maps.half = copy_maps.half;
+        st = encode_row_maps(ctx, p, &q_map, &out_map);
+        if (st != SW_OK) return st;
+        SW_CUDA(sw::launch_kv8_expand(a, ch.C, static_cast<const uint8_t*>(kv8_pool), scales, copy, list, ctx->num_sms,
+                                      static_cast<cudaStream_t>(stream)));
+        p.prefill_pages = list;
+        p.num_prefill_pages = (int)pages;
+        p.chunk_pages = pages;
+        for (int j = 0; j < ch.n; ++j) p.cPage0[j + 1] = p.cPage0[j] + (int)(((int64_t)ch.P[j] + ch.C[j] + sw::kPageSize - 1) / sw::kPageSize);
+        for (int j = ch.n; j < sw::kMaxChunks; ++j) p.cPage0[j + 1] = p.cPage0[ch.n];
+    }
+    SW_CUDA(sw::launch_kv8_attn(l.head_dim, maps, q_map, out_map, p, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+    return SW_OK;
+}
+
+// ---- weights of keys, and eviction by them ---------------------------------------------------------------------------
+namespace {
+size_t score_bytes_per_page(const sw_layout& l) { return (size_t)sw::kPageSize * l.num_q_heads * 4; }
+sw_status check_weights(const sw_key_weights* w, const char* who) {
+    if (!w || !w->weights || !w->row_of) return sw_fail(SW_ERR_INVALID_ARG, "%s: null weights or rows", who);
+    if (w->rows < 1 || w->capacity < 1) return sw_fail(SW_ERR_INVALID_ARG, "%s: %lld rows of %d weights", who, (long long)w->rows, w->capacity);
+    return SW_OK;
+}
+}  // namespace
+
+size_t sw_attn_weights_scratch_bytes(const sw_layout* layout, int64_t decode_pages) {
+    if (!layout || !layout_supported(*layout) || decode_pages < 0 || decode_pages > INT32_MAX) return 0;
+    return (size_t)decode_pages * score_bytes_per_page(*layout);
+}
+
+sw_status sw_decode_attn_weights_run(sw_ctx* ctx, const void* kv_pool, const sw_batch* batch, const void* q, void* out, float* lse,
+                                     const sw_key_weights* weights, void* scratch, size_t scratch_bytes, void* stream) {
+    const char* who = "sw_decode_attn_weights_run";
+    Chunks ch;
+    sw_status st = check_batch(ctx, batch, who, &ch);
+    if (st != SW_OK) return st;
+    if (ch.rows > 0) return sw_fail(SW_ERR_UNSUPPORTED, "%s: decode-only (no chunks)", who);
+    if (batch->num_decode == 0) return SW_OK;
+    if (!kv_pool || !q || !out || !lse || !scratch) return sw_fail(SW_ERR_INVALID_ARG, "%s: null tensor", who);
+    st = check_weights(weights, who);
+    if (st != SW_OK) return st;
+    st = check_current_device(ctx, who);
+    if (st != SW_OK) return st;
+    if (!aligned16(q, out, lse, scratch)) return sw_fail(SW_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
+    const sw::KvMaps* kv_maps = nullptr;
+    st = kv_map_for(ctx, kv_pool, &kv_maps);
+    if (st != SW_OK) return st;
+    const sw_layout& l = ctx->layout;
+    sw::MixedParams p = mixed_params(ctx, batch, ch, q, out, lse);
+    p.scores = static_cast<float*>(scratch);
+    p.score_pages = (int64_t)(scratch_bytes / score_bytes_per_page(l));
+    sw::WeightParams w{};
+    w.n = p.n;
+    w.Hkv = p.Hkv;
+    w.group = p.group;
+    w.capacity = weights->capacity;
+    w.rows = weights->rows;
+    w.kv_len = p.decode_kv_len;
+    w.page_indptr = p.decode_page_indptr;
+    w.row_of = weights->row_of;
+    w.scores = p.scores;
+    w.lse = lse;
+    w.score_pages = p.score_pages;
+    w.weights = weights->weights;
+    w.ctrl = p.ctrl;
+    SW_CUDA(sw::launch_scored_attn(l.head_dim, *kv_maps, kv_maps->half, p, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+    SW_CUDA(sw::launch_key_weights(w, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+    return SW_OK;
+}
+
+sw_status sw_kv_evict(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const sw_key_weights* weights, const int32_t* new_page_indptr,
+                      const int32_t* new_pages, const int32_t* new_row_of, int32_t budget, int32_t sinks, int32_t recent, int32_t* kept,
+                      int32_t* new_len, void* stream) {
+    const char* who = "sw_kv_evict";
+    Chunks ch;
+    sw_status st = check_batch(ctx, batch, who, &ch);
+    if (st != SW_OK) return st;
+    if (ch.rows > 0) return sw_fail(SW_ERR_UNSUPPORTED, "%s: decode requests only (no chunks)", who);
+    if (batch->num_decode == 0) return SW_OK;
+    if (!kv_pool || !new_page_indptr || !new_pages || !new_row_of || !kept || !new_len) return sw_fail(SW_ERR_INVALID_ARG, "%s: null tensor", who);
+    st = check_weights(weights, who);
+    if (st != SW_OK) return st;
+    if (budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget || budget > weights->capacity)
+        return sw_fail(SW_ERR_INVALID_ARG, "%s: budget %d (sinks %d, recent %d, capacity %d)", who, budget, sinks, recent, weights->capacity);
+    st = check_current_device(ctx, who);
+    if (st != SW_OK) return st;
+    if (!aligned16(kv_pool)) return sw_fail(SW_ERR_INVALID_ARG, "%s: kv_pool must be 16-byte aligned", who);
+    sw::EvictParams p{};
+    p.n = batch->num_decode;
+    p.Hkv = ctx->layout.num_kv_heads;
+    p.capacity = weights->capacity;
+    p.budget = budget;
+    p.sinks = sinks;
+    p.recent = recent;
+    p.num_pages = ctx->layout.num_pages;
+    p.rows = weights->rows;
+    p.kv_len = batch->decode_kv_len;
+    p.page_indptr = batch->decode_page_indptr;
+    p.pages = batch->decode_pages;
+    p.row_of = weights->row_of;
+    p.new_page_indptr = new_page_indptr;
+    p.new_pages = new_pages;
+    p.new_row_of = new_row_of;
+    p.weights = weights->weights;
+    p.pool = static_cast<__nv_bfloat16*>(kv_pool);
+    p.kept = kept;
+    p.new_len = new_len;
+    p.ctrl = reinterpret_cast<int32_t*>(ctx->ws + ctx->w.ctrl);
+    SW_CUDA(sw::launch_evict(p, ctx->layout.head_dim, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+    return SW_OK;
 }
 
 namespace {

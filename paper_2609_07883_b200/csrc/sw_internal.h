@@ -32,7 +32,7 @@ enum SetWord { kSetWork = 0, kSetPrefill = 1, kSetAppend = 2, kSetItems = 3, kSe
 
 // Device-detected problem locators written to kCtrDetail (high byte = site, low 24 bits = index).
 enum DetailSite { kSiteAppendPage = 1, kSiteAppendLen = 2, kSiteAttnLen = 3, kSiteAttnPage = 4, kSiteWait = 5,
-                  kSiteScratch = 6, kSiteTmem = 7 };
+                  kSiteScratch = 6, kSiteTmem = 7, kSiteWeights = 8, kSiteEvict = 9 };
 
 struct MixedParams {
     // shape
@@ -80,6 +80,14 @@ struct MixedParams {
     float* pf_o;         // [pf_slots][2][D / 4][128][4]
     int pf_slots;        // kMaxCtas, or kPfRoundSlots where a chunk can hold a whole round of items
     int32_t* pf_tickets; // [items][2]
+    // launches with a window: the last `window` keys and the first `sinks` are attended
+    int window, sinks, sink_pages;   // pages that hold a key below `sinks`
+    // launches over an 8-bit pool: fp32 [num_pages][2][Hkv]; pages of the chunks' 16-bit copy (prefill_pages lists those)
+    const float* kv8_scales;
+    int64_t chunk_pages;
+    // launches that leave their scores behind: fp32 [score_pages][Hkv][16][group] by place in decode_pages
+    float* scores;
+    int64_t score_pages;
 };
 
 struct AppendParams {
@@ -96,6 +104,28 @@ struct AppendParams {
     const __nv_bfloat16* k_new;
     const __nv_bfloat16* v_new;
     __nv_bfloat16* pool;
+    int32_t* ctrl;
+};
+
+// Weights of a decode-only iteration's keys from its scores (scores, lse: of the attention launch before it).
+struct WeightParams {
+    int n, Hkv, group, capacity;
+    int64_t rows;
+    const int32_t *kv_len, *page_indptr, *row_of;
+    const float *scores, *lse;
+    int64_t score_pages;
+    float* weights;   // [rows][Hkv][capacity]
+    int32_t* ctrl;
+};
+
+struct EvictParams {
+    int n, Hkv, capacity, budget, sinks, recent;
+    int64_t num_pages, rows;
+    const int32_t *kv_len, *page_indptr, *pages, *row_of;
+    const int32_t *new_page_indptr, *new_pages, *new_row_of;
+    float* weights;   // [rows][Hkv][capacity]
+    __nv_bfloat16* pool;
+    int32_t *kept, *new_len;   // [n][Hkv][budget], [n]
     int32_t* ctrl;
 };
 
@@ -136,6 +166,17 @@ inline CUresult encode_kv_maps(EncodeTiledFn encode, const sw_layout& l, const v
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
+// Tensor map of an 8-bit pool: box = all of one head's K and V in a page, K's 16 slots first, swizzled by their row's length.
+inline CUresult encode_kv8_page_map(EncodeTiledFn encode, const sw_layout& l, const void* pool, CUtensorMap* out) {
+    const cuuint64_t row = (cuuint64_t)l.head_dim, head = kPageSize * row, side = (cuuint64_t)l.num_kv_heads * head;
+    const cuuint64_t dims[5] = {row, (cuuint64_t)kPageSize, 1, (cuuint64_t)2 * l.num_pages, (cuuint64_t)l.num_kv_heads};
+    const cuuint64_t strides[4] = {row, head, side, head};
+    const cuuint32_t box[5] = {(cuuint32_t)l.head_dim, (cuuint32_t)kPageSize, 1, 2, 1}, ones[5] = {1, 1, 1, 1, 1};
+    return encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, const_cast<void*>(pool), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  l.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
 // launchers (sw_kernels.cu)
 cudaError_t launch_kv_append(const AppendParams& p, int num_sms, cudaStream_t stream);
 // MixedParams::stage_us / step_us for a device: the memory system streams about 0.76 of clock x bus width x 2 (measured
@@ -160,9 +201,27 @@ cudaError_t launch_mixed_attn(int head_dim, const KvMaps& kv_maps, const CUtenso
                               const MixedParams& p,
                               int num_sms, cudaStream_t stream);
 cudaError_t configure_kernels(int head_dim);
+// the same with a window (sw_window.cu)
+cudaError_t launch_window_attn(int head_dim, const KvMaps& kv_maps, const CUtensorMap& q_map, const CUtensorMap& out_map, const MixedParams& p,
+                               int num_sms, cudaStream_t stream);
+cudaError_t configure_window_kernels(int head_dim);
+cudaError_t window_attn_resident_ctas_per_sm(int head_dim, int* out);
+// 8-bit pools (sw_kv8.cu)
+cudaError_t launch_kv8_append(const AppendParams& a, const int* cC, uint8_t* pool, float* scales, int num_sms, cudaStream_t stream);
+cudaError_t launch_kv8_expand(const AppendParams& a, const int* cC, const uint8_t* pool, const float* scales, __nv_bfloat16* copy, int32_t* list,
+                              int num_sms, cudaStream_t stream);
+cudaError_t launch_kv8_attn(int head_dim, const KvMaps& kv_maps, const CUtensorMap& q_map, const CUtensorMap& out_map, const MixedParams& p,
+                            int num_sms, cudaStream_t stream);
+cudaError_t configure_kv8_kernels(int head_dim);
+// decode attention that adds up weights (sw_weights.cu)
+cudaError_t launch_scored_attn(int head_dim, const KvMaps& kv_maps, const CUtensorMap& any_map, const MixedParams& p, int num_sms, cudaStream_t stream);
+cudaError_t launch_key_weights(const WeightParams& p, int num_sms, cudaStream_t stream);
+cudaError_t configure_scored_kernels(int head_dim);
+// eviction (sw_evict.cu)
+cudaError_t launch_evict(const EvictParams& p, int head_dim, int num_sms, cudaStream_t stream);
+cudaError_t configure_evict_kernels();
 cudaError_t mixed_attn_resident_ctas_per_sm(int head_dim, int* out);
 cudaError_t launch_selftest_wait(int32_t* ctrl, long long budget_cycles, cudaStream_t stream);
-size_t mixed_attn_smem_bytes(int head_dim);
 
 }  // namespace sw
 

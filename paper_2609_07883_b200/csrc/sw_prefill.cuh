@@ -1,4 +1,4 @@
-// Chunk-prefill attention tiles on the 5th-generation tensor cores (tcgen05 + TMEM), included by sw_kernels.cu.
+// Chunk-prefill attention tiles on the 5th-generation tensor cores (tcgen05 + TMEM), included by sw_mixed.cuh.
 //
 // One work item = one KV head x 256 query rows (two 128-row tiles).  A tile's rows are (token, query head of the
 // group) pairs, token-major: row r <-> chunk token tok0 + r / g, head kvh*g + r % g, so all g query heads that
@@ -134,11 +134,12 @@ struct PfItem {
     int kvh;
     int chunk;       // which chunk of the iteration the item belongs to (its descriptors are in the shared table)
     int tok0[2];     // first chunk token of each tile
-    int nkv[2];      // KV tiles each tile attends in total (0 = tile has no rows)
+    int nkv[2];      // KV tiles each tile attends in total (0 = tile has no rows; kWindow: less the tiles that are passed over)
     int nk;          // steps of the item = max(nkv)
     int j0, j1;      // this entry's piece of the item: KV tiles [j0, j1)
     int piece;       // index of the piece (0 when the item is whole)
     int slot0;       // scratch slot of the item's piece 0 (tail items only)
+    int head, skip;  // kWindow: step j is KV tile j below `head` (tiles with sinks) and j + skip from there on
     int pieces;      // pieces the item is cut into (several chunks: each chunk has its own count)
 };
 
@@ -151,11 +152,25 @@ __device__ __forceinline__ int pf_num_groups(int group, int C) {
     const int tok_per_item = 256 / group;
     return (C + tok_per_item - 1) / tok_per_item;
 }
+// kWindow: an item passes over the KV tiles between the sinks and the window of its first row.  (A later row's window begins later: for
+// its tile the first steps may be masked as a whole.)
+template <Option O>
+__device__ __forceinline__ void pf_passed(const MixedParams& p, int P, int tok0, int& head, int& skip) {
+    head = skip = 0;
+    if constexpr (O == kWindow) {
+        const int first = max(0, P + tok0 + 1 - p.window) / 128;
+        head = min(first, (p.sinks + 127) / 128);
+        skip = first - head;
+    }
+}
 // steps of one item of rank r of a chunk with n_tp groups (the later tile, when it has rows, attends the most keys)
-__device__ __forceinline__ int pf_steps_of_rank(int group, int P, int C, int n_tp, int r) {
-    const int tt = 128 / group;
+template <Option O>
+__device__ __forceinline__ int pf_steps_of_rank(const MixedParams& p, int P, int C, int n_tp, int r) {
+    const int tt = 128 / p.group;
     const int tp = n_tp - 1 - r;
-    return max(pf_tiles_of(group, P, C, (tp * 2) * tt), pf_tiles_of(group, P, C, (tp * 2 + 1) * tt));
+    int head, skip;
+    pf_passed<O>(p, P, tp * 2 * tt, head, skip);
+    return max(pf_tiles_of(p.group, P, C, (tp * 2) * tt), pf_tiles_of(p.group, P, C, (tp * 2 + 1) * tt)) - skip;
 }
 // first KV tile of piece i when nk steps are cut into k pieces
 __device__ __forceinline__ int pf_piece_begin(int nk, int k, int i) { return (int)(((long long)nk * i) / k); }
@@ -198,8 +213,12 @@ __device__ __forceinline__ int pf_entry_ctas(const MixedParams& p, int G, int n_
     const int need = (int)ceilf(kEntrySafety * (wp + kEntryCostSteps * (float)n_items) / decode_steps);
     return min(max(need, max(1, G / 8)), G - min(kDecodeCtasAtFullRate, G / 2));
 }
+template <Option O>
 __device__ __forceinline__ float pf_decode_steps(const MixedParams& p) {  // the decode phase at the full rate, in steps
-    return p.n > 0 ? (float)__ldg(p.decode_page_indptr + p.n) * (float)p.Hkv * p.steps_per_stage : 0.f;
+    if (p.n <= 0) return 0.f;
+    float pages = (float)__ldg(p.decode_page_indptr + p.n);
+    if constexpr (O == kWindow) pages = fminf(pages, (float)p.n * (float)(p.window / kPageSize + 2 + p.sink_pages));   // at most what is visible
+    return pages * (float)p.Hkv * p.steps_per_stage;
 }
 
 // Several chunks in one iteration: the tail items (the last n_items mod G ones, G the CTAs that take entries) belong to chunks of very
@@ -208,6 +227,7 @@ __device__ __forceinline__ float pf_decode_steps(const MixedParams& p) {  // the
 // gives one up.  G: CTAs that take entries.  Run by one whole warp, lane j owning chunk j; fills the chunk table:
 // fields 0-3 the descriptors, 4 pieces per tail item, 5 items before the chunk, 6 tail entries before the chunk's
 // tail items (fields 5 and 6 hold INT_MAX where nothing may match), 7 scratch slots before them, then the plan's totals.
+template <Option O>
 __device__ __forceinline__ void pf_fill_chunk_table(const MixedParams& p, int* tbl, int G) {
     const int lane = threadIdx.x & 31;
     int P = 0, C = 0, row0 = 0, page0 = 0;
@@ -234,8 +254,8 @@ __device__ __forceinline__ void pf_fill_chunk_table(const MixedParams& p, int* t
     const int n_items = __shfl_sync(0xffffffffu, incl, kMaxChunks - 1);
     int longest = 0, shortest = 0x7fffffff;
     if (n_tp > 0) {
-        longest = pf_steps_of_rank(p.group, P, C, n_tp, 0);
-        shortest = pf_steps_of_rank(p.group, P, C, n_tp, n_tp - 1);
+        longest = pf_steps_of_rank<O>(p, P, C, n_tp, 0);
+        shortest = pf_steps_of_rank<O>(p, P, C, n_tp, n_tp - 1);
     }
     const int steps2 = __reduce_add_sync(0xffffffffu, n_tp > 0 ? (longest + shortest) * cnt : 0);
     int n_whole = n_items - n_items % G;
@@ -319,13 +339,15 @@ __device__ __forceinline__ void pf_fill_chunk_table(const MixedParams& p, int* t
 }
 // Beside enough decode pages a few CTAs take no entry (the rule of the single-chunk plan; pieces in one round here): how many do, for
 // a table filled with the whole grid.
+template <Option O>
 __device__ __forceinline__ int pf_table_ctas(const MixedParams& p, const int* tbl) {
     const int* tot = tbl + kChunkTotals;
-    return pf_entry_ctas(p, (int)gridDim.x, tot[0], 0.5f * (float)tot[7], pf_decode_steps(p));
+    return pf_entry_ctas(p, (int)gridDim.x, tot[0], 0.5f * (float)tot[7], pf_decode_steps<O>(p));
 }
 
 // The same for a single chunk, whose descriptors are kernel parameters: the plan's totals only.  Run by one whole warp likewise, so
 // that the planning costs the roles of the chunk-prefill phase no register.
+template <Option O>
 __device__ __forceinline__ void pf_fill_plan(const MixedParams& p, int* tbl) {
     PfPlan plan;
     int G = (int)gridDim.x;
@@ -334,10 +356,10 @@ __device__ __forceinline__ void pf_fill_plan(const MixedParams& p, int* tbl) {
     plan.longest = 0;
     plan.shortest = 0x7fffffff;
     if (n_tp > 0) {
-        plan.longest = pf_steps_of_rank(p.group, p.cP[0], p.cC[0], n_tp, 0);
-        plan.shortest = pf_steps_of_rank(p.group, p.cP[0], p.cC[0], n_tp, n_tp - 1);
+        plan.longest = pf_steps_of_rank<O>(p, p.cP[0], p.cC[0], n_tp, 0);
+        plan.shortest = pf_steps_of_rank<O>(p, p.cP[0], p.cC[0], n_tp, n_tp - 1);
     }
-    const float decode_steps = pf_decode_steps(p);
+    const float decode_steps = pf_decode_steps<O>(p);
     int entry_ctas = pf_entry_ctas(p, G, plan.n_items, 0.5f * (float)(plan.longest + plan.shortest) * (float)plan.n_items,
                                          decode_steps);
     if (p.n > 0 && plan.n_items < G && decode_steps >= kDecodeCtasMinSteps) {
@@ -431,7 +453,7 @@ __device__ __forceinline__ PfPlan pf_make_plan(uint32_t table) {  // worked out 
     return plan;
 }
 
-template <bool kMulti>
+template <bool kMulti, Option O>
 __device__ __forceinline__ PfItem pf_entry(const MixedParams& p, const PfPlan& plan, int entry) {
     PfItem it;
     it.pieces = plan.pieces;
@@ -478,9 +500,10 @@ __device__ __forceinline__ PfItem pf_entry(const MixedParams& p, const PfPlan& p
     it.kvh = local % p.Hkv;
     const int tt = 128 / p.group;
     const int tp = pf_num_groups(p.group, cC) - 1 - rank;
+    pf_passed<O>(p, cP, tp * 2 * tt, it.head, it.skip);
     for (int t = 0; t < 2; ++t) {
         it.tok0[t] = (tp * 2 + t) * tt;
-        it.nkv[t] = pf_tiles_of(p.group, cP, cC, it.tok0[t]);
+        it.nkv[t] = max(0, pf_tiles_of(p.group, cP, cC, it.tok0[t]) - it.skip);
     }
     it.nk = max(it.nkv[0], it.nkv[1]);
     if (entry < plan.n_whole) {
@@ -493,8 +516,17 @@ __device__ __forceinline__ PfItem pf_entry(const MixedParams& p, const PfPlan& p
     return it;
 }
 
+template <Option O>
+__device__ __forceinline__ int pf_tile(const PfItem& it, int j) { return O == kWindow && j >= it.head ? j + it.skip : j; }
+// kWindow: whether some row of the item attends a key of the page (if the prompt reaches that far).  The others are not read: what left
+// every window may have been given to another prompt.
+template <Option O>
+__device__ __forceinline__ bool pf_page_seen(const MixedParams& p, const PfItem& it, int P, int page) {
+    return O != kWindow || page < p.sink_pages || page * kPageSize + kPageSize > P + it.tok0[0] + 1 - p.window;
+}
+
 // ---- role: TMA producer (one warp) ----------------------------------------------------------------------------
-template <int D, bool kMulti>
+template <int D, bool kMulti, Option O>
 __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUtensorMap* q_map, const MixedParams& p,
                                            const PfShared& sh, const PfItem& it, uint32_t& kv_it) {
     using G = PfGeo<D>;
@@ -512,7 +544,7 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
                                 h * 64, it.kvh * p.group, pf_chunk<D, kMulti>(p, sh, 2, it.chunk) + it.tok0[t]);
     }
     // fused launch: tiles that reach into the chunk's own keys wait until every CTA has written its share of them
-    if (p.append_first && it.j1 * 128 > pf_chunk<D, kMulti>(p, sh, 0, it.chunk) && !wait_append(p, sh.smem + Geo<D>::kSetOffset)) {
+    if (p.append_first && (pf_tile<O>(it, it.j1 - 1) + 1) * 128 > pf_chunk<D, kMulti>(p, sh, 0, it.chunk) && !wait_append(p, sh.smem + Geo<D>::kSetOffset)) {
         if (lane == 0) {
             *sh.abort_flag = 1;
             report(p.ctrl, SW_ERR_DEVICE_TIMEOUT, kSiteWait, it.item);
@@ -520,32 +552,40 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
         return false;
     }
     const int npages = (pf_chunk<D, kMulti>(p, sh, 0, it.chunk) + pf_chunk<D, kMulti>(p, sh, 1, it.chunk) + kPageSize - 1) / kPageSize;
-    auto page_of = [&](int j) {
-        int id = (lane < 8 && j * 8 + lane < npages) ? p.prefill_pages[pf_chunk<D, kMulti>(p, sh, 3, it.chunk) + j * 8 + lane] : 0;
-        if (id < 0 || (int64_t)id >= p.num_pages) {
+    auto seen = [&](int page) { return page < npages && pf_page_seen<O>(p, it, pf_chunk<D, kMulti>(p, sh, 0, it.chunk), page); };
+    auto id_of = [&](int step) {
+        const int page = pf_tile<O>(it, step) * 8 + lane;
+        int id = (lane < 8 && seen(page)) ? p.prefill_pages[pf_chunk<D, kMulti>(p, sh, 3, it.chunk) + page] : 0;
+        if (id < 0 || (int64_t)id >= (O == kKv8 ? p.chunk_pages : p.num_pages)) {
             // reported, and page 0 fetched in its place: a bad id never reaches the copy engine
             report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteAttnPage, it.item);
             id = 0;
         }
         return id;
     };
-    int id_next = page_of(it.j0);
+    int id_next = id_of(it.j0);
     for (int j = it.j0; j < it.j1; ++j, ++kv_it) {
         const uint32_t s = kv_it & 1, n = kv_it >> 1;
         const int id = id_next;
-        if (j + 1 < it.j1) id_next = page_of(j + 1);  // in flight while this tile is issued
-        const int nvp = min(8, npages - j * 8);
+        if (j + 1 < it.j1) id_next = id_of(j + 1);  // in flight while this tile is issued
+        const int tile = pf_tile<O>(it, j);
+        int nvp = min(8, npages - tile * 8);
+        bool mine = lane < nvp;
+        if constexpr (O == kWindow) {
+            mine = mine && seen(tile * 8 + lane);
+            nvp = __popc(__ballot_sync(0xffffffffu, mine));
+        }
         const uint32_t kdst = sh.smem + G::kKVOffset + s * 2 * G::kTileBytes;
         const uint32_t vdst = kdst + G::kTileBytes;
         if (!pf_wait(sh, kBarKEmpty + s, (n & 1) ^ 1, p.ctrl, 1)) return false;
         if (lane == 0) mbar_arrive_expect_tx(sh.bars + (kBarKFull + s) * 8, nvp * G::kPageStride);
         __syncwarp();
-        if (lane < nvp)
+        if (mine)
             tma_load_5d(kdst + lane * G::kPageStride, kv_map, sh.bars + (kBarKFull + s) * 8, 0, 0, 0, 0, (2 * id) * p.Hkv + it.kvh);
         if (!pf_wait(sh, kBarVEmpty + s, (n & 1) ^ 1, p.ctrl, 2)) return false;
         if (lane == 0) mbar_arrive_expect_tx(sh.bars + (kBarVLanded + s) * 8, nvp * G::kPageStride);
         __syncwarp();
-        if (lane < nvp)
+        if (mine)
             tma_load_5d(vdst + lane * G::kPageStride, kv_map, sh.bars + (kBarVLanded + s) * 8, 0, 0, 0, 0,
                         (2 * id + 1) * p.Hkv + it.kvh);
     }
@@ -555,7 +595,7 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
 // ---- role: V sanitizer (one warp) -------------------------------------------------------------------------------
 // Keys at or past P + C are never attended, but their V rows still enter the P V product with weight zero; zero them
 // so that whatever an unwritten page slot (or a stale buffer) holds cannot turn 0 * x into NaN.
-template <int D, bool kMulti>
+template <int D, bool kMulti, Option O>
 __device__ __forceinline__ bool pf_sanitize(const MixedParams& p, const PfShared& sh, const PfItem& it, uint32_t& kv_it) {
     using G = PfGeo<D>;
     const int lane = threadIdx.x & 31;
@@ -563,7 +603,17 @@ __device__ __forceinline__ bool pf_sanitize(const MixedParams& p, const PfShared
     for (int j = it.j0; j < it.j1; ++j, ++kv_it) {
         const uint32_t s = kv_it & 1, n = kv_it >> 1;
         if (!pf_wait(sh, kBarVLanded + s, n & 1, p.ctrl, 3)) return false;
-        const int first_dead = max(0, kv_total - j * 128);
+        const int first_dead = max(0, kv_total - pf_tile<O>(it, j) * 128);
+        if constexpr (O == kWindow) {   // pages that the producer has passed over
+            const int P = pf_chunk<D, kMulti>(p, sh, 0, it.chunk), page = pf_tile<O>(it, j) * 8;
+            unsigned dead = __ballot_sync(0xffffffffu, lane < 8 && !pf_page_seen<O>(p, it, P, page + lane));
+            if (dead) {
+                const uint32_t vdst = sh.smem + G::kKVOffset + s * 2 * G::kTileBytes + G::kTileBytes;
+                for (; dead; dead &= dead - 1)
+                    for (int c = lane; c < G::kPageStride / 16; c += 32) sts_v4(vdst + (__ffs(dead) - 1) * G::kPageStride + c * 16, 0u, 0u, 0u, 0u);
+                fence_proxy_async_smem();
+            }
+        }
         if (first_dead < 128) {
             const uint32_t vdst = sh.smem + G::kKVOffset + s * 2 * G::kTileBytes + G::kTileBytes;
             const int chunks = (128 - first_dead) * 8;  // 16-byte pieces per 64-element block
@@ -764,7 +814,7 @@ struct PfScratch {
     volatile int* flags;  // shared memory, one int per tile: ticket value seen by the warpgroup's thread 0
 };
 
-template <int D, bool kMulti>
+template <int D, bool kMulti, Option O>
 __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const MixedParams& p, const PfShared& sh,
                                            const PfPlan& plan, const PfScratch& scr, const PfItem& it, int t,
                                            PfSoftmaxState& st) {
@@ -791,7 +841,8 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
         tc_fence_after_sync();
         // the whole row of S (128 fp32) in registers: one TMEM read per element
         uint32_t s[128];
-        const int limit = pos - j * 128 + 1;  // columns [0, limit) are attended
+        const int limit = pos - pf_tile<O>(it, j) * 128 + 1;  // columns [0, limit) are attended
+        const int from = limit - p.window, sinks = p.sinks - pf_tile<O>(it, j) * 128;   // kWindow: of those, from `from` on and below `sinks`
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
         tc_wait_ld();
@@ -800,7 +851,10 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
             __syncwarp();
             if (lane == 0) mbar_arrive(sh.bars + (kBarSFree + t) * 8);
         }
-        if (limit < 128) {
+        if (O == kWindow && from > 0 && sinks < 128) {
+#pragma unroll
+            for (int i = 0; i < 128; ++i) s[i] = i < limit && (i >= from || i < sinks) ? s[i] : 0xff800000u;
+        } else if (limit < 128) {
 #pragma unroll
             for (int i = 0; i < 128; ++i) s[i] = i < limit ? s[i] : 0xff800000u;  // -inf: exp2 gives exactly 0
         }
@@ -1046,7 +1100,7 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
 // ---- the prefill phase of one CTA ----------------------------------------------------------------------------------
 // `next` points at the scratch words from kMiscNext on: the idle warp fetches the following entry from the global counter while the
 // current one is processed and leaves it in next[iteration parity]; everyone reads it after the piece barrier.
-template <int D, bool kMulti>
+template <int D, bool kMulti, Option O>
 __device__ __forceinline__ void prefill_phase(const CUtensorMap* kv_map, const CUtensorMap* q_map, const CUtensorMap* out_map,
                                               const MixedParams& p, const PfShared& sh, const PfPlan& plan,
                                               const PfScratch& scr, int first_entry, volatile int* next) {
@@ -1069,13 +1123,13 @@ __device__ __forceinline__ void prefill_phase(const CUtensorMap* kv_map, const C
         setmaxnreg_dec<kPfRegsLight>();
         int entry = first_entry;
         for (int iter = 0; entry < plan.n_entries; ++iter) {
-            const PfItem it = pf_entry<kMulti>(p, plan, entry);
+            const PfItem it = pf_entry<kMulti, O>(p, plan, entry);
             if (warp == 0) {
-                if (it.j1 > it.j0) pf_produce<D, kMulti>(kv_map, q_map, p, sh, it, prod_kv_it);
+                if (it.j1 > it.j0) pf_produce<D, kMulti, O>(kv_map, q_map, p, sh, it, prod_kv_it);
             } else if (warp == 1) {
                 if (it.j1 > it.j0) PfGeo<D>::kAhead ? pf_mma_ahead<D>(p, sh, it, mma_state) : pf_mma<D>(p, sh, it, mma_state);
             } else if (warp == 2) {
-                if (it.j1 > it.j0) pf_sanitize<D, kMulti>(p, sh, it, san_kv_it);
+                if (it.j1 > it.j0) pf_sanitize<D, kMulti, O>(p, sh, it, san_kv_it);
                 // Near the end of what may be the CTA's last entry: whether the decode units have all been handed out (the CTAs
                 // that started with them have published their number).  Then the CTA need not work the decode plan out afterwards,
                 // which takes 2-3 us.  (Not with several chunks at head size 64: the compiler then makes every step of the
@@ -1100,8 +1154,8 @@ __device__ __forceinline__ void prefill_phase(const CUtensorMap* kv_map, const C
         setmaxnreg_inc<kPfRegsHeavy>();
         int entry = first_entry;
         for (int iter = 0; entry < plan.n_entries; ++iter) {
-            const PfItem it = pf_entry<kMulti>(p, plan, entry);
-            pf_softmax<D, kMulti>(out_map, p, sh, plan, scr, it, (warp - 4) >> 2, sm_state);
+            const PfItem it = pf_entry<kMulti, O>(p, plan, entry);
+            pf_softmax<D, kMulti, O>(out_map, p, sh, plan, scr, it, (warp - 4) >> 2, sm_state);
             if (!piece_sync()) break;
             entry = next[iter & 1];
         }
