@@ -171,14 +171,12 @@ sw_status sw_mixed_iteration_window_run(sw_ctx* ctx, void* kv_pool, const sw_bat
  * from the block.  Rows of different chunks or requests must lie on different pages, or the shared page holds anything afterwards
  * (append such rows by calls of their own).  Slots behind the new rows are left as they are.
  *
- * sw_kv8_attn_run is sw_mixed_attn_run over such a pool: its products see the values that the pool stands for exactly.  The scales must be
- * powers of two (between 2^-100 and 2^120) or NaN.  Iterations with chunks first copy the chunks' prompts to 16 bits, in `scratch` (256-byte aligned
- * device memory of sw_kv8_scratch_bytes(layout, sum over the chunks of ceil((P + C) / 16)) bytes, of no use between calls); decode-only
- * ones take no scratch (NULL, 0).  Both calls are asynchronous. */
-size_t sw_kv8_scratch_bytes(const sw_layout* layout, int64_t prompt_pages);
+ * sw_kv8_attn_run is sw_mixed_attn_run over such a pool.  The scales must be powers of two (between 2^-100 and 2^120) or NaN.  Its products see the
+ * values that the pool stands for exactly; queries are rounded at 2^-18 of their row's largest element, weights at 2^-40 of the largest.
+ * Both calls are asynchronous. */
 sw_status sw_kv8_append(sw_ctx* ctx, void* kv8_pool, float* scales, const sw_batch* batch, const void* k_new, const void* v_new, void* stream);
 sw_status sw_kv8_attn_run(sw_ctx* ctx, const void* kv8_pool, const float* scales, const sw_batch* batch, const void* q, void* out, float* lse,
-                          void* scratch, size_t scratch_bytes, void* stream);
+                          void* stream);
 
 /* Accumulated attention weights: fp32 [rows][num_kv_heads][capacity] (device), one row per sequence, one weight per KV head and position.
  * Request i of a batch uses row row_of[i] (device int32 [num_decode]); the requests of a call use different rows. */

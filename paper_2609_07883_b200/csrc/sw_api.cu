@@ -97,7 +97,7 @@ struct sw_ctx {
     std::vector<MapEntry> kv_maps;  // small cache: one entry per pool of a layer stack
     struct Kv8MapEntry {
         const void* pool;
-        CUtensorMap map;
+        sw::KvMaps maps;
     };
     Kv8MapEntry kv8_maps[128];   // likewise of 8-bit pools, the oldest replaced first
     int kv8_map_count = 0, kv8_map_next = 0;
@@ -533,40 +533,24 @@ sw_status sw_mixed_iteration_window_run(sw_ctx* ctx, void* kv_pool, const sw_bat
 
 // ---- the pool in 8 bits --------------------------------------------------------------------------------------------
 namespace {
-// Pages of 16 bits that the chunks' prompts take.
-int64_t prompt_pages(const Chunks& ch) {
-    int64_t pages = 0;
-    for (int j = 0; j < ch.n; ++j) pages += ((int64_t)ch.P[j] + ch.C[j] + sw::kPageSize - 1) / sw::kPageSize;
-    return pages;
-}
-size_t page_bytes(const sw_layout& l) { return (size_t)2 * l.num_kv_heads * sw::kPageSize * l.head_dim * 2; }
-size_t kv8_scratch(const sw_layout& l, int64_t pages) { return (size_t)pages * page_bytes(l) + align_up((size_t)pages * 4, 256); }
-
-sw_status kv8_map_for(sw_ctx* ctx, const void* pool, const CUtensorMap** out) {
+sw_status kv8_maps_for(sw_ctx* ctx, const void* pool, const sw::KvMaps** out) {
     for (int i = 0; i < ctx->kv8_map_count; ++i)
         if (ctx->kv8_maps[i].pool == pool) {
-            *out = &ctx->kv8_maps[i].map;
+            *out = &ctx->kv8_maps[i].maps;
             return SW_OK;
         }
     sw_ctx::Kv8MapEntry& e = ctx->kv8_maps[ctx->kv8_map_next];
     e.pool = nullptr;
-    CUresult r = sw::encode_kv8_page_map(ctx->encode, ctx->layout, pool, &e.map);
+    CUresult r = sw::encode_kv8_maps(ctx->encode, ctx->layout, pool, &e.maps);
     if (r != CUDA_SUCCESS) return sw_fail(SW_ERR_CUDA, "cuTensorMapEncodeTiled(8-bit pool) failed with CUresult %d", (int)r);
     e.pool = pool;
     constexpr int kMost = sizeof ctx->kv8_maps / sizeof ctx->kv8_maps[0];
     ctx->kv8_map_next = (ctx->kv8_map_next + 1) % kMost;
     ctx->kv8_map_count = std::min(ctx->kv8_map_count + 1, kMost);
-    *out = &e.map;
+    *out = &e.maps;
     return SW_OK;
 }
 }  // namespace
-
-size_t sw_kv8_scratch_bytes(const sw_layout* layout, int64_t prompt_pages) {
-    if (!layout || !layout_supported(*layout) || prompt_pages < 0 || prompt_pages > (int64_t)1 << 30 ||
-        2 * prompt_pages * layout->num_kv_heads >= (int64_t)1 << 31)
-        return 0;
-    return kv8_scratch(*layout, prompt_pages);
-}
 
 sw_status sw_kv8_append(sw_ctx* ctx, void* kv8_pool, float* scales, const sw_batch* batch, const void* k_new, const void* v_new, void* stream) {
     Chunks ch;
@@ -583,7 +567,7 @@ sw_status sw_kv8_append(sw_ctx* ctx, void* kv8_pool, float* scales, const sw_bat
 }
 
 sw_status sw_kv8_attn_run(sw_ctx* ctx, const void* kv8_pool, const float* scales, const sw_batch* batch, const void* q, void* out, float* lse,
-                          void* scratch, size_t scratch_bytes, void* stream) {
+                          void* stream) {
     const char* who = "sw_kv8_attn_run";
     Chunks ch;
     sw_status st = check_batch(ctx, batch, who, &ch);
@@ -594,43 +578,18 @@ sw_status sw_kv8_attn_run(sw_ctx* ctx, const void* kv8_pool, const float* scales
     if (st != SW_OK) return st;
     if (!aligned16(kv8_pool, q, out, scales)) return sw_fail(SW_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
     const sw_layout& l = ctx->layout;
-    const int64_t pages = prompt_pages(ch);
-    if (pages > (int64_t)1 << 30 || 2 * pages * l.num_kv_heads >= (int64_t)1 << 31)
-        return sw_fail(SW_ERR_UNSUPPORTED, "%s: the chunks' prompts have %lld pages", who, (long long)pages);
-    if (pages > 0 && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255) != 0 || scratch_bytes < kv8_scratch(l, pages)))
-        return sw_fail(SW_ERR_WORKSPACE, "%s: prompts of %lld pages take a 256-byte aligned scratch of %zu bytes", who, (long long)pages,
-                       kv8_scratch(l, pages));
-    const CUtensorMap* page_map = nullptr;
-    st = kv8_map_for(ctx, kv8_pool, &page_map);
+    const sw::KvMaps* maps = nullptr;
+    st = kv8_maps_for(ctx, kv8_pool, &maps);
     if (st != SW_OK) return st;
-    sw::KvMaps maps{*page_map, *page_map};
     sw::MixedParams p = mixed_params(ctx, batch, ch, q, out, lse);
     p.kv8_scales = scales;
     p.stage_us *= 0.5f;   // pages are half as long
     p.stages_per_us *= 2.f;
     p.steps_per_stage *= 0.5f;
-    CUtensorMap q_map = *page_map, out_map = *page_map;
-    if (pages > 0) {
-        __nv_bfloat16* copy = static_cast<__nv_bfloat16*>(scratch);
-        int32_t* list = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(scratch) + (size_t)pages * page_bytes(l));
-        const sw::AppendParams a = append_params(ctx, batch, ch, nullptr, nullptr, nullptr);
-        sw_layout copy_layout = l;
-        copy_layout.num_pages = pages;
-        sw::KvMaps copy_maps;
-        CUresult r = sw::encode_kv_maps(ctx->encode, copy_layout, copy, &copy_maps);
-        if (r != CUDA_SUCCESS) return sw_fail(SW_ERR_CUDA, "cuTensorMapEncodeTiled(scratch) failed with CUresult %d", (int)r);
-        maps.half = copy_maps.half;
-        st = encode_row_maps(ctx, p, &q_map, &out_map);
-        if (st != SW_OK) return st;
-        SW_CUDA(sw::launch_kv8_expand(a, ch.C, static_cast<const uint8_t*>(kv8_pool), scales, copy, list, ctx->num_sms,
-                                      static_cast<cudaStream_t>(stream)));
-        p.prefill_pages = list;
-        p.num_prefill_pages = (int)pages;
-        p.chunk_pages = pages;
-        for (int j = 0; j < ch.n; ++j) p.cPage0[j + 1] = p.cPage0[j] + (int)(((int64_t)ch.P[j] + ch.C[j] + sw::kPageSize - 1) / sw::kPageSize);
-        for (int j = ch.n; j < sw::kMaxChunks; ++j) p.cPage0[j + 1] = p.cPage0[ch.n];
-    }
-    SW_CUDA(sw::launch_kv8_attn(l.head_dim, maps, q_map, out_map, p, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+    CUtensorMap q_map = maps->half, out_map = maps->half;
+    st = encode_row_maps(ctx, p, &q_map, &out_map);
+    if (st != SW_OK) return st;
+    SW_CUDA(sw::launch_kv8_attn(l.head_dim, *maps, q_map, out_map, p, ctx->num_sms, static_cast<cudaStream_t>(stream)));
     return SW_OK;
 }
 

@@ -82,9 +82,8 @@ struct MixedParams {
     int32_t* pf_tickets; // [items][2]
     // launches with a window: the last `window` keys and the first `sinks` are attended
     int window, sinks, sink_pages;   // pages that hold a key below `sinks`
-    // launches over an 8-bit pool: fp32 [num_pages][2][Hkv]; pages of the chunks' 16-bit copy (prefill_pages lists those)
+    // launches over an 8-bit pool: fp32 [num_pages][2][Hkv]
     const float* kv8_scales;
-    int64_t chunk_pages;
     // launches that leave their scores behind: fp32 [score_pages][Hkv][16][group] by place in decode_pages
     float* scores;
     int64_t score_pages;
@@ -166,15 +165,20 @@ inline CUresult encode_kv_maps(EncodeTiledFn encode, const sw_layout& l, const v
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
-// Tensor map of an 8-bit pool: box = all of one head's K and V in a page, K's 16 slots first, swizzled by their row's length.
-inline CUresult encode_kv8_page_map(EncodeTiledFn encode, const sw_layout& l, const void* pool, CUtensorMap* out) {
+// Tensor maps of an 8-bit pool, swizzled by their rows' length: `page` as above, `half` one side of a head in a page.
+inline CUresult encode_kv8_maps(EncodeTiledFn encode, const sw_layout& l, const void* pool, KvMaps* out) {
     const cuuint64_t row = (cuuint64_t)l.head_dim, head = kPageSize * row, side = (cuuint64_t)l.num_kv_heads * head;
     const cuuint64_t dims[5] = {row, (cuuint64_t)kPageSize, 1, (cuuint64_t)2 * l.num_pages, (cuuint64_t)l.num_kv_heads};
     const cuuint64_t strides[4] = {row, head, side, head};
-    const cuuint32_t box[5] = {(cuuint32_t)l.head_dim, (cuuint32_t)kPageSize, 1, 2, 1}, ones[5] = {1, 1, 1, 1, 1};
-    return encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, const_cast<void*>(pool), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  l.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+    for (cuuint32_t sides = 1; sides <= 2; ++sides) {
+        const cuuint32_t box[5] = {(cuuint32_t)l.head_dim, (cuuint32_t)kPageSize, 1, sides, 1};
+        CUresult r = encode(sides == 2 ? &out->page : &out->half, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, const_cast<void*>(pool), dims, strides, box, ones,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, l.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r != CUDA_SUCCESS) return r;
+    }
+    return CUDA_SUCCESS;
 }
 
 // launchers (sw_kernels.cu)
@@ -208,8 +212,6 @@ cudaError_t configure_window_kernels(int head_dim);
 cudaError_t window_attn_resident_ctas_per_sm(int head_dim, int* out);
 // 8-bit pools (sw_kv8.cu)
 cudaError_t launch_kv8_append(const AppendParams& a, const int* cC, uint8_t* pool, float* scales, int num_sms, cudaStream_t stream);
-cudaError_t launch_kv8_expand(const AppendParams& a, const int* cC, const uint8_t* pool, const float* scales, __nv_bfloat16* copy, int32_t* list,
-                              int num_sms, cudaStream_t stream);
 cudaError_t launch_kv8_attn(int head_dim, const KvMaps& kv_maps, const CUtensorMap& q_map, const CUtensorMap& out_map, const MixedParams& p,
                             int num_sms, cudaStream_t stream);
 cudaError_t configure_kv8_kernels(int head_dim);

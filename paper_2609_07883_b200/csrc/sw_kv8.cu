@@ -1,11 +1,9 @@
-// The KV pool held in 8 bits: append, the chunks' 16-bit copy, and the mixed iteration that reads it (kernels of sw_mixed.cuh with kKv8).
+// The KV pool held in 8 bits: append, and the mixed iteration that reads it (kernels of sw_mixed.cuh with kKv8).
 //
 // Pool: e4m3 [num_pages][2 (K, V)][Hkv][16][D]; scales: fp32 [num_pages][2][Hkv], powers of two.  An element of a block (page, K|V, head)
 // stands for its e4m3 value times the block's scale.  A power of two costs a floating-point format no precision, and it makes two things
 // exact: every element is a bf16 number (the attention's products see exactly what the cache stands for), and a block whose scale has to
 // grow for a later row only moves its older rows' exponents (rounded again only where they become subnormal).
-#include <cuda_fp16.h>
-
 #include "sw_mixed.cuh"
 
 namespace sw {
@@ -16,30 +14,18 @@ constexpr int kKv8Threads = 256;
 // The blocks that an append writes, numbered: the pages of chunk 0 that get rows, of chunk 1, ..., then one of each decode request.
 struct Kv8Params {
     AppendParams a;
-    int block0[kMaxChunks + 1];   // written (expand: needed) pages before chunk j's
+    int block0[kMaxChunks + 1];   // written pages before chunk j's
     int cC[kMaxChunks];
     uint8_t* pool;
-    const float* scales_in;
     float* scales;
-    __nv_bfloat16* copy;
-    int32_t* list;
 };
 
-__device__ __forceinline__ uint32_t cvt_e4m3x4(float a, float b, float c, float d) {   // bytes a, b, c, d from the lowest on
-    uint16_t lo, hi;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
-    return (uint32_t)hi << 16 | lo;
-}
 __device__ __forceinline__ float bf16_lo(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
 // Four e4m3 values times `f`, back to e4m3.
 __device__ __forceinline__ uint32_t rescale_e4m3x4(uint32_t w, float f) {
-    uint32_t lo, hi;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(lo) : "h"((uint16_t)w));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hi) : "h"((uint16_t)(w >> 16)));
-    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo)), y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-    return cvt_e4m3x4(x.x * f, x.y * f, y.x * f, y.y * f);
+    const float2 x = f32x2_of_f16x2(f16x2_of_e4m3(w)), y = f32x2_of_f16x2(f16x2_of_e4m3(w >> 16));
+    return e4m3x4_of(x.x * f, x.y * f, y.x * f, y.y * f);
 }
 
 // sw_kv8_append: one warp per block.  The block's new rows (up to 16 of D elements) are held in registers, 16 bytes per lane and row, while
@@ -128,60 +114,9 @@ __global__ void __launch_bounds__(kKv8Threads) sw_kv8_append_kernel(const Kv8Par
             const int slot = i * kRows + sub;
             if (slot >= first && slot < last)
                 *reinterpret_cast<uint2*>(p.pool + (block * kPageSize + slot) * D + col) =
-                    make_uint2(cvt_e4m3x4(bf16_lo(x[i].x) * f, bf16_hi(x[i].x) * f, bf16_lo(x[i].y) * f, bf16_hi(x[i].y) * f),
-                               cvt_e4m3x4(bf16_lo(x[i].z) * f, bf16_hi(x[i].z) * f, bf16_lo(x[i].w) * f, bf16_hi(x[i].w) * f));
+                    make_uint2(e4m3x4_of(bf16_lo(x[i].x) * f, bf16_hi(x[i].x) * f, bf16_lo(x[i].y) * f, bf16_hi(x[i].y) * f),
+                               e4m3x4_of(bf16_lo(x[i].z) * f, bf16_hi(x[i].z) * f, bf16_lo(x[i].w) * f, bf16_hi(x[i].w) * f));
         }
-    }
-}
-
-// The prompts of the iteration's chunks as bf16 pages 0, 1, ... of `copy`, one prompt behind the other, and the list of those pages: what the
-// chunk-prefill tiles read in place of the 8-bit pool.  One warp per block; slots at or past the prompt's end become zeros.
-//
-// The tensor cores take bf16 operands here (queries and weights need them: e4m3 weights lose whatever is 2^-18 below the largest), so the 8-bit
-// keys have to be widened once per tile if not once per prompt.  Once per prompt costs 5 bytes of traffic an element, 4 % of the launch for 512 tokens
-// at prefix 28672, and leaves the tile pipeline as it is, whose shared memory (192 of 227 KB) and issue slots have no room for a converter.
-template <int D>
-__global__ void __launch_bounds__(kKv8Threads) sw_kv8_expand_kernel(const Kv8Params p) {
-    grid_launch_dependents();
-    grid_dependency_wait();
-    const int lane = threadIdx.x & 31, sides = 2 * p.a.Hkv;
-    const int64_t tasks = (int64_t)p.block0[p.a.nchunks] * sides;
-    for (int64_t t = (int64_t)blockIdx.x * (kKv8Threads / 32) + threadIdx.x / 32; t < tasks; t += (int64_t)gridDim.x * (kKv8Threads / 32)) {
-        const int b = (int)(t / sides), hs = (int)(t % sides);
-        int end = p.a.cP[0] + p.cC[0], at = 0, page0 = 0;
-#pragma unroll
-        for (int j = 1; j < kMaxChunks; ++j)
-            if (j < p.a.nchunks && b >= p.block0[j]) end = p.a.cP[j] + p.cC[j], at = p.block0[j], page0 = p.a.cPage0[j];
-        int page = p.a.prefill_pages[page0 + b - at];
-        if (page < 0 || (int64_t)page >= p.a.num_pages) {
-            if (lane == 0) report(p.a.ctrl, SW_ERR_OUT_OF_RANGE, kSiteAttnPage, b);
-            page = 0;
-        }
-        const int valid = end - (b - at) * kPageSize;
-        const int64_t block = (int64_t)page * sides + hs;
-        float rest;
-        const uint32_t factor = e4m3_factor(p.scales_in[block], rest), more = pack_bf16x2(rest, rest);
-        const uint8_t* src = p.pool + block * kPageSize * D;
-        __nv_bfloat16* dst = p.copy + ((int64_t)b * sides + hs) * kPageSize * D;
-        constexpr int kLoads = D / 32;
-        uint4 w[kLoads];
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) w[i] = __ldcs(reinterpret_cast<const uint4*>(src + (i * 32 + lane) * 16));
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const uint32_t in[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-            uint32_t out[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                out[j] = bf16x2_of_e4m3(in[j >> 1], in[j >> 1], j & 1 ? e4m3_pair(2, 3) : e4m3_pair(0, 1), factor);
-                if (rest != 1.f) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(out[j]) : "r"(out[j]), "r"(more));
-                if ((i * 32 + lane) / (D / 16) >= valid) out[j] = 0u;
-            }
-            uint4* to = reinterpret_cast<uint4*>(dst + (i * 32 + lane) * 16);
-            to[0] = make_uint4(out[0], out[1], out[2], out[3]);
-            to[1] = make_uint4(out[4], out[5], out[6], out[7]);
-        }
-        if (hs == 0 && lane == 0) p.list[b] = b;
     }
 }
 
@@ -214,23 +149,6 @@ cudaError_t launch_kv8_append(const AppendParams& a, const int* cC, uint8_t* poo
     const int64_t tasks = (int64_t)(p.block0[a.nchunks] + a.n) * 2 * a.Hkv;
     return a.D == 64 ? launch_blocks(sw_kv8_append_kernel<64>, p, tasks, num_sms, stream)
                      : launch_blocks(sw_kv8_append_kernel<128>, p, tasks, num_sms, stream);
-}
-
-cudaError_t launch_kv8_expand(const AppendParams& a, const int* cC, const uint8_t* pool, const float* scales, __nv_bfloat16* copy, int32_t* list,
-                              int num_sms, cudaStream_t stream) {
-    Kv8Params p{};
-    p.a = a;
-    p.pool = const_cast<uint8_t*>(pool);
-    p.scales_in = scales;
-    p.copy = copy;
-    p.list = list;
-    for (int j = 0; j < a.nchunks; ++j) {
-        p.cC[j] = cC[j];
-        p.block0[j + 1] = p.block0[j] + (int)(((int64_t)a.cP[j] + cC[j] - 1) / kPageSize) + 1;
-    }
-    const int64_t tasks = (int64_t)p.block0[a.nchunks] * 2 * a.Hkv;
-    return a.D == 64 ? launch_blocks(sw_kv8_expand_kernel<64>, p, tasks, num_sms, stream)
-                     : launch_blocks(sw_kv8_expand_kernel<128>, p, tasks, num_sms, stream);
 }
 
 cudaError_t configure_kv8_kernels(int head_dim) { return configure_option<kKv8>(head_dim); }

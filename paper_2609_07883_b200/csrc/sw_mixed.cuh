@@ -13,6 +13,7 @@
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
 #include "sw_internal.h"
@@ -763,6 +764,13 @@ __device__ __forceinline__ uint32_t f16x2_of_e4m3(uint32_t pair) {   // of the l
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(d) : "h"((uint16_t)pair));
     return d;
 }
+__device__ __forceinline__ float2 f32x2_of_f16x2(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
+__device__ __forceinline__ uint32_t e4m3x4_of(float a, float b, float c, float d) {   // bytes a, b, c, d from the lowest on
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+    return (uint32_t)hi << 16 | lo;
+}
 // D(16x8, f32) += A(16x16, f16, row) * B(16x8, f16, col)
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -835,26 +843,6 @@ struct PageExtra {
     float2 scale;
     float* scores;
 };
-
-// Two e4m3 values (bytes `sel` of the words a and b, and their signs in between) as bf16, times `scale`.  An e4m3 is a bf16 whose exponent is
-// 120 too small once its seven lower bits are moved up by four, subnormal values included, so one exact product with 2^120 times the page's
-// scale, a power of two, gives the value that the cache stands for.
-__device__ __forceinline__ uint32_t bf16x2_of_e4m3(uint32_t a, uint32_t b, uint32_t sel, uint32_t scale) {
-    uint32_t x;
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(x) : "r"(a), "r"(b), "r"(sel));
-    x = (x << 4) & 0x87f087f0u;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(scale));
-    return x;
-}
-__device__ __forceinline__ constexpr uint32_t e4m3_pair(int i, int j) {   // bytes i and j (0-3 of the first word, 4-7 of the second) for it
-    return (uint32_t)((8 | j) << 12 | j << 8 | (8 | i) << 4 | i);
-}
-// scale * 2^120 as two bf16, with what is beyond their range (scales above 2^7) left for `rest`
-__device__ __forceinline__ uint32_t e4m3_factor(float scale, float& rest) {
-    rest = scale > 128.f ? scale * 0.0078125f : 1.f;
-    const float f = (scale > 128.f ? 128.f : scale) * 1.329227995784916e36f;   // 2^120
-    return pack_bf16x2(f, f);
-}
 
 template <int D, Option O>
 __device__ __forceinline__ void attend_page(const MixedParams& p, uint32_t sK, int valid, const uint32_t (&qb)[D / 16][2], DecodeState<D>& st,
@@ -1608,7 +1596,7 @@ __global__ void __launch_bounds__(kThreads, 1) sw_mixed_attn_kernel(const __grid
                                                                     const __grid_constant__ CUtensorMap q_map,
                                                                     const __grid_constant__ CUtensorMap out_map,
                                                                     const MixedParams p) {
-    static_assert(PfGeo<D>::kBytes <= Geo<D>::kRingBytes, "prefill tiles must fit the region shared with the decode ring");
+    static_assert(PfGeo<D>::kBytes <= Geo<D>::kRingBytes && PfGeo8<D>::kBytes <= Geo<D>::kRingBytes, "prefill tiles must fit the region shared with the decode ring");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
@@ -1635,7 +1623,7 @@ __global__ void __launch_bounds__(kThreads, 1) sw_mixed_attn_kernel(const __grid
             tma_prefetch_desc(&kv_map);
             tma_prefetch_desc(&q_map);
             tma_prefetch_desc(&out_map);
-            pf_init_barriers(base + Geo<D>::kPfBarOffset);
+            pf_init_barriers<O>(base + Geo<D>::kPfBarOffset);
         }
         misc[kMiscTmem] = 0;
         misc[kMiscAbort] = 0;

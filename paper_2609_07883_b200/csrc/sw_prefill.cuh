@@ -39,11 +39,28 @@ struct PfGeo {
     static constexpr int kPColumn = kAhead ? 256 : 0, kPStride = kAhead ? 64 : 128, kOColumn = kAhead ? 384 : 256;
 };
 
+// kKv8: the same region holds, in tiles of 128 rows of D bytes, Q of both tiles as two e4m3 parts, two stages of K as it lies in the pool, two
+// stages of V likewise, and two stages of V as f16 operand tiles (into which Q's bf16 rows land first).  32 floats of scales for K, then for V,
+// of the pages of four stages lie where launches with a fused append list last pages.
+template <int D>
+struct PfGeo8 {
+    static constexpr int kRowTile = 128 * D;
+    static constexpr int kKOffset = 4 * kRowTile, kRawOffset = 6 * kRowTile, kVOffset = 8 * kRowTile, kBytes = 12 * kRowTile;
+    static constexpr int kScaleStages = 4, kVScales = kScaleStages * 8 * 4;
+    static_assert(PfGeo<D>::kQOffset == 0 && PfGeo<D>::kTileBytes == 2 * kRowTile, "the two parts of a tile's Q lie where its bf16 rows would");
+};
+// 16-byte chunk c of row r of a tile of D-byte rows, swizzled by the row's length
+template <int D>
+__device__ __forceinline__ constexpr uint32_t row8_chunk(int r, int c) {
+    return (uint32_t)(r * D + ((D == 128 ? c ^ (r & 7) : c ^ (r >> 1 & 3)) << 4));
+}
+
 // P of a tile is handed to the MMA warp in two halves (keys 0-63, then 64-127) so that the first four P V
 // instructions run while the second half is still being exponentiated.
 enum PfBar {
     kBarQFull = 0, kBarKFull = 1, kBarVLanded = 3, kBarVFull = 5, kBarKEmpty = 7, kBarVEmpty = 9,
-    kBarSFull = 11, kBarPHalf = 13 /* [tile][half] */, kBarODone = 17, kBarSFree = 19 /* kAhead */, kPfBars = 21
+    kBarSFull = 11, kBarPHalf = 13 /* [tile][half] */, kBarODone = 17, kBarSFree = 19 /* kAhead */, kPfBars = 21,
+    kBarQReady = 21 /* kKv8: [tile] */, kBarRawEmpty = 23, kPfBars8 = 25
 };
 
 // register budgets per warpgroup during the prefill phase: 128 * 72 + 256 * 216 <= 384 * 168
@@ -72,8 +89,18 @@ __device__ __forceinline__ int pf_chunk(const MixedParams& p, const PfShared& sh
     }
 }
 
+template <Option O>
 __device__ __forceinline__ void pf_init_barriers(uint32_t bars) {
-    for (int i = 0; i < kPfBars; ++i) mbar_init(bars + i * 8, ((i >= kBarPHalf && i < kBarPHalf + 4) || i >= kBarSFree) ? 4 : 1);
+    // arrivals: four softmax warps of a tile; kKv8: all eight, which convert V
+    for (int i = 0; i < (O == kKv8 ? kPfBars8 : kPfBars); ++i)
+        mbar_init(bars + i * 8, ((i >= kBarPHalf && i < kBarPHalf + 4) || (i >= kBarSFree && i < kBarRawEmpty)) ? 4
+                                : (O == kKv8 && (i >= kBarRawEmpty || i == kBarVFull || i == kBarVFull + 1)) ? 8 : 1);
+}
+// V's operand tile of a stage
+template <int D, Option O>
+__device__ __forceinline__ uint32_t pf_v_tile(const PfShared& sh, uint32_t s) {
+    using G = PfGeo<D>;
+    return O == kKv8 ? sh.smem + PfGeo8<D>::kVOffset + s * G::kTileBytes : sh.smem + G::kKVOffset + s * 2 * G::kTileBytes + G::kTileBytes;
 }
 
 // Bounded wait that also gives up when another role of this CTA has given up.
@@ -533,14 +560,15 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
     // The whole warp runs the role: lane i owns page i of every 128-key tile (its page id, its TMA boxes), so the
     // eight pages of a tile are issued by one instruction instead of a loop of one thread.
     const int lane = threadIdx.x & 31;
-    // Q tiles (rows past the chunk are zero-filled by the tensor map's bounds)
+    // Q tiles (rows past the chunk are zero-filled by the tensor map's bounds); kKv8: into V's operand tiles, whose first rows are made after
+    // the softmax warps have split Q
     if (lane == 0) {
         const int active = (it.nkv[0] > it.j0) + (it.nkv[1] > it.j0);
         mbar_arrive_expect_tx(sh.bars + kBarQFull * 8, active * G::kTileBytes);
         for (int t = 0; t < 2; ++t)
             if (it.nkv[t] > it.j0)
                 for (int h = 0; h < G::kHalves; ++h)
-                    tma_load_3d(sh.smem + G::kQOffset + t * G::kTileBytes + h * G::kHalfBytes, q_map, sh.bars + kBarQFull * 8,
+                    tma_load_3d((O == kKv8 ? pf_v_tile<D, O>(sh, t) : sh.smem + G::kQOffset + t * G::kTileBytes) + h * G::kHalfBytes, q_map, sh.bars + kBarQFull * 8,
                                 h * 64, it.kvh * p.group, pf_chunk<D, kMulti>(p, sh, 2, it.chunk) + it.tok0[t]);
     }
     // fused launch: tiles that reach into the chunk's own keys wait until every CTA has written its share of them
@@ -556,7 +584,7 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
     auto id_of = [&](int step) {
         const int page = pf_tile<O>(it, step) * 8 + lane;
         int id = (lane < 8 && seen(page)) ? p.prefill_pages[pf_chunk<D, kMulti>(p, sh, 3, it.chunk) + page] : 0;
-        if (id < 0 || (int64_t)id >= (O == kKv8 ? p.chunk_pages : p.num_pages)) {
+        if (id < 0 || (int64_t)id >= p.num_pages) {
             // reported, and page 0 fetched in its place: a bad id never reaches the copy engine
             report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteAttnPage, it.item);
             id = 0;
@@ -564,30 +592,65 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
         return id;
     };
     int id_next = id_of(it.j0);
-    for (int j = it.j0; j < it.j1; ++j, ++kv_it) {
-        const uint32_t s = kv_it & 1, n = kv_it >> 1;
-        const int id = id_next;
-        if (j + 1 < it.j1) id_next = id_of(j + 1);  // in flight while this tile is issued
-        const int tile = pf_tile<O>(it, j);
-        int nvp = min(8, npages - tile * 8);
-        bool mine = lane < nvp;
-        if constexpr (O == kWindow) {
-            mine = mine && seen(tile * 8 + lane);
-            nvp = __popc(__ballot_sync(0xffffffffu, mine));
+    if constexpr (O == kKv8) {
+        using G8 = PfGeo8<D>;
+        auto scales_of = [&](int id) {
+            const float* at = p.kv8_scales + (int64_t)id * 2 * p.Hkv + it.kvh;
+            return make_float2(__ldg(at), __ldg(at + p.Hkv));
+        };
+        int id_after = it.j0 + 1 < it.j1 ? id_of(it.j0 + 1) : 0;
+        float2 scale_next = scales_of(id_next);
+        for (int j = it.j0; j < it.j1; ++j, ++kv_it) {
+            const uint32_t s = kv_it & 1, n = kv_it >> 1;
+            const int id = id_next, nvp = min(8, npages - j * 8);
+            const float2 scale = scale_next;
+            id_next = id_after;
+            if (j + 1 < it.j1) scale_next = scales_of(id_next);
+            if (j + 2 < it.j1) id_after = id_of(j + 2);
+            if (!pf_wait(sh, kBarKEmpty + s, (n & 1) ^ 1, p.ctrl, 1)) return false;
+            if (lane < 8) {
+                const uint32_t at = sh.smem + Geo<D>::kLastOffset + ((kv_it % G8::kScaleStages) * 8 + lane) * 4;
+                sts_f32(at, scale.x);
+                sts_f32(at + G8::kVScales, lane < nvp ? scale.y : 0.f);   // (pages past the prompt do not count)
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive_expect_tx(sh.bars + (kBarKFull + s) * 8, nvp * kPageSize * D);
+            __syncwarp();
+            if (lane < nvp)
+                tma_load_5d(sh.smem + G8::kKOffset + s * G8::kRowTile + lane * kPageSize * D, kv_map, sh.bars + (kBarKFull + s) * 8, 0, 0, 0, 2 * id, it.kvh);
+            if (!pf_wait(sh, kBarRawEmpty + s, (n & 1) ^ 1, p.ctrl, 2)) return false;
+            if (lane == 0) mbar_arrive_expect_tx(sh.bars + (kBarVLanded + s) * 8, nvp * kPageSize * D);
+            __syncwarp();
+            if (lane < nvp)
+                tma_load_5d(sh.smem + G8::kRawOffset + s * G8::kRowTile + lane * kPageSize * D, kv_map, sh.bars + (kBarVLanded + s) * 8, 0, 0, 0,
+                            2 * id + 1, it.kvh);
         }
-        const uint32_t kdst = sh.smem + G::kKVOffset + s * 2 * G::kTileBytes;
-        const uint32_t vdst = kdst + G::kTileBytes;
-        if (!pf_wait(sh, kBarKEmpty + s, (n & 1) ^ 1, p.ctrl, 1)) return false;
-        if (lane == 0) mbar_arrive_expect_tx(sh.bars + (kBarKFull + s) * 8, nvp * G::kPageStride);
-        __syncwarp();
-        if (mine)
-            tma_load_5d(kdst + lane * G::kPageStride, kv_map, sh.bars + (kBarKFull + s) * 8, 0, 0, 0, 0, (2 * id) * p.Hkv + it.kvh);
-        if (!pf_wait(sh, kBarVEmpty + s, (n & 1) ^ 1, p.ctrl, 2)) return false;
-        if (lane == 0) mbar_arrive_expect_tx(sh.bars + (kBarVLanded + s) * 8, nvp * G::kPageStride);
-        __syncwarp();
-        if (mine)
-            tma_load_5d(vdst + lane * G::kPageStride, kv_map, sh.bars + (kBarVLanded + s) * 8, 0, 0, 0, 0,
-                        (2 * id + 1) * p.Hkv + it.kvh);
+    } else {
+        for (int j = it.j0; j < it.j1; ++j, ++kv_it) {
+            const uint32_t s = kv_it & 1, n = kv_it >> 1;
+            const int id = id_next;
+            if (j + 1 < it.j1) id_next = id_of(j + 1);  // in flight while this tile is issued
+            const int tile = pf_tile<O>(it, j);
+            int nvp = min(8, npages - tile * 8);
+            bool mine = lane < nvp;
+            if constexpr (O == kWindow) {
+                mine = mine && seen(tile * 8 + lane);
+                nvp = __popc(__ballot_sync(0xffffffffu, mine));
+            }
+            const uint32_t kdst = sh.smem + G::kKVOffset + s * 2 * G::kTileBytes;
+            const uint32_t vdst = kdst + G::kTileBytes;
+            if (!pf_wait(sh, kBarKEmpty + s, (n & 1) ^ 1, p.ctrl, 1)) return false;
+            if (lane == 0) mbar_arrive_expect_tx(sh.bars + (kBarKFull + s) * 8, nvp * G::kPageStride);
+            __syncwarp();
+            if (mine)
+                tma_load_5d(kdst + lane * G::kPageStride, kv_map, sh.bars + (kBarKFull + s) * 8, 0, 0, 0, 0, (2 * id) * p.Hkv + it.kvh);
+            if (!pf_wait(sh, kBarVEmpty + s, (n & 1) ^ 1, p.ctrl, 2)) return false;
+            if (lane == 0) mbar_arrive_expect_tx(sh.bars + (kBarVLanded + s) * 8, nvp * G::kPageStride);
+            __syncwarp();
+            if (mine)
+                tma_load_5d(vdst + lane * G::kPageStride, kv_map, sh.bars + (kBarVLanded + s) * 8, 0, 0, 0, 0,
+                            (2 * id + 1) * p.Hkv + it.kvh);
+        }
     }
     return true;
 }
@@ -631,17 +694,118 @@ __device__ __forceinline__ bool pf_sanitize(const MixedParams& p, const PfShared
     return true;
 }
 
+// ---- kKv8: V from e4m3 to f16 (the eight softmax warps, a page each) -----------------------------------------------
+// K goes to the tensor cores as it lies in the pool, against Q in two e4m3 parts.  The weights P need more than e4m3's 18 binary orders of
+// magnitude, so P V has f16 operands, and V's rows are widened once per tile, by the softmax warps: they wait for S half of the time.  (Two
+// warps of their own took 3900 cycles a tile, with the shared memory as busy as the tensor cores keep it, beside the others' 2500.)
+//
+// O is kept in units of a scale `ref` that follows the largest scale of the tile's eight pages: upward beyond 2^3 times ref (P 2^7 may
+// reach 2^15, V 448 2^3), downward below 2^-12 of it, for which the softmax warps multiply O; a page's ratio to ref goes into its rows of V, exactly
+// down to 2^-15.  Everybody works ref out from the scales.  `top`: its largest value; a tile 2^-80 below it is not followed.
+constexpr float kPfWeightBits = 7.f;   // P is 2^7 times the weight
+struct PfValueScale {
+    float ref = 0.f, top = 0.f;
+    float v[8];   // of the tile's pages
+    // Takes the step's scales; returns what O has to be multiplied with (1: ref stays).
+    __device__ __forceinline__ float follow(uint32_t scales, bool first) {
+        const float4 a = lds_f4(scales), b = lds_f4(scales + 16);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        const float most = fmaxf(max3(fmaxf(v[0], v[1]), v[2], v[3]), max3(fmaxf(v[4], v[5]), v[6], v[7]));   // (NaN does not count)
+        if (first) {
+            ref = top = most;
+        } else if (most > ref * 8.f || (most < ref * 0x1p-12f && most >= top * 0x1p-80f)) {
+            const float f = ref / most;
+            ref = most;
+            top = fmaxf(top, most);
+            return f;
+        }
+        return 1.f;
+    }
+};
+template <int D>
+__device__ __forceinline__ uint32_t pf_value_scales(const PfShared& sh, uint32_t kv_it) {
+    return sh.smem + Geo<D>::kLastOffset + PfGeo8<D>::kVScales + (kv_it % PfGeo8<D>::kScaleStages) * 32;
+}
+// The warp's page of step j; kv_it: the step's number on this CTA.
+template <int D>
+__device__ __forceinline__ bool pf_convert(const MixedParams& p, const PfShared& sh, PfValueScale& vs, int j, bool first, uint32_t kv_it, int kv_total) {
+    using G = PfGeo<D>;
+    using G8 = PfGeo8<D>;
+    constexpr int kChunks = D / 16, kLoads = D / 32;   // 16-byte chunks of a row, per lane
+    const int lane = threadIdx.x & 31, page = (threadIdx.x >> 5) - 4;
+    const uint32_t s = kv_it & 1, n = kv_it >> 1;
+    if (!pf_wait(sh, kBarVLanded + s, n & 1, p.ctrl, 3)) return false;
+    const uint32_t raw = sh.smem + G8::kRawOffset + s * G8::kRowTile, dst = pf_v_tile<D, kKv8>(sh, s);
+    uint32_t w[kLoads][4];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int row = page * kPageSize + (i * 32 + lane) / kChunks, c = (i * 32 + lane) % kChunks;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3])
+                     : "r"(raw + row8_chunk<D>(row, c)) : "memory");
+    }
+    vs.follow(pf_value_scales<D>(sh, kv_it), first);
+    const float scale = lds_f32(pf_value_scales<D>(sh, kv_it) + page * 4);
+    const int live = kv_total - j * 128;   // rows of the tile inside the prompt
+    const bool plain = scale == vs.ref && (page + 1) * kPageSize <= live;   // warp-uniform
+    if (!pf_wait(sh, kBarVEmpty + s, (n & 1) ^ 1, p.ctrl, 13)) return false;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int row = page * kPageSize + (i * 32 + lane) / kChunks, c = (i * 32 + lane) % kChunks;
+        uint32_t x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = f16x2_of_e4m3(e & 1 ? w[i][e >> 1] >> 16 : w[i][e >> 1]);
+        if (!plain) {
+            const uint32_t ratio = pack_f16x2(scale / vs.ref, scale / vs.ref);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(x[e]) : "r"(x[e]), "r"(ratio));
+                if (row >= live) x[e] = 0u;
+            }
+        }
+        // 16-byte pieces 2 c and 2 c + 1 of the row; lanes of the row's second block write theirs in the other order, which keeps the
+        // eight lanes of a row off one another's banks
+        const uint32_t to = dst + (row >> 3) * G::kGroupStride + (c >> 2) * G::kAtomBytes + (row & 7) * 128;
+        const bool second = (c & 4) != 0;
+        const uint32_t a0 = to + (((2 * c & 7) + second ^ (row & 7)) << 4), a1 = to + (((2 * c & 7) + !second ^ (row & 7)) << 4);
+        sts_v4(a0, second ? x[4] : x[0], second ? x[5] : x[1], second ? x[6] : x[2], second ? x[7] : x[3]);
+        sts_v4(a1, second ? x[0] : x[4], second ? x[1] : x[5], second ? x[2] : x[6], second ? x[3] : x[7]);
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+        mbar_arrive(sh.bars + (kBarRawEmpty + s) * 8);
+        mbar_arrive(sh.bars + (kBarVFull + s) * 8);
+    }
+    return true;
+}
+
 // ---- role: MMA issuer (one thread) ------------------------------------------------------------------------------
 struct PfMmaState {
     uint32_t kv_it = 0, q_it = 0;
-    uint32_t p_cnt[2] = {0, 0};
+    uint32_t p_cnt[2] = {0, 0}, q_cnt[2] = {0, 0};
 };
 
 // The whole MMA warp runs this role in lockstep (waits included) so that addresses and descriptors stay in uniform
 // registers; only the tcgen05.mma / tcgen05.commit instructions themselves are issued by the one elected lane.
-template <int D>
+template <int D, Option O>
 __device__ __forceinline__ void pf_issue_qk(const PfShared& sh, int t, uint32_t s, bool leader) {
     using G = PfGeo<D>;
+    if constexpr (O == kKv8) {   // S = Q_high K^T + Q_low K^T, 32 elements (bytes) an instruction
+        constexpr uint32_t idesc8 = umma_idesc_e4m3(128, 128);
+        using G8 = PfGeo8<D>;
+        auto desc = [](uint32_t at) { return D == 128 ? umma_desc_sw128(at, 16, 8 * D) : umma_desc_sw64(at, 16, 8 * D); };
+        const uint64_t high = desc(sh.smem + 2 * t * G8::kRowTile), low = desc(sh.smem + (2 * t + 1) * G8::kRowTile);
+        const uint64_t kd8 = desc(sh.smem + G8::kKOffset + s * G8::kRowTile);
+        if (leader) {
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) {
+                tc_mma_ss_f8(sh.tmem + t * 128, high + ks * 2, kd8 + ks * 2, idesc8, ks > 0);
+                tc_mma_ss_f8(sh.tmem + t * 128, low + ks * 2, kd8 + ks * 2, idesc8, 1);
+            }
+            tc_commit(sh.bars + (kBarSFull + t) * 8);
+        }
+        return;
+    }
     constexpr uint32_t idesc = umma_idesc_bf16(128, 128, 0, 0);
     const uint64_t qd = umma_desc_sw128(sh.smem + G::kQOffset + t * G::kTileBytes, 16, 1024);
     const uint64_t kd = umma_desc_sw128(sh.smem + G::kKVOffset + s * 2 * G::kTileBytes, 16, G::kGroupStride);
@@ -660,12 +824,11 @@ __device__ __forceinline__ void pf_issue_qk(const PfShared& sh, int t, uint32_t 
 
 // one half of O_t += P_t V: keys [64 * half, 64 * half + 64), 16 keys = one page per instruction (its two 8-key groups
 // are one group stride apart, the 64-element blocks of a row one block apart)
-template <int D>
+template <int D, Option O>
 __device__ __forceinline__ void pf_issue_pv_half(const PfShared& sh, int t, uint32_t s, int half, bool first, bool leader) {
     using G = PfGeo<D>;
-    constexpr uint32_t idesc = umma_idesc_bf16(128, D, 0, 1);  // B = V is MN-major: [key][d] with d contiguous
-    const uint64_t vd = umma_desc_sw128(sh.smem + G::kKVOffset + s * 2 * G::kTileBytes + G::kTileBytes + half * 4 * G::kPageStride,
-                                        G::kAtomBytes, G::kGroupStride);
+    constexpr uint32_t idesc = O == kKv8 ? umma_idesc_f16(128, D, 0, 1) : umma_idesc_bf16(128, D, 0, 1);  // B = V is MN-major: [key][d] with d contiguous
+    const uint64_t vd = umma_desc_sw128(pf_v_tile<D, O>(sh, s) + half * 4 * G::kPageStride, G::kAtomBytes, G::kGroupStride);
     const uint32_t d_tmem = sh.tmem + G::kOColumn + t * D;
     const uint32_t p_tmem = sh.tmem + G::kPColumn + t * G::kPStride + half * 32;
     const uint32_t acc_first = first && half == 0 ? 0u : 1u;
@@ -677,7 +840,22 @@ __device__ __forceinline__ void pf_issue_pv_half(const PfShared& sh, int t, uint
     }
 }
 
-template <int D>
+// The entry's Q tiles are there (kKv8: split in two parts by their softmax warps).
+template <Option O>
+__device__ __forceinline__ bool pf_wait_q(const MixedParams& p, const PfShared& sh, const PfItem& it, PfMmaState& st) {
+    if constexpr (O == kKv8) {
+        for (int t = 0; t < 2; ++t)
+            if (it.nkv[t] > it.j0) {
+                if (!pf_wait(sh, kBarQReady + t, st.q_cnt[t] & 1, p.ctrl, 4)) return false;
+                st.q_cnt[t] += 1;
+            }
+        return true;
+    } else {
+        return pf_wait(sh, kBarQFull, st.q_it & 1, p.ctrl, 4);
+    }
+}
+
+template <int D, Option O>
 __device__ __forceinline__ bool pf_mma(const MixedParams& p, const PfShared& sh, const PfItem& it, PfMmaState& st) {
     const bool leader = elect_one();
     auto act = [&](int t, int j) { return j < it.j1 && j < it.nkv[t]; };
@@ -685,13 +863,13 @@ __device__ __forceinline__ bool pf_mma(const MixedParams& p, const PfShared& sh,
     auto commit = [&](int bar) {
         if (leader) tc_commit(sh.bars + bar * 8);
     };
-    if (!pf_wait(sh, kBarQFull, st.q_it & 1, p.ctrl, 4)) return false;
+    if (!pf_wait_q<O>(p, sh, it, st)) return false;
     {
         const uint32_t s = st.kv_it & 1, n = st.kv_it >> 1;
         if (!pf_wait(sh, kBarKFull + s, n & 1, p.ctrl, 5)) return false;
         tc_fence_after_sync();
         for (int t = 0; t < 2; ++t)
-            if (act(t, it.j0)) pf_issue_qk<D>(sh, t, s, leader);
+            if (act(t, it.j0)) pf_issue_qk<D, O>(sh, t, s, leader);
         commit(kBarKEmpty + s);
     }
     for (int j = it.j0; j < it.j1; ++j) {
@@ -705,7 +883,7 @@ __device__ __forceinline__ bool pf_mma(const MixedParams& p, const PfShared& sh,
                 for (int half = 0; half < 2; ++half) {
                     if (!pf_wait(sh, kBarPHalf + 2 * t + half, st.p_cnt[t] & 1, p.ctrl, 8)) return false;
                     tc_fence_after_sync();
-                    pf_issue_pv_half<D>(sh, t, s, half, j == it.j0, leader);
+                    pf_issue_pv_half<D, O>(sh, t, s, half, j == it.j0, leader);
                 }
                 st.p_cnt[t] += 1;
             }
@@ -715,7 +893,7 @@ __device__ __forceinline__ bool pf_mma(const MixedParams& p, const PfShared& sh,
                     if (!pf_wait(sh, kBarKFull + (s ^ 1), ((cur + 1) >> 1) & 1, p.ctrl, 7)) return false;
                     k_ready = true;
                 }
-                pf_issue_qk<D>(sh, t, s ^ 1, leader);
+                pf_issue_qk<D, O>(sh, t, s ^ 1, leader);
             }
             if (more && t == last_active(j + 1)) commit(kBarKEmpty + (s ^ 1));
         }
@@ -730,7 +908,7 @@ __device__ __forceinline__ bool pf_mma(const MixedParams& p, const PfShared& sh,
 // us, 1000 + 512 of 8/2/64 21.9 -> 21.3, 256 + 128 12.3 -> 12.1; 4000 + 64, in pieces of one step, 23.4 -> 23.8.  (Entries of up to four steps
 // in the plain order, both in one kernel: 23.4, but 256 + 128 beside four contexts 13.1 -> 14.4.  One rolled loop over (step, tile)
 // with the same order: 76.7 -> 86.)
-template <int D>
+template <int D, Option O>
 __device__ __forceinline__ bool pf_mma_ahead(const MixedParams& p, const PfShared& sh, const PfItem& it, PfMmaState& st) {
     const bool leader = elect_one();
     auto act = [&](int t, int j) { return j < it.j1 && j < it.nkv[t]; };
@@ -744,11 +922,11 @@ __device__ __forceinline__ bool pf_mma_ahead(const MixedParams& p, const PfShare
         if ((t == 0 || !act(0, j)) && !pf_wait(sh, kBarKFull + s, (cur >> 1) & 1, p.ctrl, 5)) return false;
         if (used && !pf_wait(sh, kBarSFree + t, st.p_cnt[t] & 1, p.ctrl, 7)) return false;
         tc_fence_after_sync();
-        pf_issue_qk<D>(sh, t, s, leader);
+        pf_issue_qk<D, O>(sh, t, s, leader);
         if (t == 1 || !act(1, j)) commit(kBarKEmpty + s);
         return true;
     };
-    if (!pf_wait(sh, kBarQFull, st.q_it & 1, p.ctrl, 4)) return false;
+    if (!pf_wait_q<O>(p, sh, it, st)) return false;
     const int j0 = it.j0;
     if (act(0, j0) && !issue_qk(0, j0, false)) return false;
     if (act(1, j0) && !issue_qk(1, j0, false)) return false;
@@ -763,7 +941,7 @@ __device__ __forceinline__ bool pf_mma_ahead(const MixedParams& p, const PfShare
                 for (int half = 0; half < 2; ++half) {
                     if (!pf_wait(sh, kBarPHalf + 2 * t + half, st.p_cnt[t] & 1, p.ctrl, 8)) return false;
                     tc_fence_after_sync();
-                    pf_issue_pv_half<D>(sh, t, s, half, j == j0, leader);
+                    pf_issue_pv_half<D, O>(sh, t, s, half, j == j0, leader);
                 }
                 st.p_cnt[t] += 1;
                 if (t == 1 || !act(1, j)) commit(kBarVEmpty + s);
@@ -803,7 +981,48 @@ __device__ __forceinline__ void pf_exp2_pair_fma(uint64_t x2, float& p0, float& 
 
 struct PfSoftmaxState {
     uint32_t s_cnt = 0, o_cnt = 0;  // completions of this tile's S-ready / O-updated barriers consumed so far
+    uint32_t kv_it = 0, q_it = 0, q_cnt[2] = {0, 0};   // kKv8: steps and entries of the CTA before this entry; entries with rows in a tile
 };
+
+// kKv8: the thread's row of Q, bf16 in V's operand tile, as the sum of two e4m3 rows.  The row is scaled by a power of two to below 2^8 first; what the
+// larger part (4 significant bits) leaves of a bf16 element (8 bits) fits the smaller one exactly, but for what is 2^-18 of the row's largest
+// element.  Returns the scale to multiply scores with (NaN where the row holds anything that is not finite).
+template <int D>
+__device__ __forceinline__ float pf_split_q(const PfShared& sh, int t, int row) {
+    using G = PfGeo<D>;
+    const uint32_t src = pf_v_tile<D, kKv8>(sh, t) + row * 128;
+    uint32_t x[D / 2], top = 0;
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[4 * c]), "=r"(x[4 * c + 1]), "=r"(x[4 * c + 2]), "=r"(x[4 * c + 3])
+                     : "r"(src + (c >> 3) * G::kHalfBytes + (((c & 7) ^ (row & 7)) << 4)) : "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = __vmaxu2(top, x[4 * c + i] & 0x7fff7fffu);
+    }
+    top = max(top & 0xffffu, top >> 16);
+    const int e = min(max((int)(top >> 7) - 127, -99), 126);
+    const float f = __int_as_float((7 - e + 127) << 23);
+    const uint32_t dst = sh.smem + 2 * t * PfGeo8<D>::kRowTile;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+        uint32_t high[4], low[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {   // four elements
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                v[2 * k] = __uint_as_float(x[8 * c + 2 * i + k] << 16) * f;
+                v[2 * k + 1] = __uint_as_float(x[8 * c + 2 * i + k] & 0xffff0000u) * f;
+            }
+            high[i] = e4m3x4_of(v[0], v[1], v[2], v[3]);
+            const float2 a = f32x2_of_f16x2(f16x2_of_e4m3(high[i])), b = f32x2_of_f16x2(f16x2_of_e4m3(high[i] >> 16));
+            low[i] = e4m3x4_of(v[0] - a.x, v[1] - a.y, v[2] - b.x, v[3] - b.y);
+        }
+        sts_v4(dst + row8_chunk<D>(row, c), high[0], high[1], high[2], high[3]);
+        sts_v4(dst + PfGeo8<D>::kRowTile + row8_chunk<D>(row, c), low[0], low[1], low[2], low[3]);
+    }
+    return top >= 0x7f80u ? __int_as_float(0x7fc00000) : __int_as_float((e - 7 + 127) << 23);
+}
 
 // Scratch for the tail items cut into pieces.  Slot = (tail item index) * k + piece (at most gridDim slots);
 // per slot and tile: m[128], l[128] and O[128][D], all fp32.
@@ -822,8 +1041,30 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
     if (it.j1 <= it.j0) return true;  // an empty piece (more pieces than steps)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int j_end = min(it.j1, it.nkv[t]);
-    if (j_end <= it.j0) return true;  // this tile has no step in this piece
     const int row = (warp & 3) * 32 + lane;
+    float q_scale = 1.f;
+    PfValueScale vs, vs_ahead;   // of the step that is worked on, and of the one whose V is converted
+    const int kv_total = O == kKv8 ? pf_chunk<D, kMulti>(p, sh, 0, it.chunk) + pf_chunk<D, kMulti>(p, sh, 1, it.chunk) : 0;
+    auto convert = [&](int j) { return pf_convert<D>(p, sh, vs_ahead, j, j == it.j0, st.kv_it + (j - it.j0), kv_total); };
+    if constexpr (O == kKv8) {
+        if (j_end > it.j0) {
+            if (!pf_wait(sh, kBarQFull, st.q_it & 1, p.ctrl, 14)) return false;
+            q_scale = pf_split_q<D>(sh, t, row);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sh.bars + (kBarQReady + t) * 8);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)   // V's operand tiles hold Q until it is split
+            if (it.nkv[u] > it.j0) {
+                if (!pf_wait(sh, kBarQReady + u, st.q_cnt[u] & 1, p.ctrl, 12)) return false;
+                st.q_cnt[u] += 1;
+            }
+        if (!convert(it.j0)) return false;
+        for (int j = max(j_end, it.j0) + 1; j_end <= it.j0 && j < it.j1; ++j)   // a tile without rows
+            if (!convert(j)) return false;
+    }
+    if (j_end <= it.j0) return true;  // this tile has no step in this piece
     const int tok = it.tok0[t] + row / p.group;
     const int head = it.kvh * p.group + row % p.group;
     const int pos = pf_chunk<D, kMulti>(p, sh, 0, it.chunk) + tok;
@@ -858,40 +1099,68 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
 #pragma unroll
             for (int i = 0; i < 128; ++i) s[i] = i < limit ? s[i] : 0xff800000u;  // -inf: exp2 gives exactly 0
         }
+        // kKv8: what turns S into scores, for the keys of each page (not zero, which would make NaN of masked keys)
+        float page_scale[8];
+        if constexpr (O == kKv8) {
+            const uint32_t at = sh.smem + Geo<D>::kLastOffset + ((st.kv_it + (j - it.j0)) % PfGeo8<D>::kScaleStages) * 32;
+            const float4 a = lds_f4(at), b = lds_f4(at + 16);
+            const float k_scale[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                page_scale[g] = max_nan(k_scale[g] * q_scale, 1e-37f);
+            }
+        }
         // row maximum: independent chains of 3-input max, then a short tree
         float mxv[kPfMaxChains];
 #pragma unroll
         for (int c = 0; c < kPfMaxChains; ++c) mxv[c] = -INFINITY;
+        if constexpr (O == kKv8) {
 #pragma unroll
-        for (int i = 0; i < 128; i += 2 * kPfMaxChains)
+            for (int g = 0; g < 8; ++g) {
+                float a = max3(__uint_as_float(s[16 * g]), __uint_as_float(s[16 * g + 1]), __uint_as_float(s[16 * g + 2]));
+                float b = max3(__uint_as_float(s[16 * g + 3]), __uint_as_float(s[16 * g + 4]), __uint_as_float(s[16 * g + 5]));
 #pragma unroll
-            for (int c = 0; c < kPfMaxChains; ++c)
-                mxv[c] = max3(mxv[c], __uint_as_float(s[i + 2 * c]), __uint_as_float(s[i + 2 * c + 1]));
+                for (int i = 6; i < 14; i += 4) {
+                    a = max3(a, __uint_as_float(s[16 * g + i]), __uint_as_float(s[16 * g + i + 1]));
+                    b = max3(b, __uint_as_float(s[16 * g + i + 2]), __uint_as_float(s[16 * g + i + 3]));
+                }
+                a = max3(a, __uint_as_float(s[16 * g + 14]), __uint_as_float(s[16 * g + 15]));
+                mxv[g % kPfMaxChains] = fmaxf(mxv[g % kPfMaxChains], fmaxf(a, b) * page_scale[g]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 128; i += 2 * kPfMaxChains)
+#pragma unroll
+                for (int c = 0; c < kPfMaxChains; ++c)
+                    mxv[c] = max3(mxv[c], __uint_as_float(s[i + 2 * c]), __uint_as_float(s[i + 2 * c + 1]));
+        }
 #pragma unroll
         for (int w = kPfMaxChains / 2; w > 0; w >>= 1)
 #pragma unroll
             for (int c = 0; c < w; ++c) mxv[c] = fmaxf(mxv[c], mxv[c + w]);
         const float mx = mxv[0];
         const float m_new = fmaxf(m_ref, mx * sl2);
+        float v_factor = 1.f;
+        if constexpr (O == kKv8) v_factor = vs.follow(pf_value_scales<D>(sh, st.kv_it + (j - it.j0)), j == it.j0);
         if (j == it.j0) {
             m_ref = m_new;
         } else {
             // lazy rescale: keep the old reference unless some row's maximum grew by more than 2^8
             // (a row whose keys were all masked so far has m_ref = -inf and no weight yet: it just adopts m_new)
             const bool need = m_new - m_ref > 8.0f;
-            const bool any = __any_sync(0xffffffffu, need);
+            const bool any = __any_sync(0xffffffffu, need) || (O == kKv8 && v_factor != 1.f);
             if (G::kAhead || any) {   // the step before has updated O (and, with kAhead, read P)
                 if (!pf_wait(sh, kBarODone + t, (st.o_cnt + (j - it.j0) - 1) & 1, p.ctrl, 10)) return false;
                 tc_fence_after_sync();
             }
             if (any) {
-                const float f = need ? fast_exp2(m_ref - m_new) : 1.f;
+                const float f = need ? fast_exp2(m_ref - m_new) : 1.f, fo = O == kKv8 ? f * v_factor : f;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     tmem_ld_32x32b_x32(o_addr + c * 32, v);
                     tc_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+                    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * fo);
                     tmem_st_32x32b_x32(o_addr + c * 32, v);
                 }
                 tc_wait_st();
@@ -902,14 +1171,18 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
             }
         }
         // P = exp2(S * scale - m_ref), packed to bf16 (all of S is already in registers)
-        const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;
-        const uint64_t scale2 = pack_f32x2(sl2, sl2), negm2 = pack_f32x2(neg_m, neg_m);
+        const float neg_m = (m_ref == -INFINITY ? 0.f : -m_ref) + (O == kKv8 ? kPfWeightBits : 0.f);
+        uint64_t scale2 = pack_f32x2(sl2, sl2);
+        const uint64_t negm2 = pack_f32x2(neg_m, neg_m);
         uint64_t sum_a = pack_f32x2(0.f, 0.f), sum_b = sum_a;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             uint32_t pk[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
+                if constexpr (O == kKv8) {
+                    if ((i & 7) == 0) scale2 = pack_f32x2(page_scale[2 * c + (i >> 3)] * sl2, page_scale[2 * c + (i >> 3)] * sl2);
+                }
                 // two columns per instruction: x = s * scale - m, P = 2^x, row sum, bf16 pack
                 const uint64_t x2 = fma_f32x2(pack_f32x2(__uint_as_float(s[c * 32 + 2 * i]), __uint_as_float(s[c * 32 + 2 * i + 1])),
                                               scale2, negm2);
@@ -923,7 +1196,7 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
                     p1 = fast_exp2(x1);
                 }
                 if (i & 1) sum_b = add_f32x2(sum_b, pack_f32x2(p0, p1)); else sum_a = add_f32x2(sum_a, pack_f32x2(p0, p1));
-                pk[i] = pack_bf16x2(p0, p1);
+                pk[i] = O == kKv8 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1);
             }
             tmem_st_32x32b_x16(p_addr + c * 16, pk);
             if (c == 1) {  // the first 64 keys of P are in place: the first half of P V may start
@@ -943,19 +1216,28 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(sh.bars + (kBarPHalf + 2 * t + 1) * 8);
+        if constexpr (O == kKv8) {
+            if (j + 1 < it.j1 && !convert(j + 1)) return false;
+        }
+    }
+    if constexpr (O == kKv8) {
+        for (int j = j_end + 1; j < it.j1; ++j)   // steps of the other tile
+            if (!convert(j)) return false;
     }
 
     // the piece's O is complete once its last P V has been committed
     if (!pf_wait(sh, kBarODone + t, (st.o_cnt + (j_end - it.j0) - 1) & 1, p.ctrl, 11)) return false;
     st.o_cnt += j_end - it.j0;
     tc_fence_after_sync();
+    const float o_unit = O == kKv8 ? vs.ref * 0x1p-7f : 1.f;   // (kPfWeightBits)
+    if constexpr (O == kKv8) l_sum *= 0x1p-7f;
     const bool row_ok = tok < pf_chunk<D, kMulti>(p, sh, 1, it.chunk);
     const int64_t out_row = (int64_t)pf_chunk<D, kMulti>(p, sh, 2, it.chunk) + tok;
     __nv_bfloat16* dst = p.out + (out_row * p.Hq + head) * D;
     const bool whole = it.j0 == 0 && j_end == it.nkv[t];  // this piece holds every step of the tile
     if (whole) {
         // epilogue of an item this CTA did alone: O / l -> bf16 -> out
-        const float inv = 1.f / l_sum;
+        const float inv = O == kKv8 ? o_unit / l_sum : 1.f / l_sum;
         const int chunk_rows = pf_chunk<D, kMulti>(p, sh, 1, it.chunk);
         if (it.tok0[t] + 128 / p.group <= chunk_rows) {
             // Every row of the tile is a row of the chunk: the tile goes to the slot its Q tile came from (the last
@@ -1032,8 +1314,13 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
             tmem_ld_32x32b_x32(o_addr + c * 32, v);
             tc_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (O == kKv8) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[4 * i + e] = __float_as_uint(__uint_as_float(v[4 * i + e]) * o_unit);
+                }
                 *reinterpret_cast<uint4*>(po + (c * 8 + i) * 512) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            }
         }
     }
     tc_fence_before_sync();
@@ -1127,9 +1414,9 @@ __device__ __forceinline__ void prefill_phase(const CUtensorMap* kv_map, const C
             if (warp == 0) {
                 if (it.j1 > it.j0) pf_produce<D, kMulti, O>(kv_map, q_map, p, sh, it, prod_kv_it);
             } else if (warp == 1) {
-                if (it.j1 > it.j0) PfGeo<D>::kAhead ? pf_mma_ahead<D>(p, sh, it, mma_state) : pf_mma<D>(p, sh, it, mma_state);
+                if (it.j1 > it.j0) PfGeo<D>::kAhead ? pf_mma_ahead<D, O>(p, sh, it, mma_state) : pf_mma<D, O>(p, sh, it, mma_state);
             } else if (warp == 2) {
-                if (it.j1 > it.j0) pf_sanitize<D, kMulti, O>(p, sh, it, san_kv_it);
+                if (O != kKv8 && it.j1 > it.j0) pf_sanitize<D, kMulti, O>(p, sh, it, san_kv_it);
                 // Near the end of what may be the CTA's last entry: whether the decode units have all been handed out (the CTAs
                 // that started with them have published their number).  Then the CTA need not work the decode plan out afterwards,
                 // which takes 2-3 us.  (Not with several chunks at head size 64: the compiler then makes every step of the
@@ -1156,6 +1443,10 @@ __device__ __forceinline__ void prefill_phase(const CUtensorMap* kv_map, const C
         for (int iter = 0; entry < plan.n_entries; ++iter) {
             const PfItem it = pf_entry<kMulti, O>(p, plan, entry);
             pf_softmax<D, kMulti, O>(out_map, p, sh, plan, scr, it, (warp - 4) >> 2, sm_state);
+            if (O == kKv8 && it.j1 > it.j0) {
+                sm_state.kv_it += it.j1 - it.j0;
+                sm_state.q_it += 1;
+            }
             if (!piece_sync()) break;
             entry = next[iter & 1];
         }

@@ -23,9 +23,7 @@ def pool8(c):
 
 
 def attend(c, codes, scales):
-    pages = sum(-(-(P + C) // U.PAGE) for P, C, _, _ in c.batch.chunks())
-    scratch = torch.full((B.sw_kv8_scratch_bytes(c.ctx.layout, pages),), 0xFF, dtype=torch.uint8, device=c.dev) if pages else None
-    B.sw_kv8_attn_run(c.ctx, codes, scales, c.db, c.q, c.out, c.lse, scratch)
+    B.sw_kv8_attn_run(c.ctx, codes, scales, c.db, c.q, c.out, c.lse)
 
 
 def check_append(c, codes, scales):
@@ -202,13 +200,12 @@ def test_append_then_attend_many_iterations():
 def test_captured_and_replayed_on_another_stream():
     c = U.Case((32, 8, 128), [300, 5000, 40], [(700, 100)], seed=6)
     codes, scales = pool8(c)
-    scratch = torch.empty(B.sw_kv8_scratch_bytes(c.ctx.layout, 50), dtype=torch.uint8, device=c.dev)
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=s):
         B.sw_kv8_append(c.ctx, codes, scales, c.db, c.k_new, c.v_new, stream=s)
-        B.sw_kv8_attn_run(c.ctx, codes, scales, c.db, c.q, c.out, c.lse, scratch, stream=s)
+        B.sw_kv8_attn_run(c.ctx, codes, scales, c.db, c.q, c.out, c.lse, stream=s)
     for seed in (1, 2):
         for t in (c.q, c.k_new, c.v_new):
             t.copy_(torch.randn(t.shape, generator=torch.Generator().manual_seed(seed)))
@@ -239,11 +236,11 @@ def test_bad_pages_are_reported_and_nothing_else_is_written():
 def test_refusals():
     c = U.Case((8, 2, 64), [40], [(0, 20)])
     codes, scales = pool8(c)
-    small = torch.empty(B.sw_kv8_scratch_bytes(c.ctx.layout, 2) - 1, dtype=torch.uint8, device=c.dev)
-    for scratch in (None, small, torch.empty(1 << 20, dtype=torch.uint8, device=c.dev)[1:]):
+    for args in [(None, scales, c.q, c.out), (codes, None, c.q, c.out), (codes, scales, None, c.out), (codes, scales, c.q, None),
+                 (codes.view(torch.uint8).view(-1)[1:], scales, c.q, c.out), (codes, scales.view(-1)[1:], c.q, c.out)]:
         with pytest.raises(B.SwError) as e:
-            B.sw_kv8_attn_run(c.ctx, codes, scales, c.db, c.q, c.out, None, scratch)
-        assert e.value.status == B.SW_ERR_WORKSPACE
+            B.sw_kv8_attn_run(c.ctx, args[0], args[1], c.db, args[2], args[3])
+        assert e.value.status == B.SW_ERR_INVALID_ARG
     for args in [(None, scales, c.k_new, c.v_new), (codes, None, c.k_new, c.v_new), (codes, scales, None, c.v_new), (codes, scales, c.k_new, None),
                  (codes.view(torch.uint8).view(-1)[1:], scales, c.k_new, c.v_new), (codes, scales.view(-1)[1:], c.k_new, c.v_new)]:
         with pytest.raises(B.SwError) as e:
