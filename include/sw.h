@@ -173,10 +173,13 @@ sw_status sw_mixed_iteration_window_run(sw_ctx* ctx, void* kv_pool, const sw_bat
  *
  * sw_kv8_attn_run is sw_mixed_attn_run over such a pool.  The scales must be powers of two (between 2^-100 and 2^120) or NaN.  Its products see the
  * values that the pool stands for exactly; queries are rounded at 2^-18 of their row's largest element, weights at 2^-40 of the largest.
+ * scratch (optional; 256-byte aligned device memory of sw_kv8_scratch_bytes(layout, sum over the chunks of ceil((P + C) / 16)) bytes, of no use
+ * between calls): where it is large enough and that is faster, long chunks read a copy of their prompts in 16 bits, made there first.
  * Both calls are asynchronous. */
+size_t sw_kv8_scratch_bytes(const sw_layout* layout, int64_t prompt_pages);
 sw_status sw_kv8_append(sw_ctx* ctx, void* kv8_pool, float* scales, const sw_batch* batch, const void* k_new, const void* v_new, void* stream);
 sw_status sw_kv8_attn_run(sw_ctx* ctx, const void* kv8_pool, const float* scales, const sw_batch* batch, const void* q, void* out, float* lse,
-                          void* stream);
+                          void* scratch, size_t scratch_bytes, void* stream);
 
 /* Accumulated attention weights: fp32 [rows][num_kv_heads][capacity] (device), one row per sequence, one weight per KV head and position.
  * Request i of a batch uses row row_of[i] (device int32 [num_decode]); the requests of a call use different rows. */

@@ -72,7 +72,7 @@ EXPORTS = ["sw_workspace_bytes", "sw_create", "sw_destroy", "sw_kv_append", "sw_
            "sw_cost_table_destroy", "sw_cost_table_lookup", "sw_choose_chunk", "sw_choose_chunks", "sw_last_error",
            "sw_decode_attn_static", "sw_selftest_wait_timeout", "sw_telemetry_create", "sw_telemetry_destroy",
            "sw_telemetry_record", "sw_telemetry_margin", "sw_telemetry_exceeds", "sw_telemetry_get_totals",
-           "sw_telemetry_reset", "sw_mixed_attn_window_run", "sw_mixed_iteration_window_run", "sw_kv8_append",
+           "sw_telemetry_reset", "sw_mixed_attn_window_run", "sw_mixed_iteration_window_run", "sw_kv8_scratch_bytes", "sw_kv8_append",
            "sw_kv8_attn_run", "sw_attn_weights_scratch_bytes", "sw_decode_attn_weights_run", "sw_kv_evict"]
 
 _vp, _i32, _i64 = C.c_void_p, C.c_int32, C.c_int64
@@ -87,8 +87,10 @@ _lib.sw_mixed_iteration_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _vp, _vp,
 _lib.sw_mixed_iteration_host.argtypes = [_vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.sw_mixed_attn_window_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _i32, _i32, _vp, _vp, _vp, _vp]
 _lib.sw_mixed_iteration_window_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.sw_kv8_scratch_bytes.restype = C.c_size_t
+_lib.sw_kv8_scratch_bytes.argtypes = [C.POINTER(sw_layout), _i64]
 _lib.sw_kv8_append.argtypes = [_vp, _vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp]
-_lib.sw_kv8_attn_run.argtypes = [_vp, _vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, _vp]
+_lib.sw_kv8_attn_run.argtypes = [_vp, _vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, _vp, C.c_size_t, _vp]
 _lib.sw_attn_weights_scratch_bytes.restype = C.c_size_t
 _lib.sw_attn_weights_scratch_bytes.argtypes = [C.POINTER(sw_layout), _i64]
 _lib.sw_decode_attn_weights_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, C.POINTER(sw_key_weights), _vp, C.c_size_t, _vp]
@@ -259,16 +261,20 @@ def _bytes_of(t) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
 
+def sw_kv8_scratch_bytes(layout: sw_layout, prompt_pages: int) -> int:
+    return int(_lib.sw_kv8_scratch_bytes(C.byref(layout), prompt_pages))
+
+
 def sw_kv8_append(ctx: Context, kv8_pool, scales, batch: DeviceBatch, k_new, v_new, stream=None) -> None:
     """The iteration's new rows into an 8-bit pool (``torch.float8_e4m3fn`` or ``uint8``) with its fp32 ``scales``."""
     _check(_lib.sw_kv8_append(ctx.handle, _ptr(kv8_pool), _ptr(scales), C.byref(batch.struct), _ptr(k_new), _ptr(v_new),
                               _stream_handle(stream)), "sw_kv8_append")
 
 
-def sw_kv8_attn_run(ctx: Context, kv8_pool, scales, batch: DeviceBatch, q, out, lse=None, stream=None) -> None:
-    """``sw_mixed_attn_run`` over an 8-bit pool."""
+def sw_kv8_attn_run(ctx: Context, kv8_pool, scales, batch: DeviceBatch, q, out, lse=None, scratch=None, stream=None) -> None:
+    """``sw_mixed_attn_run`` over an 8-bit pool; ``scratch`` (optional): ``sw_kv8_scratch_bytes`` bytes, with which long chunks are faster."""
     _check(_lib.sw_kv8_attn_run(ctx.handle, _ptr(kv8_pool), _ptr(scales), C.byref(batch.struct), _ptr(q), _ptr(out), _ptr(lse),
-                                _stream_handle(stream)), "sw_kv8_attn_run")
+                                _ptr(scratch), _bytes_of(scratch), _stream_handle(stream)), "sw_kv8_attn_run")
 
 
 class KeyWeights:

@@ -380,7 +380,7 @@ sw::MixedParams mixed_params(const sw_ctx* ctx, const sw_batch* batch, const Chu
     p.Hq = l.num_q_heads;
     p.Hkv = l.num_kv_heads;
     p.group = l.num_q_heads / l.num_kv_heads;
-    p.num_pages = l.num_pages;
+    p.num_pages = p.chunk_pool_pages = l.num_pages;
     p.sm_scale = l.sm_scale;
     p.sm_scale_log2 = l.sm_scale * 1.4426950408889634f;
     p.stage_us = ctx->stage_us;
@@ -533,6 +533,30 @@ sw_status sw_mixed_iteration_window_run(sw_ctx* ctx, void* kv_pool, const sw_bat
 
 // ---- the pool in 8 bits --------------------------------------------------------------------------------------------
 namespace {
+// Pages that the chunks' prompts take in 16 bits, and what they take in bytes with their list.
+int64_t prompt_pages(const Chunks& ch) {
+    int64_t pages = 0;
+    for (int j = 0; j < ch.n; ++j) pages += ((int64_t)ch.P[j] + ch.C[j] + sw::kPageSize - 1) / sw::kPageSize;
+    return pages;
+}
+size_t page_bytes(const sw_layout& l) { return (size_t)2 * l.num_kv_heads * sw::kPageSize * l.head_dim * 2; }
+size_t kv8_scratch(const sw_layout& l, int64_t pages) { return (size_t)pages * page_bytes(l) + align_up((size_t)pages * 4, 256); }
+
+// Whether an iteration's chunks read a 16-bit copy of their prompts, made by a launch of its own, rather than the 8-bit pool.  Measured with
+// 32/8/128: a 128-key step of an entry is up to 0.9 us longer over the 8-bit pool (the widened V tiles go through a shared memory that the
+// tensor cores' operands keep busy), a copy costs 4 us and 0.6 us a megabyte of the prompts, and most of the rest is the same.  Over the
+// pool | with a copy, us: 1024 tokens at prefix 4096 104 | 81, 512 at 512 28 | 26, 4096 at 28672 2060 | 1600; 128 at 28672 94 | 110.
+bool chunks_copied(const sw_layout& l, const Chunks& ch, int num_sms) {
+    const int group = l.num_q_heads / l.num_kv_heads;
+    double steps = 0., megabytes = 0.;
+    for (int j = 0; j < ch.n; ++j) {
+        const double items = ((int64_t)ch.C[j] * group + 255) / 256 * (double)l.num_kv_heads;
+        steps += items * (((double)ch.P[j] + 0.5 * ch.C[j]) / 128. + 1.);
+        megabytes += ((double)ch.P[j] + ch.C[j]) * 2 * l.num_kv_heads * l.head_dim * 1e-6;
+    }
+    return 0.9 * steps / num_sms > 1. + 0.6 * megabytes;
+}
+
 sw_status kv8_maps_for(sw_ctx* ctx, const void* pool, const sw::KvMaps** out) {
     for (int i = 0; i < ctx->kv8_map_count; ++i)
         if (ctx->kv8_maps[i].pool == pool) {
@@ -552,6 +576,13 @@ sw_status kv8_maps_for(sw_ctx* ctx, const void* pool, const sw::KvMaps** out) {
 }
 }  // namespace
 
+size_t sw_kv8_scratch_bytes(const sw_layout* layout, int64_t prompt_pages) {
+    if (!layout || !layout_supported(*layout) || prompt_pages < 0 || prompt_pages > (int64_t)1 << 30 ||
+        2 * prompt_pages * layout->num_kv_heads >= (int64_t)1 << 31)
+        return 0;
+    return kv8_scratch(*layout, prompt_pages);
+}
+
 sw_status sw_kv8_append(sw_ctx* ctx, void* kv8_pool, float* scales, const sw_batch* batch, const void* k_new, const void* v_new, void* stream) {
     Chunks ch;
     sw_status st = check_batch(ctx, batch, "sw_kv8_append", &ch);
@@ -567,7 +598,7 @@ sw_status sw_kv8_append(sw_ctx* ctx, void* kv8_pool, float* scales, const sw_bat
 }
 
 sw_status sw_kv8_attn_run(sw_ctx* ctx, const void* kv8_pool, const float* scales, const sw_batch* batch, const void* q, void* out, float* lse,
-                          void* stream) {
+                          void* scratch, size_t scratch_bytes, void* stream) {
     const char* who = "sw_kv8_attn_run";
     Chunks ch;
     sw_status st = check_batch(ctx, batch, who, &ch);
@@ -583,13 +614,38 @@ sw_status sw_kv8_attn_run(sw_ctx* ctx, const void* kv8_pool, const float* scales
     if (st != SW_OK) return st;
     sw::MixedParams p = mixed_params(ctx, batch, ch, q, out, lse);
     p.kv8_scales = scales;
-    p.stage_us *= 0.5f;   // pages are half as long
-    p.stages_per_us *= 2.f;
-    p.steps_per_stage *= 0.5f;
+    // Pages are half as long, but a warp needs two thirds of the time for one: 64 contexts of 256-2048 tokens beside 512 at prefix 512 take
+    // 70 us with the half, 59 with three quarters, 61 with the whole; 128 log-normal ones beside 1024 at 4096 274, 262 and 277.
+    p.stage_us *= 0.75f;
+    p.stages_per_us *= 4.f / 3.f;
+    p.steps_per_stage *= 0.75f;
     CUtensorMap q_map = maps->half, out_map = maps->half;
     st = encode_row_maps(ctx, p, &q_map, &out_map);
     if (st != SW_OK) return st;
-    SW_CUDA(sw::launch_kv8_attn(l.head_dim, *maps, q_map, out_map, p, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+    const int64_t pages = prompt_pages(ch);
+    if (scratch && (reinterpret_cast<uintptr_t>(scratch) & 255) != 0)
+        return sw_fail(SW_ERR_WORKSPACE, "%s: scratch must be 256-byte aligned", who);
+    if (scratch && pages > 0 && pages <= (int64_t)1 << 30 && 2 * pages * l.num_kv_heads < (int64_t)1 << 31 &&
+        scratch_bytes >= kv8_scratch(l, pages) && chunks_copied(l, ch, ctx->num_sms)) {
+        __nv_bfloat16* copy = static_cast<__nv_bfloat16*>(scratch);
+        int32_t* list = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(scratch) + (size_t)pages * page_bytes(l));
+        sw_layout copy_layout = l;
+        copy_layout.num_pages = pages;
+        sw::KvMaps copy_maps;
+        CUresult r = sw::encode_kv_maps(ctx->encode, copy_layout, copy, &copy_maps);
+        if (r != CUDA_SUCCESS) return sw_fail(SW_ERR_CUDA, "cuTensorMapEncodeTiled(scratch) failed with CUresult %d", (int)r);
+        copy_maps.page = maps->page;
+        SW_CUDA(sw::launch_kv8_expand(append_params(ctx, batch, ch, nullptr, nullptr, nullptr), ch.C, static_cast<const uint8_t*>(kv8_pool), scales,
+                                      copy, list, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+        p.prefill_pages = list;
+        p.num_prefill_pages = (int)pages;
+        p.chunk_pool_pages = pages;
+        for (int j = 0; j < sw::kMaxChunks; ++j)
+            p.cPage0[j + 1] = p.cPage0[j] + (j < ch.n ? (int)(((int64_t)ch.P[j] + ch.C[j] + sw::kPageSize - 1) / sw::kPageSize) : 0);
+        SW_CUDA(sw::launch_kv8_attn(l.head_dim, true, copy_maps, q_map, out_map, p, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+        return SW_OK;
+    }
+    SW_CUDA(sw::launch_kv8_attn(l.head_dim, false, *maps, q_map, out_map, p, ctx->num_sms, static_cast<cudaStream_t>(stream)));
     return SW_OK;
 }
 

@@ -82,6 +82,7 @@ struct MixedParams {
     int32_t* pf_tickets; // [items][2]
     // launches with a window: the last `window` keys and the first `sinks` are attended
     int window, sinks, sink_pages;   // pages that hold a key below `sinks`
+    int64_t chunk_pool_pages;   // pages of the pool that the chunks read: num_pages, or of their prompts' copy
     // launches over an 8-bit pool: fp32 [num_pages][2][Hkv]
     const float* kv8_scales;
     // launches that leave their scores behind: fp32 [score_pages][Hkv][16][group] by place in decode_pages
@@ -212,8 +213,10 @@ cudaError_t configure_window_kernels(int head_dim);
 cudaError_t window_attn_resident_ctas_per_sm(int head_dim, int* out);
 // 8-bit pools (sw_kv8.cu)
 cudaError_t launch_kv8_append(const AppendParams& a, const int* cC, uint8_t* pool, float* scales, int num_sms, cudaStream_t stream);
-cudaError_t launch_kv8_attn(int head_dim, const KvMaps& kv_maps, const CUtensorMap& q_map, const CUtensorMap& out_map, const MixedParams& p,
-                            int num_sms, cudaStream_t stream);
+cudaError_t launch_kv8_expand(const AppendParams& a, const int* cC, const uint8_t* pool, const float* scales, __nv_bfloat16* copy, int32_t* list,
+                              int num_sms, cudaStream_t stream);
+cudaError_t launch_kv8_attn(int head_dim, bool copied, const KvMaps& kv_maps, const CUtensorMap& q_map, const CUtensorMap& out_map,
+                            const MixedParams& p, int num_sms, cudaStream_t stream);
 cudaError_t configure_kv8_kernels(int head_dim);
 // decode attention that adds up weights (sw_weights.cu)
 cudaError_t launch_scored_attn(int head_dim, const KvMaps& kv_maps, const CUtensorMap& any_map, const MixedParams& p, int num_sms, cudaStream_t stream);

@@ -14,10 +14,12 @@ constexpr int kKv8Threads = 256;
 // The blocks that an append writes, numbered: the pages of chunk 0 that get rows, of chunk 1, ..., then one of each decode request.
 struct Kv8Params {
     AppendParams a;
-    int block0[kMaxChunks + 1];   // written pages before chunk j's
+    int block0[kMaxChunks + 1];   // written (expand: the prompt's) pages before chunk j's
     int cC[kMaxChunks];
     uint8_t* pool;
     float* scales;
+    __nv_bfloat16* copy;   // expand only
+    int32_t* list;
 };
 
 __device__ __forceinline__ float bf16_lo(uint32_t x) { return __uint_as_float(x << 16); }
@@ -120,6 +122,54 @@ __global__ void __launch_bounds__(kKv8Threads) sw_kv8_append_kernel(const Kv8Par
     }
 }
 
+// The prompts of the iteration's chunks as bf16 pages 0, 1, ... of `copy`, one prompt behind the other, and the list of those pages: what the
+// chunk-prefill tiles read in place of the 8-bit pool where that is faster (chunks_copied).  One warp per block, 8 bytes a lane and load;
+// slots at or past the prompt's end become zeros.  Exact: e4m3 times a power of two is a bf16 number.  An e4m3 is a bf16 whose exponent is 120
+// too small once its seven lower bits are moved up by four, subnormal values included; one product with 2^120 times the scale does the rest.
+template <int D>
+__global__ void __launch_bounds__(kKv8Threads) sw_kv8_expand_kernel(const Kv8Params p) {
+    constexpr int kLoads = D / 16, kRowLanes = D / 8;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int lane = threadIdx.x & 31, sides = 2 * p.a.Hkv;
+    const int64_t tasks = (int64_t)p.block0[p.a.nchunks] * sides;
+    for (int64_t t = (int64_t)blockIdx.x * (kKv8Threads / 32) + threadIdx.x / 32; t < tasks; t += (int64_t)gridDim.x * (kKv8Threads / 32)) {
+        const int b = (int)(t / sides), hs = (int)(t % sides);
+        int end = p.a.cP[0] + p.cC[0], at = 0, page0 = 0;
+#pragma unroll
+        for (int j = 1; j < kMaxChunks; ++j)
+            if (j < p.a.nchunks && b >= p.block0[j]) end = p.a.cP[j] + p.cC[j], at = p.block0[j], page0 = p.a.cPage0[j];
+        int page = p.a.prefill_pages[page0 + b - at];
+        if (page < 0 || (int64_t)page >= p.a.num_pages) {
+            if (lane == 0) report(p.a.ctrl, SW_ERR_OUT_OF_RANGE, kSiteAttnPage, b);
+            page = 0;
+        }
+        const int valid = end - (b - at) * kPageSize;
+        const int64_t block = (int64_t)page * sides + hs;
+        const uint2* src = reinterpret_cast<const uint2*>(p.pool + block * kPageSize * D) + lane;
+        uint4* dst = reinterpret_cast<uint4*>(p.copy + ((int64_t)b * sides + hs) * kPageSize * D) + lane;
+        uint2 w[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) w[i] = __ldcs(src + i * 32);
+        const float scale = p.scales[block], rest = scale > 128.f ? scale * 0.0078125f : 1.f;   // 2^127 is as far as one factor goes
+        const float f = (scale > 128.f ? 128.f : scale) * 1.329227995784916e36f;   // 2^120
+        const uint32_t factor = pack_bf16x2(f, f), more = pack_bf16x2(rest, rest);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {   // bytes 2 e and 2 e + 1, each with eight copies of its sign above it
+                asm("prmt.b32 %0, %1, %1, %2;" : "=r"(x[e]) : "r"(e < 2 ? w[i].x : w[i].y), "r"(e & 1 ? 0xb3a2 : 0x9180));
+                x[e] = (x[e] << 4) & 0x87f087f0u;
+                asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(x[e]) : "r"(x[e]), "r"(factor));
+                if (rest != 1.f) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(x[e]) : "r"(x[e]), "r"(more));
+            }
+            dst[i * 32] = (i * 32 + lane) / kRowLanes < valid ? make_uint4(x[0], x[1], x[2], x[3]) : make_uint4(0u, 0u, 0u, 0u);
+        }
+        if (hs == 0 && lane == 0) p.list[b] = b;
+    }
+}
+
 namespace {
 template <class K>
 cudaError_t launch_blocks(K* kernel, const Kv8Params& p, int64_t tasks, int num_sms, cudaStream_t stream) {
@@ -151,10 +201,28 @@ cudaError_t launch_kv8_append(const AppendParams& a, const int* cC, uint8_t* poo
                      : launch_blocks(sw_kv8_append_kernel<128>, p, tasks, num_sms, stream);
 }
 
+cudaError_t launch_kv8_expand(const AppendParams& a, const int* cC, const uint8_t* pool, const float* scales, __nv_bfloat16* copy, int32_t* list,
+                              int num_sms, cudaStream_t stream) {
+    Kv8Params p{};
+    p.a = a;
+    p.pool = const_cast<uint8_t*>(pool);
+    p.scales = const_cast<float*>(scales);
+    p.copy = copy;
+    p.list = list;
+    for (int j = 0; j < a.nchunks; ++j) {
+        p.cC[j] = cC[j];
+        p.block0[j + 1] = p.block0[j] + (int)(((int64_t)a.cP[j] + cC[j] - 1) / kPageSize) + 1;
+    }
+    const int64_t tasks = (int64_t)p.block0[a.nchunks] * 2 * a.Hkv;
+    return a.D == 64 ? launch_blocks(sw_kv8_expand_kernel<64>, p, tasks, num_sms, stream)
+                     : launch_blocks(sw_kv8_expand_kernel<128>, p, tasks, num_sms, stream);
+}
+
 cudaError_t configure_kv8_kernels(int head_dim) { return configure_option<kKv8>(head_dim); }
-cudaError_t launch_kv8_attn(int head_dim, const KvMaps& kv_maps, const CUtensorMap& q_map, const CUtensorMap& out_map, const MixedParams& p,
-                            int num_sms, cudaStream_t stream) {
-    return launch_option<kKv8>(head_dim, kv_maps, q_map, out_map, p, num_sms, stream);
+cudaError_t launch_kv8_attn(int head_dim, bool copied, const KvMaps& kv_maps, const CUtensorMap& q_map, const CUtensorMap& out_map,
+                            const MixedParams& p, int num_sms, cudaStream_t stream) {
+    return copied ? launch_option<kKv8, kPlain>(head_dim, kv_maps, q_map, out_map, p, num_sms, stream)
+                  : launch_option<kKv8>(head_dim, kv_maps, q_map, out_map, p, num_sms, stream);
 }
 
 }  // namespace sw

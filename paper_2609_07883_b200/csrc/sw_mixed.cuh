@@ -1590,7 +1590,8 @@ namespace sw {
 // and 64 contexts beside 512 tokens 63.7, with kernels of their own 13.2 and 62.5; 20 contexts of 8/1/128, worked off as units, take
 // 16.8 us in a kernel of their own and 21.6 beside the line's code (18.3 with all in one).
 enum Form { kOneChunk, kSeveralChunks, kLine, kUnits };
-template <int D, Form kForm, Option O>
+// P: the option of the chunk-prefill part; kPlain beside kKv8 where the chunks' prompts were copied to 16 bits before (sw_kv8.cu)
+template <int D, Form kForm, Option O, Option P>
 __global__ void __launch_bounds__(kThreads, 1) sw_mixed_attn_kernel(const __grid_constant__ CUtensorMap kv_map,
                                                                        const __grid_constant__ CUtensorMap kvp_map,
                                                                     const __grid_constant__ CUtensorMap q_map,
@@ -1623,7 +1624,7 @@ __global__ void __launch_bounds__(kThreads, 1) sw_mixed_attn_kernel(const __grid
             tma_prefetch_desc(&kv_map);
             tma_prefetch_desc(&q_map);
             tma_prefetch_desc(&out_map);
-            pf_init_barriers<O>(base + Geo<D>::kPfBarOffset);
+            pf_init_barriers<P>(base + Geo<D>::kPfBarOffset);
         }
         misc[kMiscTmem] = 0;
         misc[kMiscAbort] = 0;
@@ -1635,7 +1636,7 @@ __global__ void __launch_bounds__(kThreads, 1) sw_mixed_attn_kernel(const __grid
     // so it is made after the wait below; the table of several chunks (a microsecond) is filled here for the usual case, that
     // every CTA takes entries, and filled again after the wait where that turns out otherwise.
     if constexpr (kMulti) {
-        if (warp == 2) pf_fill_chunk_table<O>(p, scratch + kChunkTable, (int)gridDim.x);
+        if (warp == 2) pf_fill_chunk_table<P>(p, scratch + kChunkTable, (int)gridDim.x);
     }
     // Everything above touched only shared memory and kernel parameters.  From here on the kernel reads what earlier
     // kernels of the stream wrote (the pool after the KV append, q, the page tables): wait for them to finish.
@@ -1651,11 +1652,11 @@ __global__ void __launch_bounds__(kThreads, 1) sw_mixed_attn_kernel(const __grid
     if (tensor_prefill && warp == 2) {
         if constexpr (kMulti) {
             __syncwarp();
-            const int ctas = pf_table_ctas<O>(p, scratch + kChunkTable);
+            const int ctas = pf_table_ctas<P>(p, scratch + kChunkTable);
             __syncwarp();
-            if (ctas != (int)gridDim.x) pf_fill_chunk_table<O>(p, scratch + kChunkTable, ctas);
+            if (ctas != (int)gridDim.x) pf_fill_chunk_table<P>(p, scratch + kChunkTable, ctas);
         } else {
-            pf_fill_plan<O>(p, scratch + kChunkTable);
+            pf_fill_plan<P>(p, scratch + kChunkTable);
         }
         __syncwarp();
     }
@@ -1703,7 +1704,7 @@ __global__ void __launch_bounds__(kThreads, 1) sw_mixed_attn_kernel(const __grid
             scr.o = p.pf_o;
             scr.tickets = p.pf_tickets;
             scr.flags = &misc[kMiscFlags];
-            prefill_phase<D, kMulti, O>(&kv_map, &q_map, &out_map, p, sh, pplan, scr, first_entry, &misc[kMiscNext]);
+            prefill_phase<D, kMulti, P>(&kv_map, &q_map, &out_map, p, sh, pplan, scr, first_entry, &misc[kMiscNext]);
             tc_fence_before_sync();
             __syncthreads();
             if (warp == 1) tmem_dealloc(sh.tmem, 512);
@@ -1801,11 +1802,15 @@ inline size_t mixed_attn_smem_bytes(int head_dim) {
 
 template <int D, Option O, class F>
 cudaError_t for_each_form(F f) {
-    cudaError_t e = f(sw_mixed_attn_kernel<D, kLine, O>);
-    if (e == cudaSuccess) e = f(sw_mixed_attn_kernel<D, kUnits, O>);
+    cudaError_t e = f(sw_mixed_attn_kernel<D, kLine, O, O>);
+    if (e == cudaSuccess) e = f(sw_mixed_attn_kernel<D, kUnits, O, O>);
     if constexpr (O != kScored) {
-        if (e == cudaSuccess) e = f(sw_mixed_attn_kernel<D, kOneChunk, O>);
-        if (e == cudaSuccess) e = f(sw_mixed_attn_kernel<D, kSeveralChunks, O>);
+        if (e == cudaSuccess) e = f(sw_mixed_attn_kernel<D, kOneChunk, O, O>);
+        if (e == cudaSuccess) e = f(sw_mixed_attn_kernel<D, kSeveralChunks, O, O>);
+    }
+    if constexpr (O == kKv8) {
+        if (e == cudaSuccess) e = f(sw_mixed_attn_kernel<D, kOneChunk, O, kPlain>);
+        if (e == cudaSuccess) e = f(sw_mixed_attn_kernel<D, kSeveralChunks, O, kPlain>);
     }
     return e;
 }
@@ -1829,17 +1834,17 @@ cudaError_t resident_ctas_of_option(int head_dim, int* out) {
     });
 }
 
-template <int D, Option O>
+template <int D, Option O, Option P>
 cudaError_t launch_option_of(const cudaLaunchConfig_t& cfg, const KvMaps& kv_maps, const CUtensorMap& q_map, const CUtensorMap& out_map,
                              const MixedParams& p) {
     auto launch = [&](auto* kernel) { return cudaLaunchKernelEx(&cfg, kernel, kv_maps.half, kv_maps.page, q_map, out_map, p); };
     if constexpr (O != kScored) {
-        if (p.nchunks > 1) return launch(sw_mixed_attn_kernel<D, kSeveralChunks, O>);
-        if (p.nchunks == 1) return launch(sw_mixed_attn_kernel<D, kOneChunk, O>);
+        if (p.nchunks > 1) return launch(sw_mixed_attn_kernel<D, kSeveralChunks, O, P>);
+        if (p.nchunks == 1) return launch(sw_mixed_attn_kernel<D, kOneChunk, O, P>);
     }
-    return line_form(p, D) ? launch(sw_mixed_attn_kernel<D, kLine, O>) : launch(sw_mixed_attn_kernel<D, kUnits, O>);
+    return line_form(p, D) ? launch(sw_mixed_attn_kernel<D, kLine, O, O>) : launch(sw_mixed_attn_kernel<D, kUnits, O, O>);
 }
-template <Option O>
+template <Option O, Option P = O>
 cudaError_t launch_option(int head_dim, const KvMaps& kv_maps, const CUtensorMap& q_map, const CUtensorMap& out_map, const MixedParams& p,
                           int num_sms, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
@@ -1852,7 +1857,7 @@ cudaError_t launch_option(int head_dim, const KvMaps& kv_maps, const CUtensorMap
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return head_dim == 64 ? launch_option_of<64, O>(cfg, kv_maps, q_map, out_map, p) : launch_option_of<128, O>(cfg, kv_maps, q_map, out_map, p);
+    return head_dim == 64 ? launch_option_of<64, O, P>(cfg, kv_maps, q_map, out_map, p) : launch_option_of<128, O, P>(cfg, kv_maps, q_map, out_map, p);
 }
 
 }  // namespace sw

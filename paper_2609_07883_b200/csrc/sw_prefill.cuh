@@ -40,7 +40,7 @@ struct PfGeo {
 };
 
 // kKv8: the same region holds, in tiles of 128 rows of D bytes, Q of both tiles as two e4m3 parts, two stages of K as it lies in the pool, two
-// stages of V likewise, and two stages of V as f16 operand tiles (into which Q's bf16 rows land first).  32 floats of scales for K, then for V,
+// stages of V likewise, and two stages of V as f16 operand tiles.  (Q's bf16 rows land where their two parts are put.)  32 floats of scales for K, then for V,
 // of the pages of four stages lie where launches with a fused append list last pages.
 template <int D>
 struct PfGeo8 {
@@ -560,15 +560,14 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
     // The whole warp runs the role: lane i owns page i of every 128-key tile (its page id, its TMA boxes), so the
     // eight pages of a tile are issued by one instruction instead of a loop of one thread.
     const int lane = threadIdx.x & 31;
-    // Q tiles (rows past the chunk are zero-filled by the tensor map's bounds); kKv8: into V's operand tiles, whose first rows are made after
-    // the softmax warps have split Q
+    // Q tiles (rows past the chunk are zero-filled by the tensor map's bounds)
     if (lane == 0) {
         const int active = (it.nkv[0] > it.j0) + (it.nkv[1] > it.j0);
         mbar_arrive_expect_tx(sh.bars + kBarQFull * 8, active * G::kTileBytes);
         for (int t = 0; t < 2; ++t)
             if (it.nkv[t] > it.j0)
                 for (int h = 0; h < G::kHalves; ++h)
-                    tma_load_3d((O == kKv8 ? pf_v_tile<D, O>(sh, t) : sh.smem + G::kQOffset + t * G::kTileBytes) + h * G::kHalfBytes, q_map, sh.bars + kBarQFull * 8,
+                    tma_load_3d(sh.smem + G::kQOffset + t * G::kTileBytes + h * G::kHalfBytes, q_map, sh.bars + kBarQFull * 8,
                                 h * 64, it.kvh * p.group, pf_chunk<D, kMulti>(p, sh, 2, it.chunk) + it.tok0[t]);
     }
     // fused launch: tiles that reach into the chunk's own keys wait until every CTA has written its share of them
@@ -584,7 +583,7 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
     auto id_of = [&](int step) {
         const int page = pf_tile<O>(it, step) * 8 + lane;
         int id = (lane < 8 && seen(page)) ? p.prefill_pages[pf_chunk<D, kMulti>(p, sh, 3, it.chunk) + page] : 0;
-        if (id < 0 || (int64_t)id >= p.num_pages) {
+        if (id < 0 || (int64_t)id >= p.chunk_pool_pages) {
             // reported, and page 0 fetched in its place: a bad id never reaches the copy engine
             report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteAttnPage, it.item);
             id = 0;
@@ -704,31 +703,27 @@ __device__ __forceinline__ bool pf_sanitize(const MixedParams& p, const PfShared
 // down to 2^-15.  Everybody works ref out from the scales.  `top`: its largest value; a tile 2^-80 below it is not followed.
 constexpr float kPfWeightBits = 7.f;   // P is 2^7 times the weight
 struct PfValueScale {
-    float ref = 0.f, top = 0.f;
-    float v[8];   // of the tile's pages
-    // Takes the step's scales; returns what O has to be multiplied with (1: ref stays).
+    float ref = 0.f, top = 0.f, inverse = 0.f;   // inverse: 1 / ref
+    // Takes the step's eight scales; returns what O has to be multiplied with (1: ref stays).
     __device__ __forceinline__ float follow(uint32_t scales, bool first) {
         const float4 a = lds_f4(scales), b = lds_f4(scales + 16);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-        const float most = fmaxf(max3(fmaxf(v[0], v[1]), v[2], v[3]), max3(fmaxf(v[4], v[5]), v[6], v[7]));   // (NaN does not count)
-        if (first) {
-            ref = top = most;
-        } else if (most > ref * 8.f || (most < ref * 0x1p-12f && most >= top * 0x1p-80f)) {
-            const float f = ref / most;
-            ref = most;
-            top = fmaxf(top, most);
-            return f;
-        }
-        return 1.f;
+        const float most = fmaxf(max3(fmaxf(a.x, a.y), a.z, a.w), max3(fmaxf(b.x, b.y), b.z, b.w));   // (NaN does not count)
+        if (!first && most <= ref * 8.f && !(most < ref * 0x1p-12f && most >= top * 0x1p-80f)) return 1.f;
+        const float f = ref / most;
+        ref = most;
+        top = first ? most : fmaxf(top, most);
+        inverse = 1.f / most;
+        return f;
     }
 };
 template <int D>
 __device__ __forceinline__ uint32_t pf_value_scales(const PfShared& sh, uint32_t kv_it) {
     return sh.smem + Geo<D>::kLastOffset + PfGeo8<D>::kVScales + (kv_it % PfGeo8<D>::kScaleStages) * 32;
 }
-// The warp's page of step j; kv_it: the step's number on this CTA.
+// The warp's page of step j; kv_it: the step's number on this CTA.  v_factor: see PfValueScale::follow.
 template <int D>
-__device__ __forceinline__ bool pf_convert(const MixedParams& p, const PfShared& sh, PfValueScale& vs, int j, bool first, uint32_t kv_it, int kv_total) {
+__device__ __forceinline__ bool pf_convert(const MixedParams& p, const PfShared& sh, PfValueScale& vs, float& v_factor, int j, bool first, uint32_t kv_it,
+                                           int kv_total) {
     using G = PfGeo<D>;
     using G8 = PfGeo8<D>;
     constexpr int kChunks = D / 16, kLoads = D / 32;   // 16-byte chunks of a row, per lane
@@ -743,24 +738,24 @@ __device__ __forceinline__ bool pf_convert(const MixedParams& p, const PfShared&
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3])
                      : "r"(raw + row8_chunk<D>(row, c)) : "memory");
     }
-    vs.follow(pf_value_scales<D>(sh, kv_it), first);
     const float scale = lds_f32(pf_value_scales<D>(sh, kv_it) + page * 4);
+    v_factor = vs.follow(pf_value_scales<D>(sh, kv_it), first);
     const int live = kv_total - j * 128;   // rows of the tile inside the prompt
-    const bool plain = scale == vs.ref && (page + 1) * kPageSize <= live;   // warp-uniform
+    const float ratio = scale * vs.inverse;
+    const uint32_t ratio2 = pack_f16x2(ratio, ratio);
     if (!pf_wait(sh, kBarVEmpty + s, (n & 1) ^ 1, p.ctrl, 13)) return false;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
         const int row = page * kPageSize + (i * 32 + lane) / kChunks, c = (i * 32 + lane) % kChunks;
         uint32_t x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = f16x2_of_e4m3(e & 1 ? w[i][e >> 1] >> 16 : w[i][e >> 1]);
-        if (!plain) {
-            const uint32_t ratio = pack_f16x2(scale / vs.ref, scale / vs.ref);
+        for (int e = 0; e < 8; ++e) {
+            x[e] = f16x2_of_e4m3(e & 1 ? w[i][e >> 1] >> 16 : w[i][e >> 1]);
+            asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(x[e]) : "r"(x[e]), "r"(ratio2));
+        }
+        if ((page + 1) * kPageSize > live) {   // warp-uniform
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(x[e]) : "r"(x[e]), "r"(ratio));
-                if (row >= live) x[e] = 0u;
-            }
+            for (int e = 0; e < 8; ++e) x[e] = row >= live ? 0u : x[e];
         }
         // 16-byte pieces 2 c and 2 c + 1 of the row; lanes of the row's second block write theirs in the other order, which keeps the
         // eight lanes of a row off one another's banks
@@ -981,16 +976,16 @@ __device__ __forceinline__ void pf_exp2_pair_fma(uint64_t x2, float& p0, float& 
 
 struct PfSoftmaxState {
     uint32_t s_cnt = 0, o_cnt = 0;  // completions of this tile's S-ready / O-updated barriers consumed so far
-    uint32_t kv_it = 0, q_it = 0, q_cnt[2] = {0, 0};   // kKv8: steps and entries of the CTA before this entry; entries with rows in a tile
+    uint32_t kv_it = 0, q_it = 0;   // kKv8: steps and entries of the CTA before this entry
 };
 
-// kKv8: the thread's row of Q, bf16 in V's operand tile, as the sum of two e4m3 rows.  The row is scaled by a power of two to below 2^8 first; what the
+// kKv8: the thread's row of Q, from bf16 to the sum of two e4m3 rows in the same place (whole tile; 128 threads).  The row is scaled by a power of two to below 2^8 first; what the
 // larger part (4 significant bits) leaves of a bf16 element (8 bits) fits the smaller one exactly, but for what is 2^-18 of the row's largest
 // element.  Returns the scale to multiply scores with (NaN where the row holds anything that is not finite).
 template <int D>
 __device__ __forceinline__ float pf_split_q(const PfShared& sh, int t, int row) {
     using G = PfGeo<D>;
-    const uint32_t src = pf_v_tile<D, kKv8>(sh, t) + row * 128;
+    const uint32_t src = sh.smem + G::kQOffset + t * G::kTileBytes + row * 128;
     uint32_t x[D / 2], top = 0;
 #pragma unroll
     for (int c = 0; c < D / 8; ++c) {
@@ -1002,6 +997,7 @@ __device__ __forceinline__ float pf_split_q(const PfShared& sh, int t, int row) 
     top = max(top & 0xffffu, top >> 16);
     const int e = min(max((int)(top >> 7) - 127, -99), 126);
     const float f = __int_as_float((7 - e + 127) << 23);
+    named_barrier_sync(2 + t, 128);   // every row is in registers
     const uint32_t dst = sh.smem + 2 * t * PfGeo8<D>::kRowTile;
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
@@ -1042,10 +1038,10 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int j_end = min(it.j1, it.nkv[t]);
     const int row = (warp & 3) * 32 + lane;
-    float q_scale = 1.f;
-    PfValueScale vs, vs_ahead;   // of the step that is worked on, and of the one whose V is converted
+    float q_scale = 1.f, v_factor = 1.f, v_ref = 1.f;   // kKv8 (v_ref: the scale that O is in units of)
+    PfValueScale vs;   // of the step whose V was converted last
     const int kv_total = O == kKv8 ? pf_chunk<D, kMulti>(p, sh, 0, it.chunk) + pf_chunk<D, kMulti>(p, sh, 1, it.chunk) : 0;
-    auto convert = [&](int j) { return pf_convert<D>(p, sh, vs_ahead, j, j == it.j0, st.kv_it + (j - it.j0), kv_total); };
+    auto convert = [&](int j) { return pf_convert<D>(p, sh, vs, v_factor, j, j == it.j0, st.kv_it + (j - it.j0), kv_total); };
     if constexpr (O == kKv8) {
         if (j_end > it.j0) {
             if (!pf_wait(sh, kBarQFull, st.q_it & 1, p.ctrl, 14)) return false;
@@ -1054,14 +1050,8 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
             __syncwarp();
             if (lane == 0) mbar_arrive(sh.bars + (kBarQReady + t) * 8);
         }
-#pragma unroll
-        for (int u = 0; u < 2; ++u)   // V's operand tiles hold Q until it is split
-            if (it.nkv[u] > it.j0) {
-                if (!pf_wait(sh, kBarQReady + u, st.q_cnt[u] & 1, p.ctrl, 12)) return false;
-                st.q_cnt[u] += 1;
-            }
         if (!convert(it.j0)) return false;
-        for (int j = max(j_end, it.j0) + 1; j_end <= it.j0 && j < it.j1; ++j)   // a tile without rows
+        for (int j = it.j0 + 1; j_end <= it.j0 && j < it.j1; ++j)   // a tile without rows
             if (!convert(j)) return false;
     }
     if (j_end <= it.j0) return true;  // this tile has no step in this piece
@@ -1140,8 +1130,7 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
             for (int c = 0; c < w; ++c) mxv[c] = fmaxf(mxv[c], mxv[c + w]);
         const float mx = mxv[0];
         const float m_new = fmaxf(m_ref, mx * sl2);
-        float v_factor = 1.f;
-        if constexpr (O == kKv8) v_factor = vs.follow(pf_value_scales<D>(sh, st.kv_it + (j - it.j0)), j == it.j0);
+        if constexpr (O == kKv8) v_ref = vs.ref;
         if (j == it.j0) {
             m_ref = m_new;
         } else {
@@ -1229,7 +1218,7 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
     if (!pf_wait(sh, kBarODone + t, (st.o_cnt + (j_end - it.j0) - 1) & 1, p.ctrl, 11)) return false;
     st.o_cnt += j_end - it.j0;
     tc_fence_after_sync();
-    const float o_unit = O == kKv8 ? vs.ref * 0x1p-7f : 1.f;   // (kPfWeightBits)
+    const float o_unit = O == kKv8 ? v_ref * 0x1p-7f : 1.f;   // (kPfWeightBits)
     if constexpr (O == kKv8) l_sum *= 0x1p-7f;
     const bool row_ok = tok < pf_chunk<D, kMulti>(p, sh, 1, it.chunk);
     const int64_t out_row = (int64_t)pf_chunk<D, kMulti>(p, sh, 2, it.chunk) + tok;

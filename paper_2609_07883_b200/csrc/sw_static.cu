@@ -134,7 +134,7 @@ extern "C" sw_status sw_decode_attn_static(const sw_layout* layout, int device, 
     p.Hq = l.num_q_heads;
     p.Hkv = l.num_kv_heads;
     p.group = g;
-    p.num_pages = l.num_pages;
+    p.num_pages = p.chunk_pool_pages = l.num_pages;
     p.sm_scale = l.sm_scale > 0.f ? l.sm_scale : 1.0f / std::sqrt((float)l.head_dim);
     p.sm_scale_log2 = p.sm_scale * 1.4426950408889634f;
     sw::device_timing(st->mem_khz, st->bus_bits, st->sm_khz, l.head_dim, &p.stage_us, &p.step_us);

@@ -22,8 +22,11 @@ def pool8(c):
     return codes, scales
 
 
-def attend(c, codes, scales):
-    B.sw_kv8_attn_run(c.ctx, codes, scales, c.db, c.q, c.out, c.lse)
+def attend(c, codes, scales, scratch=True):
+    """With a scratch long chunks read a 16-bit copy of their prompts, without one the pool."""
+    pages = sum(-(-(P + C) // U.PAGE) for P, C, _, _ in c.batch.chunks())
+    room = torch.full((B.sw_kv8_scratch_bytes(c.ctx.layout, pages),), 0xFF, dtype=torch.uint8, device=c.dev) if scratch and pages else None
+    B.sw_kv8_attn_run(c.ctx, codes, scales, c.db, c.q, c.out, c.lse, room)
 
 
 def check_append(c, codes, scales):
@@ -130,9 +133,9 @@ def test_decode_units(heads, n):
 
 
 @pytest.mark.parametrize("heads", [(8, 2, 64), (32, 8, 128), (8, 1, 128), (4, 4, 64)])
-@pytest.mark.parametrize("chunks", [[(0, 1)], [(0, 300)], [(1000, 77)], [(3000, 40), (130, 300), (0, 17)]])
-@pytest.mark.parametrize("lens", [[], [100, 1, 700, 3000]])
-def test_chunks(heads, chunks, lens):
+@pytest.mark.parametrize("chunks", [[(0, 1)], [(0, 300)], [(1000, 77)], [(3000, 40), (130, 300), (0, 17)], [(700, 1500)], [(2000, 900), (2000, 900)]])
+@pytest.mark.parametrize("lens,scratch", [([], True), ([100, 1, 700, 3000], True), ([], False), ([100, 1, 700, 3000], False)])
+def test_chunks(heads, chunks, lens, scratch):
     c = U.Case(heads, lens, chunks, seed=len(chunks))
     codes, scales = pool8(c)
     want = U.dequantise(codes, scales)
@@ -140,9 +143,24 @@ def test_chunks(heads, chunks, lens):
     for P, C, _, pages in c.batch.chunks():
         if (P + C) % U.PAGE:
             raw[int(pages[-1]), :, :, (P + C) % U.PAGE:] = 0x7F
-    attend(c, codes, scales)
+    attend(c, codes, scales, scratch)
     c.ok()
     c.check(want)
+
+
+@pytest.mark.parametrize("far", [2.0 ** -13, 2.0 ** -30, 2.0 ** -90, 2.0 ** 5, 2.0 ** 40])
+@pytest.mark.parametrize("chunks,lens,scratch", [([(600, 300)], [], False), ([(600, 300)], [], True), ([], [700, 45], False)])
+def test_scales_that_change_inside_a_context(far, chunks, lens, scratch):
+    """V's scales a long way apart from one stretch of a context to the next, and back; what lies far below the largest counts as little as it
+    weighs.  (Within a stretch of 128 keys they differ by factors of up to 8, as those of neighbouring blocks do.)"""
+    c = U.Case((8, 2, 64), lens, chunks, seed=14)
+    codes, scales = pool8(c)
+    for _, _, _, pages in U.entries_of(c.batch):
+        for j, page in enumerate(pages):
+            scales[int(page), 1] = 2.0 ** (j % 4 - 8) * (far if j // 8 % 2 else 1.0)
+    attend(c, codes, scales, scratch)
+    c.ok()
+    c.check(U.dequantise(codes, scales))
 
 
 @pytest.mark.parametrize("exponent", [-100, -60, -20, 6, 7, 8, 20, 60])
