@@ -4,11 +4,15 @@
 // weights the ones at the lowest positions; NaN counts as the lightest).  The kept keys keep their order.  They go to other pages and
 // another row of weights: pages that requests share stay as they are, and no thread reads what another one writes.
 //
-// Selection (sw_evict_select_kernel): a cluster of 1 to 8 CTAs per pair finds the threshold by radix, 11 + 11 + 10 bits of the weights as ordered
-// integers, with histograms in shared memory that the cluster's CTAs read from one another.  Each CTA has an equal stretch of the pair's keys, the
-// first kHeldKeys of it in shared memory, so the weights are read from memory once.  A last pass writes the kept positions in order.
+// Selection (sw_evict_select_kernel): a cluster of 1 to 8 CTAs per pair finds the threshold by radix, four digits of 8 bits of the weights as ordered
+// integers.  Each CTA has an equal stretch of the pair's keys, the first ones of it in shared memory, so the weights are read from memory once, and a
+// histogram per digit that the cluster's CTAs read from one another.  That traffic is what a pass costs beside its barrier: with digits of 11
+// bits (three passes, 64 KB into every CTA of a cluster of eight) a 32768-token context took 22 us.  From the same histograms every CTA
+// knows how many keys the CTAs before it keep, so a last round writes the kept positions in order.
 // Copy (sw_evict_move_kernel): one warp per (request, new page, KV head); bound by memory.
 #include <cooperative_groups.h>
+
+#include <algorithm>
 
 #include "sw_mixed.cuh"
 
@@ -16,15 +20,19 @@ namespace sw {
 namespace cg = cooperative_groups;
 
 constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
-constexpr int kBins = 2048, kHeldKeys = 12288;   // 48 KB of keys: four CTAs on an SM
+constexpr int kBins = 256, kHeldKeys = 16384, kMaxRanks = 8, kLoadsAhead = 8;
+// Eight lanes in a row count in words of their own: weights have few different exponents, and lanes that add to one word wait for each other
+// (16 contexts of 8192-32768 tokens, 4 CTAs a pair: 53 us with one word a digit).
+constexpr int kCopies = 8;
 constexpr int kMoveThreads = 256;
 
 struct SelectShared {
-    uint32_t hist[kBins];
-    uint32_t held[kHeldKeys];
+    alignas(16) uint32_t counts[kBins * kCopies];   // keys of each digit, by lanes modulo kCopies
+    uint32_t hist[2][kBins];              // the copies' sums, by the parity of the digit
+    uint32_t all[kBins], before[kBins];   // summed over the cluster; over the CTAs before this one
     uint32_t scan[2][kSelectWarps];   // by the parity of the use
-    uint32_t counts[2];   // keys above the threshold and at it in this CTA's stretch
-    uint32_t digit, rest;
+    alignas(16) uint32_t found[4];                // the digit, keys above it in the cluster and in the CTAs before, keys of it in those
+    alignas(16) float held[];
 };
 
 // Floats as integers of the same order; NaN as the lowest.
@@ -47,24 +55,63 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t v, SelectShared& s, in
     uint32_t* words = s.scan[use++ & 1];
     if (lane == 31) words[warp] = inc;
     __syncthreads();
-    uint32_t before = 0, all = 0;
+    uint32_t sum = lane < kSelectWarps ? words[lane] : 0u;
 #pragma unroll
-    for (int w = 0; w < kSelectWarps; ++w) {
-        const uint32_t t = words[w];
-        all += t;
-        if (w < warp) before += t;
+    for (int o = 1; o < kSelectWarps; o <<= 1) {
+        const uint32_t t = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += t;
     }
-    *total = all;
+    *total = __shfl_sync(0xffffffffu, sum, kSelectWarps - 1);
+    const uint32_t before = warp == 0 ? 0u : __shfl_sync(0xffffffffu, sum, warp - 1);
     return before + inc - v;
 }
 
-__global__ void __launch_bounds__(kSelectThreads) sw_evict_select_kernel(const EvictParams p) {
+// The rows of one new page of a pair that keeps `kept` keys (list: p.kept).  Lane groups of D / 8 lanes copy a row each, 16 bytes a lane; all loads of
+// the page's K rows (then V's) are in flight before the first store.
+template <int D>
+__device__ __forceinline__ void move_page(const EvictParams& p, int i, int h, int pg, int kept) {
+    constexpr int kRowLanes = D / 8, kRows = 32 / kRowLanes, kLoads = kPageSize / kRows;
+    const int lane = threadIdx.x & 31, sub = lane / kRowLanes, col = lane % kRowLanes * 8;
+    const int rows = min(kept - pg * kPageSize, kPageSize);
+    if (rows <= 0) return;
+    const int to = p.new_pages[p.new_page_indptr[i] + pg];
+    int from = -1, page = -1;   // lane l < rows: position of slot l's row, and its page
+    if (lane < rows) {
+        from = __ldcg(p.kept + ((int64_t)i * p.Hkv + h) * p.budget + pg * kPageSize + lane);
+        page = p.pages[p.page_indptr[i] + from / kPageSize];
+    }
+    const bool bad = to < 0 || (int64_t)to >= p.num_pages || (lane < rows && (page < 0 || (int64_t)page >= p.num_pages));
+    if (__any_sync(0xffffffffu, bad)) {
+        if (lane == 0) report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteEvict, i);
+        return;
+    }
+#pragma unroll 1
+    for (int side = 0; side < 2; ++side) {
+        const __nv_bfloat16* src = p.pool + (int64_t)side * p.Hkv * kPageSize * D + col;
+        __nv_bfloat16* dst = p.pool + (((int64_t)to * 2 + side) * p.Hkv + h) * kPageSize * D + col;
+        uint4 x[kLoads];
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int slot = j * kRows + sub;
+            const int f = __shfl_sync(0xffffffffu, from, slot), id = __shfl_sync(0xffffffffu, page, slot);
+            if (slot < rows) x[j] = __ldcs(reinterpret_cast<const uint4*>(src + (((int64_t)id * 2 * p.Hkv + h) * kPageSize + f % kPageSize) * D));
+        }
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j)
+            if (j * kRows + sub < rows) __stcs(reinterpret_cast<uint4*>(dst + (j * kRows + sub) * D), x[j]);
+    }
+}
+
+// D: head size where the cluster copies its pair's rows as well, 0 where a launch of its own does.
+template <int D>
+__global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(const EvictParams p) {
     extern __shared__ __align__(16) unsigned char select_raw[];
     SelectShared& s = *reinterpret_cast<SelectShared*>(select_raw);
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int pair = blockIdx.x / ranks, i = pair / p.Hkv, h = pair % p.Hkv;
-    for (int b = threadIdx.x; b < kBins; b += kSelectThreads) s.hist[b] = 0;
+    const int lane = threadIdx.x & 31;
+    for (int b = threadIdx.x; b < kBins * kCopies; b += kSelectThreads) s.counts[b] = 0;
     grid_launch_dependents();
     grid_dependency_wait();
 
@@ -79,6 +126,12 @@ __global__ void __launch_bounds__(kSelectThreads) sw_evict_select_kernel(const E
         if (!fits) report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteEvict, i);
     }
     if (!fits || kept == 0) return;
+    auto move = [&](int count, bool listed_already = false) {   // (in step with the cluster's other CTAs, which write parts of the list)
+        if constexpr (D > 0) {
+            if (!listed_already) cluster.sync();
+            for (int pg = rank * kSelectWarps + (int)threadIdx.x / 32; pg * kPageSize < count; pg += ranks * kSelectWarps) move_page<D>(p, i, h, pg, count);
+        }
+    };
     const float* w = p.weights + ((int64_t)row * p.Hkv + h) * p.capacity;
     float* new_w = p.weights + ((int64_t)new_row * p.Hkv + h) * p.capacity;
     int32_t* list = p.kept + ((int64_t)i * p.Hkv + h) * p.budget;
@@ -88,177 +141,205 @@ __global__ void __launch_bounds__(kSelectThreads) sw_evict_select_kernel(const E
             list[k] = k;
             new_w[k] = w[k];
         }
+        move(kept);
         return;
     }
-    // the keys that stay without asking
     const int fixed = p.sinks + p.recent, wanted = p.budget - fixed;
+    const int keys = len - fixed;   // those that are asked: positions sinks .. sinks + keys - 1
+    const int begin = (int)((int64_t)keys * rank / ranks), mine = (int)((int64_t)keys * (rank + 1) / ranks) - begin;
+    const float* x0 = w + p.sinks + begin;
+    const int held = min(mine, p.held);
+    // four neighbours from k on (a multiple of four), zeros past the end
+    auto weights_of = [&](int k, float (&x)[4]) {
+        if (k + 4 <= held) {
+            const float4 v = *reinterpret_cast<const float4*>(s.held + k);
+            x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[u] = k + u >= mine ? 0.f : (k + u < held ? s.held[k + u] : __ldg(x0 + k + u));
+        }
+    };
+
+    uint32_t prefix = 0, rest = (uint32_t)wanted;   // digits of the threshold so far; how many keys to take among those that share them
+    uint32_t above_before = 0, equal_before = 0;    // keys above the threshold, and at it, in the CTAs before this one
+    __syncthreads();
+#pragma unroll 1
+    for (int pass = 0; wanted > 0 && pass < 4; ++pass) {
+        const int shift = 24 - 8 * pass;
+        uint32_t* hist = s.hist[pass & 1];
+        uint32_t* counts = s.counts + (lane & (kCopies - 1));
+        if (pass == 0) {
+            for (int k0 = threadIdx.x; k0 < mine; k0 += kLoadsAhead * kSelectThreads) {
+                float x[kLoadsAhead];
+#pragma unroll
+                for (int u = 0; u < kLoadsAhead; ++u) x[u] = k0 + u * kSelectThreads < mine ? __ldg(x0 + k0 + u * kSelectThreads) : 0.f;
+#pragma unroll
+                for (int u = 0; u < kLoadsAhead; ++u) {
+                    const int k = k0 + u * kSelectThreads;
+                    if (k < mine) {
+                        if (k < held) s.held[k] = x[u];
+                        atomicAdd(&counts[(ordered(x[u]) >> 24) * kCopies], 1u);
+                    }
+                }
+            }
+        } else {
+#pragma unroll 2
+            for (int k = 4 * threadIdx.x; k < mine; k += 4 * kSelectThreads) {
+                float x[4];
+                weights_of(k, x);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t key = ordered(x[u]);
+                    if (k + u < mine && (key ^ prefix) >> (shift + 8) == 0) atomicAdd(&counts[(key >> shift & (kBins - 1)) * kCopies], 1u);
+                }
+            }
+        }
+        __syncthreads();
+        if (threadIdx.x < kBins) {
+            uint4* own = reinterpret_cast<uint4*>(s.counts + threadIdx.x * kCopies);
+            const uint4 a = own[0], b = own[1];
+            hist[threadIdx.x] = ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
+            own[0] = own[1] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        cluster.sync();   // (also: nobody reads the digit's before the last any more)
+        if (threadIdx.x < kBins) {
+            uint32_t n[kMaxRanks], all = 0, before = 0;   // all in flight at once
+#pragma unroll
+            for (int r = 0; r < kMaxRanks; ++r) n[r] = r < ranks ? cluster.map_shared_rank(hist, r)[threadIdx.x] : 0u;
+#pragma unroll
+            for (int r = 0; r < kMaxRanks; ++r) {
+                all += n[r];
+                before += r < rank ? n[r] : 0u;
+            }
+            s.all[threadIdx.x] = all;
+            s.before[threadIdx.x] = before;
+        }
+        __syncthreads();
+        if (threadIdx.x < 32) {   // eight neighbouring bins a lane, from the highest down
+            const int top = kBins - 8 * (lane + 1);
+            const uint4 a0 = *reinterpret_cast<const uint4*>(s.all + top + 4), a1 = *reinterpret_cast<const uint4*>(s.all + top);
+            const uint4 b0 = *reinterpret_cast<const uint4*>(s.before + top + 4), b1 = *reinterpret_cast<const uint4*>(s.before + top);
+            const uint32_t n[8] = {a0.w, a0.z, a0.y, a0.x, a1.w, a1.z, a1.y, a1.x}, m[8] = {b0.w, b0.z, b0.y, b0.x, b1.w, b1.z, b1.y, b1.x};
+            uint32_t all = 0, before = 0;
+#pragma unroll
+            for (int b = 0; b < 8; ++b) all += n[b], before += m[b];
+            uint32_t n_sum = all, m_sum = before;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t a = __shfl_up_sync(0xffffffffu, n_sum, o), c = __shfl_up_sync(0xffffffffu, m_sum, o);
+                if (lane >= o) n_sum += a, m_sum += c;
+            }
+            n_sum -= all;   // in the bins above the lane's
+            m_sum -= before;
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                if (n_sum < rest && n_sum + n[b] >= rest)   // exactly one bin of one lane
+                    *reinterpret_cast<uint4*>(s.found) = make_uint4((uint32_t)(top + 7 - b), n_sum, m_sum, m[b]);
+                n_sum += n[b];
+                m_sum += m[b];
+            }
+        }
+        __syncthreads();   // (also: the sums are read before they are written again)
+        const uint4 found = *reinterpret_cast<const uint4*>(s.found);
+        prefix |= found.x << shift;
+        rest -= found.y;
+        above_before += found.z;
+        equal_before = found.w;
+    }
+    // the keys that stay without asking
     for (int k = everything; k < fixed; k += step) {
         const int slot = k < p.sinks ? k : p.budget - fixed + k, from = k < p.sinks ? k : len - fixed + k;
         list[slot] = from;
         new_w[slot] = w[from];
     }
-    if (wanted == 0) return;
-    const int keys = len - fixed;   // the others: positions sinks .. sinks + keys - 1
-    const int begin = (int)((int64_t)keys * rank / ranks), mine = (int)((int64_t)keys * (rank + 1) / ranks) - begin;
-    w += p.sinks + begin;
-    const int held = min(mine, kHeldKeys);
-    auto key_of = [&](int k) { return k < held ? s.held[k] : ordered(__ldg(w + k)); };
-
-    uint32_t prefix = 0, rest = (uint32_t)wanted;   // bits of the threshold found so far; how many keys to take among those that share them
+    if (wanted == 0) {
+        move(kept);
+        return;
+    }
     int use = 0;
+    // In order of position, four neighbours per thread and round.  (Put side by side in shared memory first, to leave in whole lines: no faster.)
+    constexpr int kEach = 4;
 #pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : 2048;
-        const uint32_t known = pass == 0 ? 0u : ~0u << (pass == 1 ? 21 : 10);   // the bits that are fixed already
-        if (pass > 0)
-            for (int b = threadIdx.x; b < kBins; b += kSelectThreads) s.hist[b] = 0;
-        __syncthreads();
-        if (pass == 0) {
-#pragma unroll 4
-            for (int k = threadIdx.x; k < mine; k += kSelectThreads) {
-                const uint32_t key = ordered(__ldg(w + k));
-                if (k < held) s.held[k] = key;
-                atomicAdd(&s.hist[key >> 21], 1u);
-            }
-        } else {
-            for (int k = threadIdx.x; k < mine; k += kSelectThreads) {
-                const uint32_t key = key_of(k);
-                if ((key & known) == prefix) atomicAdd(&s.hist[(key >> shift) & (bins - 1)], 1u);
-            }
-        }
-        cluster.sync();
-        // four neighbouring bins per thread, from the highest down, summed over the cluster
-        uint32_t n[4] = {0, 0, 0, 0}, all = 0, total;
-        const int top = kBins - 1 - 4 * (int)threadIdx.x;
-        for (int r = 0; r < ranks; ++r) {
-            const uint4 v = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(s.hist, r) + top - 3);
-            n[0] += v.w, n[1] += v.z, n[2] += v.y, n[3] += v.x;
-        }
+    for (int k0 = 0; k0 < mine; k0 += kEach * kSelectThreads) {
+        const int first = k0 + kEach * (int)threadIdx.x;
+        float x[kEach];
+        weights_of(first, x);
+        uint32_t flags = 0, counts = 0;   // bit u: above, bit 4 + u: equal; two counts of at most 2048
 #pragma unroll
-        for (int b = 0; b < 4; ++b) all += n[b];
-        uint32_t before = block_prefix(all, s, use, &total);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            if (before < rest && before + n[b] >= rest) {   // exactly one thread and bin
-                s.digit = (uint32_t)(top - b);
-                s.rest = rest - before;
-            }
-            before += n[b];
+        for (int u = 0; u < kEach; ++u) {
+            const uint32_t key = ordered(x[u]);
+            if (first + u < mine && key > prefix) flags |= 1u << u, counts += 1u << 16;
+            if (first + u < mine && key == prefix) flags |= 16u << u, counts += 1u;
         }
-        cluster.sync();   // (also: nobody clears a histogram that another CTA still reads)
-        prefix |= s.digit << shift;
-        rest = s.rest;
-        __syncthreads();
-    }
-    // keys above the threshold, and at it: of those the first `rest` by position
-    uint32_t above = 0, equal = 0;
-    for (int k = threadIdx.x; k < mine; k += kSelectThreads) {
-        const uint32_t key = key_of(k);
-        above += key > prefix;
-        equal += key == prefix;
-    }
-    uint32_t total_above, total_equal;
-    block_prefix(above, s, use, &total_above);
-    block_prefix(equal, s, use, &total_equal);
-    if (threadIdx.x == 0) {
-        s.counts[0] = total_above;
-        s.counts[1] = total_equal;
-    }
-    cluster.sync();
-    uint32_t above_before = 0, equal_before = 0;
-    for (int r = 0; r < rank; ++r) {
-        const uint32_t* c = cluster.map_shared_rank(s.counts, r);
-        above_before += c[0];
-        equal_before += c[1];
-    }
-#pragma unroll 1
-    for (int k0 = 0; k0 < mine; k0 += kSelectThreads) {
-        const int k = k0 + threadIdx.x;
-        const uint32_t key = k < mine ? key_of(k) : 0u;
-        const bool is_above = k < mine && key > prefix, is_equal = k < mine && key == prefix;
-        uint32_t tile;   // two counts of at most 512
-        const uint32_t b = block_prefix((is_above ? 1u << 16 : 0u) | (is_equal ? 1u : 0u), s, use, &tile);
-        const uint32_t my_above = above_before + (b >> 16), my_equal = equal_before + (b & 0xffffu);
-        if (is_above || (is_equal && my_equal < rest)) {
-            const int slot = p.sinks + (int)(my_above + min(my_equal, rest)), from = p.sinks + begin + k;
-            list[slot] = from;
-            new_w[slot] = w[k];
+        uint32_t tile;
+        const uint32_t b = block_prefix(counts, s, use, &tile);
+        uint32_t my_above = above_before + (b >> 16), my_equal = equal_before + (b & 0xffffu);
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            const bool is_above = flags >> u & 1, is_equal = flags >> (4 + u) & 1;
+            if (is_above || (is_equal && my_equal < rest)) {
+                const int slot = p.sinks + (int)(my_above + min(my_equal, rest));
+                list[slot] = p.sinks + begin + first + u;
+                new_w[slot] = x[u];
+            }
+            my_above += is_above;
+            my_equal += is_equal;
         }
         above_before += tile >> 16;
         equal_before += tile & 0xffffu;
     }
-    cluster.sync();   // a CTA's counts and histogram are read by the others
+    cluster.sync();   // a CTA's last histogram is read by the others
+    if constexpr (D > 0) move(kept, true);
 }
 
-// Lane groups of D / 8 lanes copy a row each, 16 bytes a lane; all loads of a page's K and V rows are in flight before the first store.
+// One launch: a warp per (request, new page, KV head).
 template <int D>
 __global__ void __launch_bounds__(kMoveThreads) sw_evict_move_kernel(const EvictParams p) {
-    constexpr int kRowLanes = D / 8, kRows = 32 / kRowLanes, kLoads = kPageSize / kRows;
     grid_dependency_wait();
-    const int lane = threadIdx.x & 31, sub = lane / kRowLanes, col = lane % kRowLanes * 8;
     const int new_pages = (p.budget - 1) / kPageSize + 1;
     const int64_t tasks = (int64_t)p.n * new_pages * p.Hkv;
     for (int64_t t = (int64_t)blockIdx.x * (kMoveThreads / 32) + threadIdx.x / 32; t < tasks; t += (int64_t)gridDim.x * (kMoveThreads / 32)) {
         const int h = (int)(t % p.Hkv), pg = (int)(t / p.Hkv % new_pages), i = (int)(t / p.Hkv / new_pages);
-        const int rows = min(p.new_len[i] - pg * kPageSize, kPageSize);
-        if (rows <= 0) continue;
-        const int to = p.new_pages[p.new_page_indptr[i] + pg];
-        int from = -1, page = -1;   // lane l < rows: position of slot l's row, and its page
-        if (lane < rows) {
-            from = p.kept[((int64_t)i * p.Hkv + h) * p.budget + pg * kPageSize + lane];
-            page = p.pages[p.page_indptr[i] + from / kPageSize];
-        }
-        const bool bad = to < 0 || (int64_t)to >= p.num_pages || (lane < rows && (page < 0 || (int64_t)page >= p.num_pages));
-        if (__any_sync(0xffffffffu, bad)) {
-            if (lane == 0) report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteEvict, i);
-            continue;
-        }
-        uint4 k[kLoads], v[kLoads];
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int slot = j * kRows + sub;
-            const int f = __shfl_sync(0xffffffffu, from, slot), pgid = __shfl_sync(0xffffffffu, page, slot);
-            if (slot < rows) {
-                const __nv_bfloat16* src = p.pool + ((((int64_t)pgid * 2 * p.Hkv) + h) * kPageSize + f % kPageSize) * D + col;
-                k[j] = __ldcs(reinterpret_cast<const uint4*>(src));
-                v[j] = __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)p.Hkv * kPageSize * D));
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int slot = j * kRows + sub;
-            if (slot < rows) {
-                __nv_bfloat16* dst = p.pool + ((((int64_t)to * 2 * p.Hkv) + h) * kPageSize + slot) * D + col;
-                __stcs(reinterpret_cast<uint4*>(dst), k[j]);
-                __stcs(reinterpret_cast<uint4*>(dst + (int64_t)p.Hkv * kPageSize * D), v[j]);
-            }
-        }
+        move_page<D>(p, i, h, pg, p.new_len[i]);
     }
 }
 
+template <class F>
+cudaError_t for_each_select(F f) {
+    cudaError_t e = f(sw_evict_select_kernel<0>);
+    if (e == cudaSuccess) e = f(sw_evict_select_kernel<64>);
+    return e == cudaSuccess ? f(sw_evict_select_kernel<128>) : e;
+}
 cudaError_t configure_evict_kernels() {
-    return cudaFuncSetAttribute(sw_evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SelectShared));
+    return for_each_select([](auto* kernel) {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(SelectShared) + kHeldKeys * sizeof(float)));
+    });
 }
 
-cudaError_t launch_evict(const EvictParams& p, int head_dim, int num_sms, cudaStream_t stream) {
+cudaError_t launch_evict(const EvictParams& params, int head_dim, int num_sms, cudaStream_t stream) {
+    EvictParams p = params;
+    const int64_t pairs = (int64_t)p.n * p.Hkv;
+    // as many CTAs per pair as keep the launch within two CTAs an SM
+    int ranks = kMaxRanks;
+    while (ranks > 1 && pairs * ranks > 2 * (int64_t)num_sms) ranks /= 2;
+    p.held = std::min(kHeldKeys, (p.capacity + ranks - 1) / ranks);
+    const bool fused = pairs * ranks >= num_sms;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    // as many CTAs per pair as keep the launch within three CTAs an SM
-    const int64_t pairs = (int64_t)p.n * p.Hkv;
-    int ranks = 8;
-    while (ranks > 1 && pairs * ranks > 3 * (int64_t)num_sms) ranks /= 2;
     attr[1].val.clusterDim.x = ranks;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(pairs * ranks));
     cfg.blockDim = dim3(kSelectThreads);
-    cfg.dynamicSmemBytes = sizeof(SelectShared);
+    cfg.dynamicSmemBytes = sizeof(SelectShared) + (size_t)p.held * sizeof(float);
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, sw_evict_select_kernel, p);
+    if (fused)
+        return head_dim == 64 ? cudaLaunchKernelEx(&cfg, sw_evict_select_kernel<64>, p) : cudaLaunchKernelEx(&cfg, sw_evict_select_kernel<128>, p);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, sw_evict_select_kernel<0>, p);
     if (e != cudaSuccess) return e;
     const int64_t tasks = pairs * ((p.budget - 1) / kPageSize + 1), blocks = (tasks + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
     cfg.gridDim = dim3((unsigned)(blocks < 8 * (int64_t)num_sms ? blocks : 8 * (int64_t)num_sms));

@@ -120,6 +120,7 @@ struct WeightParams {
 
 struct EvictParams {
     int n, Hkv, capacity, budget, sinks, recent;
+    int held;   // weights that a CTA of the selection keeps in shared memory
     int64_t num_pages, rows;
     const int32_t *kv_len, *page_indptr, *pages, *row_of;
     const int32_t *new_page_indptr, *new_pages, *new_row_of;
