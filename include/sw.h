@@ -192,7 +192,7 @@ typedef struct {
 
 /* sw_mixed_attn_run of a decode-only iteration that also adds up what weight every key got: the weight of key k of request i and a KV head grows
  * by the sum over the head's group of exp(score - log-sum-exp).  The request's last key is set instead (it is attended for the first time).
- * lse must be given, on a 16-byte boundary.  scratch: 16-byte aligned device memory of sw_attn_weights_scratch_bytes(layout,
+ * lse must be given, on a 16-byte boundary.  scratch: 128-byte aligned device memory of sw_attn_weights_scratch_bytes(layout,
  * decode_page_indptr[num_decode]) bytes, of no use between calls.  A request that does not fit (row outside the weights, context longer than a
  * row, pages beyond the scratch) is reported by sw_check_status; its output is written, its weights are not (nor, beyond the scratch, those of
  * the pages there).  The sums do not depend on any order.  SW_ERR_UNSUPPORTED for batches with chunks.  Asynchronous (two launches). */

@@ -677,7 +677,8 @@ sw_status sw_decode_attn_weights_run(sw_ctx* ctx, const void* kv_pool, const sw_
     if (st != SW_OK) return st;
     st = check_current_device(ctx, who);
     if (st != SW_OK) return st;
-    if (!aligned16(q, out, lse, scratch)) return sw_fail(SW_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
+    if (!aligned16(q, out, lse)) return sw_fail(SW_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
+    if ((reinterpret_cast<uintptr_t>(scratch) & 127) != 0) return sw_fail(SW_ERR_WORKSPACE, "%s: scratch must be 128-byte aligned", who);
     const sw::KvMaps* kv_maps = nullptr;
     st = kv_map_for(ctx, kv_pool, &kv_maps);
     if (st != SW_OK) return st;

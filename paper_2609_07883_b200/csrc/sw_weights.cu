@@ -13,21 +13,24 @@ namespace sw {
 constexpr int kWeightThreads = 256, kWeightBlocksPerSm = 4;
 
 // A warp has an equal stretch of the entries of decode_pages; of a page, lane l has key l % 16 and every second KV head.
+//
+// Scores that have been read are discarded from L2: written back to memory, as 25 MB of them are in the course of four contexts of 49152 tokens, they
+// cost the launches 7 us of 147.
 __global__ void __launch_bounds__(kWeightThreads, kWeightBlocksPerSm) sw_key_weights_kernel(const WeightParams p) {
     grid_launch_dependents();
-    grid_dependency_wait();
+    // The batch was there before the attention launch started: where the warp's stretch lies is found while that ends.
     const int lane = threadIdx.x & 31, warps = gridDim.x * (kWeightThreads / 32), w = blockIdx.x * (kWeightThreads / 32) + threadIdx.x / 32;
-    const int64_t total = p.n > 0 ? p.page_indptr[p.n] : 0;
+    const int64_t total = __ldcg(p.page_indptr + p.n);
     const int begin = (int)(total * w / warps), end = (int)(total * (w + 1) / warps);
-    if (begin >= end) return;
-    int lo = 0, hi = p.n;   // largest i with page_indptr[i] <= begin
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.page_indptr[mid] <= begin) lo = mid; else hi = mid;
+    int i = 0;
+    for (int hi = p.n; hi - i > 1;) {   // largest i with page_indptr[i] <= begin
+        const int mid = (i + hi) >> 1;
+        if (__ldcg(p.page_indptr + mid) <= begin) i = mid; else hi = mid;
     }
+    grid_dependency_wait();
     constexpr float kLog2E = 1.4426950408889634f;
-    const int key = lane & 15, g = p.group;
-    int i = lo, at = 0, next = begin, len = 0, row = 0;
+    const int key = lane & 15, g = p.group, lines = p.Hkv * kPageSize * g / 32;   // of 128 bytes, of a page's scores
+    int at = 0, next = begin, len = 0, row = 0;
     bool ok = false;
     for (int e = begin; e < end; ++e) {
         if (e == begin || e >= next) {
@@ -44,28 +47,33 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocksPerSm) sw_key_wei
             }
         }
         const int pos = (e - at) * kPageSize + key;
-        if (!ok || pos >= len) continue;
-        if (e >= p.score_pages) {
-            report(p.ctrl, SW_ERR_WORKSPACE, kSiteScratch, e & 0xffffff);
-            continue;
+        if (ok && pos - key < len && e >= p.score_pages) {
+            if (lane == 0) report(p.ctrl, SW_ERR_WORKSPACE, kSiteScratch, e);
+            ok = false;   // (like all pages behind it)
         }
-        const float* scores = p.scores + ((int64_t)e * p.Hkv * kPageSize + key) * g;
-        const float* lse = p.lse + (int64_t)i * p.Hkv * g;
-        float* dst = p.weights + (int64_t)row * p.Hkv * p.capacity + pos;
+        const float* scores = p.scores + (int64_t)e * p.Hkv * kPageSize * g;
+        if (ok && pos < len) {
+            const float* lse = p.lse + (int64_t)i * p.Hkv * g;
+            float* dst = p.weights + (int64_t)row * p.Hkv * p.capacity + pos;
 #pragma unroll 4
-        for (int h = lane >> 4; h < p.Hkv; h += 2) {
-            const float before = pos == len - 1 ? 0.f : dst[(int64_t)h * p.capacity];   // the key of this step starts at nothing
-            float sum = 0.f;
-            if (g == 4) {
-                const float4 s = __ldcs(reinterpret_cast<const float4*>(scores + h * kPageSize * 4));
-                const float4 l = __ldg(reinterpret_cast<const float4*>(lse + h * 4));
-                sum = (fast_exp2(fmaf(l.x, -kLog2E, s.x)) + fast_exp2(fmaf(l.y, -kLog2E, s.y))) +
-                      (fast_exp2(fmaf(l.z, -kLog2E, s.z)) + fast_exp2(fmaf(l.w, -kLog2E, s.w)));
-            } else {
-                for (int r = 0; r < g; ++r) sum += fast_exp2(fmaf(__ldg(lse + h * g + r), -kLog2E, __ldcs(scores + h * kPageSize * g + r)));
+            for (int h = lane >> 4; h < p.Hkv; h += 2) {
+                const float before = pos == len - 1 ? 0.f : dst[(int64_t)h * p.capacity];   // the key of this step starts at nothing
+                const float* s0 = scores + (h * kPageSize + key) * g;
+                float sum = 0.f;
+                if (g == 4) {
+                    const float4 s = __ldcs(reinterpret_cast<const float4*>(s0));
+                    const float4 l = __ldg(reinterpret_cast<const float4*>(lse + h * 4));
+                    sum = (fast_exp2(fmaf(l.x, -kLog2E, s.x)) + fast_exp2(fmaf(l.y, -kLog2E, s.y))) +
+                          (fast_exp2(fmaf(l.z, -kLog2E, s.z)) + fast_exp2(fmaf(l.w, -kLog2E, s.w)));
+                } else {
+                    for (int r = 0; r < g; ++r) sum += fast_exp2(fmaf(__ldg(lse + h * g + r), -kLog2E, __ldcs(s0 + r)));
+                }
+                dst[(int64_t)h * p.capacity] = before + sum;
             }
-            dst[(int64_t)h * p.capacity] = before + sum;
         }
+        __syncwarp();
+        if (e < p.score_pages && (lines * 32) == p.Hkv * kPageSize * g)
+            for (int l = lane; l < lines; l += 32) asm volatile("discard.global.L2 [%0], 128;" ::"l"(scores + l * 32) : "memory");
     }
 }
 

@@ -284,6 +284,9 @@ def test_refusals():
         with pytest.raises(B.SwError) as e:
             B.sw_decode_attn_weights_run(d.ctx, d.pool, d.db, d.q, d.out, lse, kw, s)
         assert e.value.status == B.SW_ERR_INVALID_ARG
+    with pytest.raises(B.SwError) as e:
+        B.sw_decode_attn_weights_run(d.ctx, d.pool, d.db, d.q, d.out, d.lse, kw, scratch[16:])
+    assert e.value.status == B.SW_ERR_WORKSPACE
     for budget, sinks, recent in [(0, 0, 0), (65, 0, 0), (16, 10, 7), (16, -1, 0), (16, 0, -1)]:
         with pytest.raises(B.SwError) as e:
             B.sw_kv_evict(d.ctx, d.pool, d.db, kw, ints, ints, new, budget, sinks, recent, ints, ints)
