@@ -739,85 +739,6 @@ __device__ __forceinline__ int rows_to_merge(int32_t* ready, const int32_t* star
     return own;
 }
 
-// A decode unit's queries as B fragments of Q^T: the lane holds head lane / 4, elements 2 (lane % 4) + {0, 1} (+ 8) of every 16.
-// kKv8: what an 8-bit unit carries beside DecodeState.  Its products take f16 operands, into which e4m3 values convert exactly.
-//   Queries: a head's row is scaled by a power of two to below 2^15, so its bf16 elements are f16 numbers (those 2^-31 below the largest and more are
-//   rounded); q0, q1 undo that for the lane's two heads.
-//   Weights: p 2^15 as f16, which is finer than bf16 down to 2^-29 of the largest weight and loses what is 2^-40 below it.
-//   V's scales: O is kept in units of `ref`, the scale of a page so far, which follows the pages' scales upward, and downward where a page's is
-//   2^-16 of it or less; in between the ratio goes into the page's weights.  Following takes no instruction beside the online softmax's own
-//   correction.  `top`: the largest ref; a scale 2^-80 below it (a block of zeros, say) is not followed, or O might overflow.
-template <Option O>
-struct Kv8State {};
-template <>
-struct Kv8State<kKv8> {
-    float q0, q1, ref, top;
-};
-constexpr float kKv8WeightBits = 15.f, kKv8WeightUnit = 0.000030517578125f;   // 2^-15
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
-    uint32_t d;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
-}
-__device__ __forceinline__ uint32_t f16x2_of_e4m3(uint32_t pair) {   // of the lower two bytes
-    uint32_t d;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(d) : "h"((uint16_t)pair));
-    return d;
-}
-__device__ __forceinline__ float2 f32x2_of_f16x2(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
-__device__ __forceinline__ uint32_t e4m3x4_of(float a, float b, float c, float d) {   // bytes a, b, c, d from the lowest on
-    uint16_t lo, hi;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
-    return (uint32_t)hi << 16 | lo;
-}
-// D(16x8, f32) += A(16x16, f16, row) * B(16x8, f16, col)
-__device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-// (kKv8: elements 4 (lane % 4) + {0, 1} and + {2, 3}, the order in which 8-bit keys come out of their words.)
-template <int D, Option O>
-__device__ __forceinline__ void load_query(const MixedParams& p, int q_row, int kvh, uint32_t (&qb)[D / 16][2], Kv8State<O>& k8) {
-    const int lane = threadIdx.x & 31;
-    if constexpr (O == kKv8) {
-        const uint2* src = reinterpret_cast<const uint2*>(p.q + ((int64_t)q_row * p.Hq + kvh * p.group + (lane >> 2)) * D + (lane & 3) * 4);
-        uint32_t top = 0;   // bf16 magnitudes compare like integers
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-            const uint2 x = (lane >> 2) < p.group ? src[ks * 4] : make_uint2(0u, 0u);
-            qb[ks][0] = x.x;
-            qb[ks][1] = x.y;
-            top = __vmaxu2(top, __vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu));
-        }
-        top = max(top & 0xffffu, top >> 16);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // 2^(14 - exponent of the largest), between 2^-113 and 2^113
-        const int e = min(max((int)(top >> 7) - 127, -99), 126);
-        const float f = __int_as_float((14 - e + 127) << 23), inverse = __int_as_float((e - 14 + 127) << 23);
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                qb[ks][i] = pack_f16x2(__uint_as_float(qb[ks][i] << 16) * f, __uint_as_float(qb[ks][i] & 0xffff0000u) * f);
-        k8.q0 = __shfl_sync(0xffffffffu, inverse, (lane & 3) * 8);       // lanes of heads 2 (lane % 4) and the next
-        k8.q1 = __shfl_sync(0xffffffffu, inverse, (lane & 3) * 8 + 4);
-        k8.ref = k8.top = 0.f;
-        return;
-    }
-    const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + ((int64_t)q_row * p.Hq + kvh * p.group + (lane >> 2)) * D + (lane & 3) * 2);
-    const bool live = (lane >> 2) < p.group;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-        qb[ks][0] = live ? src[ks * 8] : 0u;
-        qb[ks][1] = live ? src[ks * 8 + 4] : 0u;
-    }
-}
-
 // O^T of the keys so far: columns 16 t + lane / 4 (+ 8) of heads 2 (lane % 4) + {0, 1}; m of those two heads; l over the lane's own keys.
 template <int D>
 struct DecodeState {
@@ -831,22 +752,43 @@ struct DecodeState {
     }
 };
 
+}  // namespace sw
+#include "sw_kv8.cuh"
+namespace sw {
+
+// A decode unit's queries as B fragments of Q^T: the lane holds head lane / 4, elements 2 (lane % 4) + {0, 1} (+ 8) of every 16.
+// (kKv8: elements 4 (lane % 4) + {0, 1} and + {2, 3}, the order in which 8-bit keys come out of their words.)
+template <int D, Option O>
+__device__ __forceinline__ void load_query(const MixedParams& p, int q_row, int kvh, uint32_t (&qb)[D / 16][2], Kv8State<O>& k8) {
+    const int lane = threadIdx.x & 31;
+    if constexpr (O == kKv8) {
+        load_query8<D>(p, q_row, kvh, qb, k8);
+        return;
+    }
+    const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + ((int64_t)q_row * p.Hq + kvh * p.group + (lane >> 2)) * D + (lane & 3) * 2);
+    const bool live = (lane >> 2) < p.group;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        qb[ks][0] = live ? src[ks * 8] : 0u;
+        qb[ks][1] = live ? src[ks * 8 + 4] : 0u;
+    }
+}
+
+// What else a page's products need.  kWindow: its keys from `from` on and those below `sinks` are attended (counted from the page's first
+// key).  kScored: where its scores go (the page's [16 keys][group]), null for nowhere.
+struct PageExtra {
+    int from, sinks;
+    float* scores;
+};
+
 // One page (K and V of a head at sK, `valid` keys of it attended) on one warp.
 //
 // The products are transposed: the 16 rows of an mma.m16n8k16 are keys (of S = K Q^T) or output columns (of O^T = V^T P^T) and
 // its 8 columns are the query heads of the group (columns past the group are zero queries), half the instructions of the form
 // with the heads as rows, which would be padded to 16.
-// What else a page's products need.  kWindow: its keys from `from` on and those below `sinks` are attended (counted from the page's first
-// key).  kKv8: the scales of its K and V.  kScored: where its scores go (the page's [16 keys][group]), null for nowhere.
-struct PageExtra {
-    int from, sinks;
-    float2 scale;
-    float* scores;
-};
-
 template <int D, Option O>
 __device__ __forceinline__ void attend_page(const MixedParams& p, uint32_t sK, int valid, const uint32_t (&qb)[D / 16][2], DecodeState<D>& st,
-                                            Kv8State<O>& k8, const PageExtra& x) {
+                                            const PageExtra& x) {
     constexpr int KS = D / 16;  // k-slices of K Q^T; also 16-column tiles of O
     const int lane = threadIdx.x & 31;
     // Per-lane offsets of the ldmatrix rows: the four 8x8 matrices are keys 0-7 / 8-15 of one 8-element block, then of the next
@@ -857,38 +799,19 @@ __device__ __forceinline__ void attend_page(const MixedParams& p, uint32_t sK, i
                             ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
     // S^T = K Q^T for 16 keys, in two chains
     float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};
-    if constexpr (O == kKv8) {
-        // 8-bit keys: the two words of a lane are its two keys' bytes 4 (lane % 4) .. + 3 of a 16-byte chunk, hence the order of load_query
-        const uint32_t addr = D == 128 ? k_addr : sK + (lane & 15) * 64 + (((lane >> 4) ^ (lane >> 1 & 3)) << 4);
 #pragma unroll
-        for (int ks = 0; ks < KS; ks += 2) {
-            uint32_t r[4];   // keys 0-7 and 8-15 of one chunk, then of the next
-            ldmatrix_x4(addr ^ (ks * 16), r[0], r[1], r[2], r[3]);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                mma_f16_16816(h ? s2 : s, f16x2_of_e4m3(r[2 * h]), f16x2_of_e4m3(r[2 * h + 1]), f16x2_of_e4m3(r[2 * h] >> 16),
-                              f16x2_of_e4m3(r[2 * h + 1] >> 16), qb[ks + h][0], qb[ks + h][1]);
-        }
-        const float f0 = x.scale.x * k8.q0, f1 = x.scale.x * k8.q1;
-        s[0] = (s[0] + s2[0]) * f0;
-        s[1] = (s[1] + s2[1]) * f1;
-        s[2] = (s[2] + s2[2]) * f0;
-        s[3] = (s[3] + s2[3]) * f1;
-    } else {
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            uint32_t a0, a1, a2, a3;
-            ldmatrix_x4((k_addr ^ ((ks & 3) * 32)) + (ks >> 2) * Geo<D>::kBlockBytes, a0, a1, a2, a3);
-            mma_bf16_16816(ks & 1 ? s2 : s, a0, a1, a2, a3, qb[ks][0], qb[ks][1]);
-        }
+    for (int ks = 0; ks < KS; ++ks) {
+        uint32_t a0, a1, a2, a3;
+        ldmatrix_x4((k_addr ^ ((ks & 3) * 32)) + (ks >> 2) * Geo<D>::kBlockBytes, a0, a1, a2, a3);
+        mma_bf16_16816(ks & 1 ? s2 : s, a0, a1, a2, a3, qb[ks][0], qb[ks][1]);
     }
     // the lane's keys are lane / 4 and lane / 4 + 8; keys past the context (and, with a window, in front of it) are masked
     auto attended = [&](int key) { return key < valid && (O != kWindow || key >= x.from || key < x.sinks); };
     const bool ok0 = attended(lane >> 2), ok1 = attended((lane >> 2) + 8);
-    s[0] = ok0 ? (O == kKv8 ? s[0] : s[0] + s2[0]) : -INFINITY;
-    s[1] = ok0 ? (O == kKv8 ? s[1] : s[1] + s2[1]) : -INFINITY;
-    s[2] = ok1 ? (O == kKv8 ? s[2] : s[2] + s2[2]) : -INFINITY;
-    s[3] = ok1 ? (O == kKv8 ? s[3] : s[3] + s2[3]) : -INFINITY;
+    s[0] = ok0 ? s[0] + s2[0] : -INFINITY;
+    s[1] = ok0 ? s[1] + s2[1] : -INFINITY;
+    s[2] = ok1 ? s[2] + s2[2] : -INFINITY;
+    s[3] = ok1 ? s[3] + s2[3] : -INFINITY;
     if constexpr (O == kScored) {   // in powers of two, like the sums of weights that are taken from them
         const int h = 2 * (lane & 3);
         if (x.scores && h < p.group) {
@@ -910,32 +833,16 @@ __device__ __forceinline__ void attend_page(const MixedParams& p, uint32_t sK, i
     }
     mx0 = fmaxf(st.m0, mx0);
     mx1 = fmaxf(st.m1, mx1);
-    float c0 = fast_exp2((st.m0 - mx0) * p.sm_scale_log2), c1 = fast_exp2((st.m1 - mx1) * p.sm_scale_log2);
+    const float c0 = fast_exp2((st.m0 - mx0) * p.sm_scale_log2), c1 = fast_exp2((st.m1 - mx1) * p.sm_scale_log2);
     st.m0 = mx0;
     st.m1 = mx1;
-    const float bits = O == kKv8 ? kKv8WeightBits : 0.f;
-    const float b0 = mx0 * p.sm_scale_log2 - bits, b1 = mx1 * p.sm_scale_log2 - bits;
+    const float b0 = mx0 * p.sm_scale_log2, b1 = mx1 * p.sm_scale_log2;
     s[0] = fast_exp2(fmaf(s[0], p.sm_scale_log2, -b0));
     s[1] = fast_exp2(fmaf(s[1], p.sm_scale_log2, -b1));
     s[2] = fast_exp2(fmaf(s[2], p.sm_scale_log2, -b0));
     s[3] = fast_exp2(fmaf(s[3], p.sm_scale_log2, -b1));
     st.l0 = st.l0 * c0 + (s[0] + s[2]);
     st.l1 = st.l1 * c1 + (s[1] + s[3]);
-    if constexpr (O == kKv8) {
-        const float sv = x.scale.y;
-        if (!(sv == k8.ref)) {   // warp-uniform
-            const float ratio = sv / k8.ref;
-            if (sv > k8.ref || (ratio < 0x1p-16f && sv >= k8.top * 0x1p-80f)) {
-                c0 *= k8.ref / sv;
-                c1 *= k8.ref / sv;
-                k8.ref = sv;
-                k8.top = fmaxf(k8.top, sv);
-            } else {   // (a NaN ends here)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] *= ratio;
-            }
-        }
-    }
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
         st.o[i][0] *= c0;
@@ -944,41 +851,8 @@ __device__ __forceinline__ void attend_page(const MixedParams& p, uint32_t sK, i
         st.o[i][3] *= c1;
     }
     // P^T [keys][heads] as the B operand: keys along the fragment's registers, so the 8x8 blocks are transposed
-    const uint32_t p0 = movmatrix_trans(O == kKv8 ? pack_f16x2(s[0], s[1]) : pack_bf16x2(s[0], s[1]));
-    const uint32_t p1 = movmatrix_trans(O == kKv8 ? pack_f16x2(s[2], s[3]) : pack_bf16x2(s[2], s[3]));
+    const uint32_t p0 = movmatrix_trans(pack_bf16x2(s[0], s[1])), p1 = movmatrix_trans(pack_bf16x2(s[2], s[3]));
 
-    if constexpr (O == kKv8) {
-        // A lane's four keys are 2 (lane % 4) + {0, 1} (+ 8), its columns the (lane / 4)-th eighth of the row: the bytes of two keys in one
-        // column make a register of V^T, without a transpose.
-        constexpr int W = D / 32;   // words of a row's eighth
-        uint32_t w[4][W];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = 2 * (lane & 3) + (i & 1) + 8 * (i >> 1), c = lane >> 2;
-            const uint32_t v8 = sK + kPageSize * D + row * D;
-            if constexpr (D == 128)
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3])
-                             : "r"(v8 + ((c ^ (row & 7)) << 4)) : "memory");
-            else
-                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[i][0]), "=r"(w[i][1])
-                             : "r"(v8 + (((c >> 1) ^ (row >> 1 & 3)) << 4) + (c & 1) * 8) : "memory");
-        }
-        if (valid < kPageSize) {   // slots past the context hold anything, NaN among it
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < W; ++j)
-                    if (2 * (lane & 3) + (i & 1) + 8 * (i >> 1) >= valid) w[i][j] = 0u;
-        }
-#pragma unroll
-        for (int t = 0; t < KS; ++t) {
-            const int j = t >> 1;
-            const uint32_t sel = t & 1 ? 0x7362 : 0x5140;   // of two keys' words: byte 0 (2) of both, then byte 1 (3) of both
-            const uint32_t lo = __byte_perm(w[0][j], w[1][j], sel), hi = __byte_perm(w[2][j], w[3][j], sel);
-            mma_f16_16816(st.o[t], f16x2_of_e4m3(lo), f16x2_of_e4m3(lo >> 16), f16x2_of_e4m3(hi), f16x2_of_e4m3(hi >> 16), p0, p1);
-        }
-        return;
-    }
     if constexpr (O == kWindow) {   // the rows in front of the window are not attended by anybody any more: they may hold anything
         if (x.from > max(0, x.sinks)) {
             __syncwarp();
@@ -1025,17 +899,8 @@ __device__ __forceinline__ void stage_result(uint32_t dst, int g, DecodeState<D>
         st.l1 += __shfl_xor_sync(0xffffffffu, st.l1, w);
     }
     const int h = (lane & 3) * 2;
-    if constexpr (O == kKv8) {   // the lane's columns are 2 t + {0, 1} of the row's (lane / 4)-th eighth
-        const float f = k8.ref * kKv8WeightUnit;
-        st.l0 *= kKv8WeightUnit;
-        st.l1 *= kKv8WeightUnit;
-#pragma unroll
-        for (int t = 0; t < D / 16; ++t) {
-            const uint32_t at = dst + (h * D + (((lane >> 2) * (D / 8) + 2 * t) ^ (h * 4))) * 4;
-            if (h < g) asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(st.o[t][0] * f), "f"(st.o[t][2] * f) : "memory");
-            if (h + 1 < g) asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(at + D * 4), "f"(st.o[t][1] * f), "f"(st.o[t][3] * f) : "memory");
-        }
-        __syncwarp();
+    if constexpr (O == kKv8) {
+        stage_result8<D>(dst, g, st, k8);
         return;
     }
     const uint32_t addr = dst + (h * D + (lane >> 2)) * 4;
@@ -1174,9 +1039,8 @@ __device__ bool run_unit(const CUtensorMap* kvp_map, const MixedParams& p, const
 
         PageExtra extra;
         if constexpr (O == kWindow) extra.from = span.from - page * kPageSize, extra.sinks = p.sinks - page * kPageSize;
-        if constexpr (O == kKv8) extra.scale = scales.of(k, issued);
         if constexpr (O == kScored) extra.scores = scores_of(p, u.pages - p.decode_pages + page, u.kvh);
-        attend_page<D, O>(p, sK, valid, qb, st, k8, extra);
+        if constexpr (O == kKv8) attend_page8<D>(p, sK, valid, qb, st, k8, scales.of(k, issued)); else attend_page<D, O>(p, sK, valid, qb, st, extra);
         ring.it += 1;
         __syncwarp();  // every lane is done reading this stage before it is refilled
         if (issued < npg) issue_next();
@@ -1412,8 +1276,7 @@ __device__ __forceinline__ void run_line(const CUtensorMap* kvp_map, const Mixed
                 break;
             }
             if (patched) patch_page<D>(p, smem, sK, i, kvh, valid, row);
-            if constexpr (O == kKv8) extra.scale = scales.of((int)ring.it, issued);
-            attend_page<D, O>(p, sK, valid, qb, st, k8, extra);
+            if constexpr (O == kKv8) attend_page8<D>(p, sK, valid, qb, st, k8, scales.of((int)ring.it, issued)); else attend_page<D, O>(p, sK, valid, qb, st, extra);
             ring.it += 1;
             __syncwarp();  // every lane is done reading this stage before it is refilled
             if (x + 1 < end && issued < total) issue_next();
