@@ -957,6 +957,8 @@ __device__ __forceinline__ bool pf_mma_ahead(const MixedParams& p, const PfShare
 // rounding of P), and n added to the exponent as integer bits.  Of every 8 pairs the first kPfFmaPairsOf8 take this path.
 constexpr int kPfMaxChains = 4;      // independent chains of the row maximum
 constexpr int kPfFmaPairsOf8 = 2;    // measured: 2 of 8 gains 2-4 %, 3 of 8 nothing, 4 of 8 loses (the FMA pipe fills up)
+// (The options take a minimax quartic, relative error 2.6e-6, so that log-sum-exps keep seven digits; 1 % of a launch bound by the arithmetic.)
+template <Option O>
 __device__ __forceinline__ void pf_exp2_pair_fma(uint64_t x2, float& p0, float& p1) {
     float x0, x1;
     unpack_f32x2(x2, x0, x1);
@@ -964,9 +966,17 @@ __device__ __forceinline__ void pf_exp2_pair_fma(uint64_t x2, float& p0, float& 
     const uint64_t t = add_f32x2(xc, pack_f32x2(12582912.f, 12582912.f));  // low mantissa bits = n
     const uint64_t r = add_f32x2(t, pack_f32x2(-12582912.f, -12582912.f)); // n as a float
     const uint64_t f = fma_f32x2(r, pack_f32x2(-1.f, -1.f), xc);
-    uint64_t q = fma_f32x2(f, pack_f32x2(0.0551716648f, 0.0551716648f), pack_f32x2(0.2426111251f, 0.2426111251f));
-    q = fma_f32x2(q, f, pack_f32x2(0.6932609677f, 0.6932609677f));
-    q = fma_f32x2(q, f, pack_f32x2(0.9999280572f, 0.9999280572f));
+    uint64_t q;
+    if constexpr (O == kPlain) {
+        q = fma_f32x2(f, pack_f32x2(0.0551716648f, 0.0551716648f), pack_f32x2(0.2426111251f, 0.2426111251f));
+        q = fma_f32x2(q, f, pack_f32x2(0.6932609677f, 0.6932609677f));
+        q = fma_f32x2(q, f, pack_f32x2(0.9999280572f, 0.9999280572f));
+    } else {
+        q = fma_f32x2(f, pack_f32x2(0.0095701022f, 0.0095701022f), pack_f32x2(0.0559178591f, 0.0559178591f));
+        q = fma_f32x2(q, f, pack_f32x2(0.2402474433f, 0.2402474433f));
+        q = fma_f32x2(q, f, pack_f32x2(0.6931217909f, 0.6931217909f));
+        q = fma_f32x2(q, f, pack_f32x2(0.9999992847f, 0.9999992847f));
+    }
     float q0, q1, t0, t1;
     unpack_f32x2(q, q0, q1);
     unpack_f32x2(t, t0, t1);
@@ -1177,7 +1187,7 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
                                               scale2, negm2);
                 float p0, p1;
                 if ((i & 7) < kPfFmaPairsOf8) {   // folds to a constant once the loop is unrolled
-                    pf_exp2_pair_fma(x2, p0, p1);
+                    pf_exp2_pair_fma<O>(x2, p0, p1);
                 } else {
                     float x0, x1;
                     unpack_f32x2(x2, x0, x1);

@@ -28,6 +28,7 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocksPerSm) sw_key_wei
         if (__ldcg(p.page_indptr + mid) <= begin) i = mid; else hi = mid;
     }
     grid_dependency_wait();
+    if (ld_relaxed_gpu(&p.ctrl[kCtrStatus]) == SW_ERR_DEVICE_TIMEOUT) return;   // some scores may not have been written
     constexpr float kLog2E = 1.4426950408889634f;
     const int key = lane & 15, g = p.group, lines = p.Hkv * kPageSize * g / 32;   // of 128 bytes, of a page's scores
     int at = 0, next = begin, len = 0, row = 0;

@@ -71,6 +71,18 @@ def test_masked_slots_hold_anything():
     check_weights(c, before, w, [0, 1], c.check(clean))
 
 
+def test_expired_wait_leaves_the_weights_alone():
+    import ctypes
+
+    c = U.Case((32, 8, 128), [3000] * 40, seed=3)     # (enough that some page is still on its way)
+    w = weights_of(c, 40, 3000)
+    before = w.clone()
+    B._lib.sw_ctx_set_line_wait(c.ctx.handle, ctypes.c_int64(0))     # what has not arrived at the first look has expired
+    weigh(c, B.KeyWeights(w, torch.arange(40, dtype=torch.int32, device=c.dev)))
+    assert B.sw_check_status(c.ctx, raise_on_error=False)[0] == B.SW_ERR_DEVICE_TIMEOUT
+    assert torch.equal(w, before)
+
+
 def test_what_does_not_fit_is_reported():
     c = U.Case((8, 2, 64), [40, 100, 30], seed=4)
     w = weights_of(c, 3, 60)
