@@ -295,8 +295,17 @@ def sw_attn_weights_scratch_bytes(layout: sw_layout, decode_pages: int) -> int:
     return int(_lib.sw_attn_weights_scratch_bytes(C.byref(layout), decode_pages))
 
 
+def _check_key_weights(ctx: Context, batch: DeviceBatch, weights: KeyWeights) -> None:
+    # what the library cannot see from the pointers
+    if weights.weights.shape[1] != ctx.shape.num_kv_heads:
+        raise ValueError(f"weights have {weights.weights.shape[1]} KV heads, the context {ctx.shape.num_kv_heads}")
+    if weights.row_of.numel() < batch.struct.num_decode:
+        raise ValueError(f"row_of names {weights.row_of.numel()} rows, the batch has {batch.struct.num_decode} requests")
+
+
 def sw_decode_attn_weights_run(ctx: Context, kv_pool, batch: DeviceBatch, q, out, lse, weights: KeyWeights, scratch, stream=None) -> None:
     """Decode attention that adds what weight every key got to ``weights``; ``scratch``: ``sw_attn_weights_scratch_bytes`` bytes."""
+    _check_key_weights(ctx, batch, weights)
     _check(_lib.sw_decode_attn_weights_run(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), _ptr(q), _ptr(out), _ptr(lse),
                                            C.byref(weights.struct), _ptr(scratch), _bytes_of(scratch), _stream_handle(stream)),
            "sw_decode_attn_weights_run")
@@ -307,6 +316,10 @@ def sw_kv_evict(ctx: Context, kv_pool, batch: DeviceBatch, weights: KeyWeights, 
     """Keep ``budget`` keys of every (request, KV head) pair; ``new_weights``: the same tensor with the rows they go to."""
     if new_weights.weights.data_ptr() != weights.weights.data_ptr():
         raise ValueError("new_weights must be rows of the same tensor")
+    _check_key_weights(ctx, batch, weights)
+    _check_key_weights(ctx, batch, new_weights)
+    if kept.numel() < batch.struct.num_decode * ctx.shape.num_kv_heads * budget or new_len.numel() < batch.struct.num_decode:
+        raise ValueError("kept and new_len must hold [num_decode][num_kv_heads][budget] and [num_decode]")
     _check(_lib.sw_kv_evict(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), C.byref(weights.struct), _ptr(new_page_indptr),
                             _ptr(new_pages), _ptr(new_weights.row_of), budget, sinks, recent, _ptr(kept), _ptr(new_len),
                             _stream_handle(stream)), "sw_kv_evict")

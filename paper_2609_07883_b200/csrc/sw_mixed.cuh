@@ -862,6 +862,7 @@ __device__ __forceinline__ void attend_page(const MixedParams& p, uint32_t sK, i
                     sts_v4(sK + (Geo<D>::kHalves + (chunk >> 3)) * Geo<D>::kBlockBytes + row_i * 128 + (((chunk & 7) ^ (row_i & 7)) << 4),
                            0u, 0u, 0u, 0u);
             }
+            fence_proxy_async_smem();   // the buffer is refilled by the copy engine, and this need not be the pair's last page
             __syncwarp();
         }
     }

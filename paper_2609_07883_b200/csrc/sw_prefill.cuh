@@ -992,8 +992,9 @@ struct PfSoftmaxState {
 // kKv8: the thread's row of Q, from bf16 to the sum of two e4m3 rows in the same place (whole tile; 128 threads).  The row is scaled by a power of two to below 2^8 first; what the
 // larger part (4 significant bits) leaves of a bf16 element (8 bits) fits the smaller one exactly, but for what is 2^-18 of the row's largest
 // element.  Returns the scale to multiply scores with (NaN where the row holds anything that is not finite).
+// (`landed`: false where the wait for Q expired in this warp; it still meets the tile's others at the barrier.)
 template <int D>
-__device__ __forceinline__ float pf_split_q(const PfShared& sh, int t, int row) {
+__device__ __forceinline__ float pf_split_q(const PfShared& sh, int t, int row, bool landed) {
     using G = PfGeo<D>;
     const uint32_t src = sh.smem + G::kQOffset + t * G::kTileBytes + row * 128;
     uint32_t x[D / 2], top = 0;
@@ -1008,6 +1009,7 @@ __device__ __forceinline__ float pf_split_q(const PfShared& sh, int t, int row) 
     const int e = min(max((int)(top >> 7) - 127, -99), 126);
     const float f = __int_as_float((7 - e + 127) << 23);
     named_barrier_sync(2 + t, 128);   // every row is in registers
+    if (!landed) return 0.f;
     const uint32_t dst = sh.smem + 2 * t * PfGeo8<D>::kRowTile;
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
@@ -1054,8 +1056,9 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
     auto convert = [&](int j) { return pf_convert<D>(p, sh, vs, v_factor, j, j == it.j0, st.kv_it + (j - it.j0), kv_total); };
     if constexpr (O == kKv8) {
         if (j_end > it.j0) {
-            if (!pf_wait(sh, kBarQFull, st.q_it & 1, p.ctrl, 14)) return false;
-            q_scale = pf_split_q<D>(sh, t, row);
+            const bool landed = __all_sync(0xffffffffu, pf_wait(sh, kBarQFull, st.q_it & 1, p.ctrl, 14));
+            q_scale = pf_split_q<D>(sh, t, row, landed);
+            if (!landed) return false;
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(sh.bars + (kBarQReady + t) * 8);

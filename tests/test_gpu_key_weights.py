@@ -284,7 +284,7 @@ def test_refusals():
     w = weights_of(c, 2, 64)
     kw, new = B.KeyWeights(w, torch.zeros(1, dtype=torch.int32, device=c.dev)), B.KeyWeights(w, torch.ones(1, dtype=torch.int32, device=c.dev))
     scratch = torch.empty(1 << 20, dtype=torch.uint8, device=c.dev)
-    ints = torch.zeros(64, dtype=torch.int32, device=c.dev)
+    ints = torch.zeros(256, dtype=torch.int32, device=c.dev)
     with pytest.raises(B.SwError) as e:      # a chunk
         B.sw_decode_attn_weights_run(c.ctx, c.pool, c.db, c.q, c.out, c.lse, kw, scratch)
     assert e.value.status == B.SW_ERR_UNSUPPORTED
@@ -306,5 +306,10 @@ def test_refusals():
     for bad in (w.double(), w[:, :, ::2], w[0]):
         with pytest.raises(ValueError):
             B.KeyWeights(bad, torch.zeros(1, dtype=torch.int32, device=c.dev))
+    one_head, no_rows = weights_of(c, 2, 64)[:, :1].contiguous(), torch.zeros(0, dtype=torch.int32, device=c.dev)
+    for old, fresh, kept in [(kw, B.KeyWeights(w.clone(), new.row_of), ints), (B.KeyWeights(w, no_rows), new, ints), (kw, B.KeyWeights(w, no_rows), ints),
+                             (B.KeyWeights(one_head, kw.row_of), B.KeyWeights(one_head, new.row_of), ints), (kw, new, ints[:31])]:
+        with pytest.raises(ValueError):
+            B.sw_kv_evict(d.ctx, d.pool, d.db, old, ints, ints, fresh, 16, 0, 0, kept, ints)
     with pytest.raises(ValueError):
-        B.sw_kv_evict(d.ctx, d.pool, d.db, kw, ints, ints, B.KeyWeights(w.clone(), new.row_of), 16, 0, 0, ints, ints)
+        B.sw_decode_attn_weights_run(d.ctx, d.pool, d.db, d.q, d.out, d.lse, B.KeyWeights(one_head, kw.row_of), scratch)
