@@ -161,32 +161,33 @@ struct PfItem {
     int kvh;
     int chunk;       // which chunk of the iteration the item belongs to (its descriptors are in the shared table)
     int tok0[2];     // first chunk token of each tile
-    int nkv[2];      // KV tiles each tile attends in total (0 = tile has no rows; kWindow: less the tiles that are passed over)
+    int nkv[2];      // KV tiles each tile attends in total (0 = tile has no rows; kWindow: of the item's pages)
     int nk;          // steps of the item = max(nkv)
     int j0, j1;      // this entry's piece of the item: KV tiles [j0, j1)
     int piece;       // index of the piece (0 when the item is whole)
     int slot0;       // scratch slot of the item's piece 0 (tail items only)
-    int head, skip;  // kWindow: step j is KV tile j below `head` (tiles with sinks) and j + skip from there on
+    int head, skip;  // kWindow: page j of the item is page j of the prompt below `head` (pages with sinks), j + skip from there on
     int pieces;      // pieces the item is cut into (several chunks: each chunk has its own count)
 };
 
-__device__ __forceinline__ int pf_tiles_of(int group, int P, int C, int tok0) {
+__device__ __forceinline__ int pf_tiles_of(int group, int P, int C, int tok0, int skip = 0) {
     const int tt = 128 / group;  // tokens per tile
     if (tok0 >= C) return 0;
-    return (P + min(tok0 + tt, C) - 1) / 128 + 1;
+    return (P + min(tok0 + tt, C) - 1 - skip * kPageSize) / 128 + 1;
 }
 __device__ __forceinline__ int pf_num_groups(int group, int C) {
     const int tok_per_item = 256 / group;
     return (C + tok_per_item - 1) / tok_per_item;
 }
-// kWindow: an item passes over the KV tiles between the sinks and the window of its first row.  (A later row's window begins later: for
-// its tile the first steps may be masked as a whole.)
+// kWindow: an item passes over the pages between the sinks and the window of its first row; its KV tiles are made of the others, side by side.
+// (Passing over whole tiles, 4096 tokens at prefix 28672 in a window of 4096 took two steps more of 33.)  Every page that is read holds a key that
+// some row of the item attends: what left every window may have been given to another prompt.
 template <Option O>
 __device__ __forceinline__ void pf_passed(const MixedParams& p, int P, int tok0, int& head, int& skip) {
     head = skip = 0;
     if constexpr (O == kWindow) {
-        const int first = max(0, P + tok0 + 1 - p.window) / 128;
-        head = min(first, (p.sinks + 127) / 128);
+        const int first = max(0, P + tok0 + 1 - p.window) / kPageSize;
+        head = min(first, p.sink_pages);
         skip = first - head;
     }
 }
@@ -197,7 +198,7 @@ __device__ __forceinline__ int pf_steps_of_rank(const MixedParams& p, int P, int
     const int tp = n_tp - 1 - r;
     int head, skip;
     pf_passed<O>(p, P, tp * 2 * tt, head, skip);
-    return max(pf_tiles_of(p.group, P, C, (tp * 2) * tt), pf_tiles_of(p.group, P, C, (tp * 2 + 1) * tt)) - skip;
+    return max(pf_tiles_of(p.group, P, C, (tp * 2) * tt, skip), pf_tiles_of(p.group, P, C, (tp * 2 + 1) * tt, skip));
 }
 // first KV tile of piece i when nk steps are cut into k pieces
 __device__ __forceinline__ int pf_piece_begin(int nk, int k, int i) { return (int)(((long long)nk * i) / k); }
@@ -530,7 +531,7 @@ __device__ __forceinline__ PfItem pf_entry(const MixedParams& p, const PfPlan& p
     pf_passed<O>(p, cP, tp * 2 * tt, it.head, it.skip);
     for (int t = 0; t < 2; ++t) {
         it.tok0[t] = (tp * 2 + t) * tt;
-        it.nkv[t] = max(0, pf_tiles_of(p.group, cP, cC, it.tok0[t]) - it.skip);
+        it.nkv[t] = pf_tiles_of(p.group, cP, cC, it.tok0[t], it.skip);
     }
     it.nk = max(it.nkv[0], it.nkv[1]);
     if (entry < plan.n_whole) {
@@ -541,15 +542,6 @@ __device__ __forceinline__ PfItem pf_entry(const MixedParams& p, const PfPlan& p
         it.j1 = pf_piece_begin(it.nk, it.pieces, it.piece + 1);
     }
     return it;
-}
-
-template <Option O>
-__device__ __forceinline__ int pf_tile(const PfItem& it, int j) { return O == kWindow && j >= it.head ? j + it.skip : j; }
-// kWindow: whether some row of the item attends a key of the page (if the prompt reaches that far).  The others are not read: what left
-// every window may have been given to another prompt.
-template <Option O>
-__device__ __forceinline__ bool pf_page_seen(const MixedParams& p, const PfItem& it, int P, int page) {
-    return O != kWindow || page < p.sink_pages || page * kPageSize + kPageSize > P + it.tok0[0] + 1 - p.window;
 }
 
 // ---- role: TMA producer (one warp) ----------------------------------------------------------------------------
@@ -571,7 +563,7 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
                                 h * 64, it.kvh * p.group, pf_chunk<D, kMulti>(p, sh, 2, it.chunk) + it.tok0[t]);
     }
     // fused launch: tiles that reach into the chunk's own keys wait until every CTA has written its share of them
-    if (p.append_first && (pf_tile<O>(it, it.j1 - 1) + 1) * 128 > pf_chunk<D, kMulti>(p, sh, 0, it.chunk) && !wait_append(p, sh.smem + Geo<D>::kSetOffset)) {
+    if (p.append_first && it.j1 * 128 + it.skip * kPageSize > pf_chunk<D, kMulti>(p, sh, 0, it.chunk) && !wait_append(p, sh.smem + Geo<D>::kSetOffset)) {
         if (lane == 0) {
             *sh.abort_flag = 1;
             report(p.ctrl, SW_ERR_DEVICE_TIMEOUT, kSiteWait, it.item);
@@ -579,10 +571,10 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
         return false;
     }
     const int npages = (pf_chunk<D, kMulti>(p, sh, 0, it.chunk) + pf_chunk<D, kMulti>(p, sh, 1, it.chunk) + kPageSize - 1) / kPageSize;
-    auto seen = [&](int page) { return page < npages && pf_page_seen<O>(p, it, pf_chunk<D, kMulti>(p, sh, 0, it.chunk), page); };
     auto id_of = [&](int step) {
-        const int page = pf_tile<O>(it, step) * 8 + lane;
-        int id = (lane < 8 && seen(page)) ? p.prefill_pages[pf_chunk<D, kMulti>(p, sh, 3, it.chunk) + page] : 0;
+        int page = step * 8 + lane;
+        if (O == kWindow && page >= it.head) page += it.skip;
+        int id = (lane < 8 && page < npages) ? p.prefill_pages[pf_chunk<D, kMulti>(p, sh, 3, it.chunk) + page] : 0;
         if (id < 0 || (int64_t)id >= p.chunk_pool_pages) {
             // reported, and page 0 fetched in its place: a bad id never reaches the copy engine
             report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteAttnPage, it.item);
@@ -629,24 +621,18 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
             const uint32_t s = kv_it & 1, n = kv_it >> 1;
             const int id = id_next;
             if (j + 1 < it.j1) id_next = id_of(j + 1);  // in flight while this tile is issued
-            const int tile = pf_tile<O>(it, j);
-            int nvp = min(8, npages - tile * 8);
-            bool mine = lane < nvp;
-            if constexpr (O == kWindow) {
-                mine = mine && seen(tile * 8 + lane);
-                nvp = __popc(__ballot_sync(0xffffffffu, mine));
-            }
+            const int nvp = min(8, npages - it.skip - j * 8);
             const uint32_t kdst = sh.smem + G::kKVOffset + s * 2 * G::kTileBytes;
             const uint32_t vdst = kdst + G::kTileBytes;
             if (!pf_wait(sh, kBarKEmpty + s, (n & 1) ^ 1, p.ctrl, 1)) return false;
             if (lane == 0) mbar_arrive_expect_tx(sh.bars + (kBarKFull + s) * 8, nvp * G::kPageStride);
             __syncwarp();
-            if (mine)
+            if (lane < nvp)
                 tma_load_5d(kdst + lane * G::kPageStride, kv_map, sh.bars + (kBarKFull + s) * 8, 0, 0, 0, 0, (2 * id) * p.Hkv + it.kvh);
             if (!pf_wait(sh, kBarVEmpty + s, (n & 1) ^ 1, p.ctrl, 2)) return false;
             if (lane == 0) mbar_arrive_expect_tx(sh.bars + (kBarVLanded + s) * 8, nvp * G::kPageStride);
             __syncwarp();
-            if (mine)
+            if (lane < nvp)
                 tma_load_5d(vdst + lane * G::kPageStride, kv_map, sh.bars + (kBarVLanded + s) * 8, 0, 0, 0, 0,
                             (2 * id + 1) * p.Hkv + it.kvh);
         }
@@ -665,17 +651,7 @@ __device__ __forceinline__ bool pf_sanitize(const MixedParams& p, const PfShared
     for (int j = it.j0; j < it.j1; ++j, ++kv_it) {
         const uint32_t s = kv_it & 1, n = kv_it >> 1;
         if (!pf_wait(sh, kBarVLanded + s, n & 1, p.ctrl, 3)) return false;
-        const int first_dead = max(0, kv_total - pf_tile<O>(it, j) * 128);
-        if constexpr (O == kWindow) {   // pages that the producer has passed over
-            const int P = pf_chunk<D, kMulti>(p, sh, 0, it.chunk), page = pf_tile<O>(it, j) * 8;
-            unsigned dead = __ballot_sync(0xffffffffu, lane < 8 && !pf_page_seen<O>(p, it, P, page + lane));
-            if (dead) {
-                const uint32_t vdst = sh.smem + G::kKVOffset + s * 2 * G::kTileBytes + G::kTileBytes;
-                for (; dead; dead &= dead - 1)
-                    for (int c = lane; c < G::kPageStride / 16; c += 32) sts_v4(vdst + (__ffs(dead) - 1) * G::kPageStride + c * 16, 0u, 0u, 0u, 0u);
-                fence_proxy_async_smem();
-            }
-        }
+        const int first_dead = max(0, kv_total - it.skip * kPageSize - j * 128);
         if (first_dead < 128) {
             const uint32_t vdst = sh.smem + G::kKVOffset + s * 2 * G::kTileBytes + G::kTileBytes;
             const int chunks = (128 - first_dead) * 8;  // 16-byte pieces per 64-element block
@@ -1085,8 +1061,8 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
         tc_fence_after_sync();
         // the whole row of S (128 fp32) in registers: one TMEM read per element
         uint32_t s[128];
-        const int limit = pos - pf_tile<O>(it, j) * 128 + 1;  // columns [0, limit) are attended
-        const int from = limit - p.window, sinks = p.sinks - pf_tile<O>(it, j) * 128;   // kWindow: of those, from `from` on and below `sinks`
+        const int limit = pos - it.skip * kPageSize - j * 128 + 1;  // columns [0, limit) are attended
+        const int from = limit - p.window, sinks = p.sinks - j * 128;   // kWindow: of those, from `from` on and below `sinks`
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
         tc_wait_ld();
