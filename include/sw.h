@@ -172,7 +172,8 @@ sw_status sw_mixed_iteration_window_run(sw_ctx* ctx, void* kv_pool, const sw_bat
  * (append such rows by calls of their own).  Slots behind the new rows are left as they are.
  *
  * sw_kv8_attn_run is sw_mixed_attn_run over such a pool.  The scales must be powers of two (between 2^-100 and 2^120) or NaN.  Its products see the
- * values that the pool stands for exactly; queries are rounded at 2^-18 of their row's largest element, weights at 2^-40 of the largest.
+ * values that the pool stands for exactly; queries are rounded at 2^-18 of their row's largest element, softmax weights at 2^-32 of
+ * their row's largest, and V at 2^-33 of the largest magnitude that the scales of the 128 keys around it allow.
  * scratch (optional; 256-byte aligned device memory of sw_kv8_scratch_bytes(layout, sum over the chunks of ceil((P + C) / 16)) bytes, of no use
  * between calls): where it is large enough and that is faster, long chunks read a copy of their prompts in 16 bits, made there first.
  * Both calls are asynchronous. */

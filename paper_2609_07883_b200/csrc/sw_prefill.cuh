@@ -677,7 +677,9 @@ __device__ __forceinline__ bool pf_sanitize(const MixedParams& p, const PfShared
 // O is kept in units of a scale `ref` that follows the largest scale of the tile's eight pages: upward beyond 2^3 times ref (P 2^7 may
 // reach 2^15, V 448 2^3), downward below 2^-12 of it, for which the softmax warps multiply O; a page's ratio to ref goes into its rows of V, exactly
 // down to 2^-15.  Everybody works ref out from the scales.  `top`: its largest value; a tile 2^-80 below it is not followed.
-constexpr float kPfWeightBits = 7.f;   // P is 2^7 times the weight
+// P is 2^7 times the weight (which may reach 2^8 before O is rescaled), in f16: finer than bf16 down to 2^-21 of the row's largest weight, and
+// never off by more than 2^-32 of it.
+constexpr float kPfWeightBits = 7.f;
 struct PfValueScale {
     float ref = 0.f, top = 0.f, inverse = 0.f;   // inverse: 1 / ref
     // Takes the step's eight scales; returns what O has to be multiplied with (1: ref stays).

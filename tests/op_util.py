@@ -6,6 +6,8 @@ Tolerances are sums of the roundings that a result goes through, taken at their 
   softmax weights as bf16        2^-8 sum p |v|              (the products take them in 16 bits; their sum l is kept in 32)
   2^x on the FMA pipe            7.5e-5 of a weight, numerator and denominator: 1.5e-4 sum p |v|
   a score's products and sum     D additions of fp32: D 2^-24 sum |q k| scale, an exponent's error, so relative in p; twice (p and l)
+  weights as f16 (8-bit pools)   times 2^7 (chunks) or 2^15 (decodes) in a format whose smallest step is 2^-24: half of that, 2^-32 of the row's
+                                 largest weight at most, for each key: 2^-32 sum |v| (`floor`)
   sums of p and of p v           N additions of fp32, pairwise or in tiles of 16 or 128: N 2^-24 at most with N <= 8192 here: 5e-4
 """
 from __future__ import annotations
@@ -84,7 +86,7 @@ def entries_of(batch):
     return out
 
 
-def attention(batch, pool, q, window=None, sinks=0, scale=None):
+def attention(batch, pool, q, window=None, sinks=0, scale=None, floor=0.0):
     """Outputs, log-sum-exps and their tolerances in float64; ``pool`` float64 [pages][2][heads][16][D].  Keys nobody attends may be NaN."""
     sh = batch.shape
     g, D = sh.group, sh.head_dim
@@ -115,7 +117,8 @@ def attention(batch, pool, q, window=None, sinks=0, scale=None):
             s_err = (D + 8) * 2.0 ** -24 * torch.where(seen[:, None], x.abs() @ k.abs().T * scale, 0.0).amax(-1)
             out[row:row + count, h], lse[row:row + count, h] = o, total
             rel = 2.0 ** -8 + 1.5e-4 + 5e-4 + 2 * s_err
-            tol[row:row + count, h] = 2.0 ** -8 * o.abs() + rel[..., None] * mass + 1e-30
+            least = floor * seen.double() @ v.abs()
+            tol[row:row + count, h] = 2.0 ** -8 * o.abs() + rel[..., None] * mass + least[:, None] + 1e-30
             lse_tol[row:row + count, h] = s_err + 7.5e-5 + 5e-4 + 2.0 ** -22 * total.abs()
             if e >= len(batch.chunks()):
                 weights[e - len(batch.chunks()), h] = (p[0].sum(0), seen[0], (2 * s_err[0].max() + 1e-5).item())
@@ -161,10 +164,10 @@ class Case:
     def ok(self):
         assert B.sw_check_status(self.ctx, raise_on_error=False) == (0, 0)
 
-    def check(self, pool64, window=None, sinks=0, rows=None):
+    def check(self, pool64, window=None, sinks=0, rows=None, floor=0.0):
         """out and lse against the plain form over ``pool64``."""
         torch.cuda.synchronize()
-        out, lse, tol, lse_tol, weights = attention(self.batch, pool64, self.q, window, sinks)
+        out, lse, tol, lse_tol, weights = attention(self.batch, pool64, self.q, window, sinks, floor=floor)
         live = torch.ones(out.shape[0], dtype=torch.bool, device=self.dev)
         for row, count, _, _ in entries_of(self.batch):
             if count == 0:

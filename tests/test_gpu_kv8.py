@@ -29,6 +29,10 @@ def attend(c, codes, scales, scratch=True):
     B.sw_kv8_attn_run(c.ctx, codes, scales, c.db, c.q, c.out, c.lse, room)
 
 
+def check8(c, want, **kw):
+    c.check(want, floor=2.0 ** -32, **kw)
+
+
 def check_append(c, codes, scales):
     want, want_scales = codes.view(torch.uint8).cpu().clone(), scales.cpu().clone()
     U.append8(want, want_scales, U.entries_of(c.batch), c.k_new.cpu(), c.v_new.cpu())
@@ -119,7 +123,7 @@ def test_decode(heads, lens):
             raw[int(c.batch.decode_pages[c.batch.decode_page_indptr[i + 1] - 1]), :, :, n % U.PAGE:] = 0x7F
     attend(c, codes, scales)
     c.ok()
-    c.check(want)
+    check8(c, want)
 
 
 @pytest.mark.parametrize("heads,n", [((8, 2, 64), 500), ((8, 1, 128), 40), ((8, 1, 64), 450)])   # units
@@ -129,7 +133,7 @@ def test_decode_units(heads, n):
     codes, scales = pool8(c)
     attend(c, codes, scales)
     c.ok()
-    c.check(U.dequantise(codes, scales))
+    check8(c, U.dequantise(codes, scales))
 
 
 @pytest.mark.parametrize("heads", [(8, 2, 64), (32, 8, 128), (8, 1, 128), (4, 4, 64)])
@@ -145,7 +149,7 @@ def test_chunks(heads, chunks, lens, scratch):
             raw[int(pages[-1]), :, :, (P + C) % U.PAGE:] = 0x7F
     attend(c, codes, scales, scratch)
     c.ok()
-    c.check(want)
+    check8(c, want)
 
 
 @pytest.mark.parametrize("far", [2.0 ** -13, 2.0 ** -30, 2.0 ** -90, 2.0 ** 5, 2.0 ** 40])
@@ -160,7 +164,7 @@ def test_scales_that_change_inside_a_context(far, chunks, lens, scratch):
             scales[int(page), 1] = 2.0 ** (j % 4 - 8) * (far if j // 8 % 2 else 1.0)
     attend(c, codes, scales, scratch)
     c.ok()
-    c.check(U.dequantise(codes, scales))
+    check8(c, U.dequantise(codes, scales))
 
 
 @pytest.mark.parametrize("exponent", [-100, -60, -20, 6, 7, 8, 20, 60])
@@ -176,7 +180,7 @@ def test_scales_far_from_one(exponent):
         scales[:, 0] *= 0.25
     attend(c, codes, scales)
     c.ok()
-    c.check(U.dequantise(codes, scales))
+    check8(c, U.dequantise(codes, scales))
 
 
 def test_nan_scale_reaches_the_rows_that_read_it():
@@ -188,7 +192,7 @@ def test_nan_scale_reaches_the_rows_that_read_it():
     c.ok()
     torch.cuda.synchronize()
     assert bool(torch.isnan(c.out[0, :4]).all()) and not bool(torch.isnan(c.out[0, 4:]).any())
-    c.check(want, rows=[1])
+    check8(c, want, rows=[1])
 
 
 def test_append_then_attend_many_iterations():
@@ -212,7 +216,7 @@ def test_append_then_attend_many_iterations():
         c.ok()
         U.append8(host, host_scales, U.entries_of(c.batch), c.k_new.cpu(), c.v_new.cpu())
         assert torch.equal(codes.view(torch.uint8).cpu(), host) and torch.equal(scales.cpu(), host_scales)
-        c.check(U.dequantise(codes, scales))
+        check8(c, U.dequantise(codes, scales))
 
 
 def test_captured_and_replayed_on_another_stream():
@@ -231,7 +235,7 @@ def test_captured_and_replayed_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         c.ok()
-        c.check(U.dequantise(codes, scales))
+        check8(c, U.dequantise(codes, scales))
 
 
 def test_bad_pages_are_reported_and_nothing_else_is_written():
