@@ -21,15 +21,11 @@ namespace cg = cooperative_groups;
 
 constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
 constexpr int kBins = 256, kHeldKeys = 16384, kMaxRanks = 8, kLoadsAhead = 8;
-// Eight lanes in a row count in words of their own: weights have few different exponents, and lanes that add to one word wait for each other
-// (16 contexts of 8192-32768 tokens, 4 CTAs a pair: 53 us with one word a digit).
-constexpr int kCopies = 8;
 constexpr int kMoveThreads = 256;
 
 struct SelectShared {
-    alignas(16) uint32_t counts[kBins * kCopies];   // keys of each digit, by lanes modulo kCopies
-    uint32_t hist[2][kBins];              // the copies' sums, by the parity of the digit
-    uint32_t all[kBins], before[kBins];   // summed over the cluster; over the CTAs before this one
+    uint32_t hist[2][kBins];          // keys of each digit, by the parity of the pass (eight words a digit, by lane: no faster)
+    alignas(16) uint32_t all[kBins], before[kBins];   // summed over the cluster; over the CTAs before this one
     uint32_t scan[2][kSelectWarps];   // by the parity of the use
     alignas(16) uint32_t found[4];                // the digit, keys above it in the cluster and in the CTAs before, keys of it in those
     alignas(16) float held[];
@@ -111,7 +107,8 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int pair = blockIdx.x / ranks, i = pair / p.Hkv, h = pair % p.Hkv;
     const int lane = threadIdx.x & 31;
-    for (int b = threadIdx.x; b < kBins * kCopies; b += kSelectThreads) s.counts[b] = 0;
+    s.hist[0][threadIdx.x] = 0;   // (both)
+    static_assert(kSelectThreads == 2 * kBins, "a thread per word");
     grid_launch_dependents();
     grid_dependency_wait();
 
@@ -167,7 +164,6 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
     for (int pass = 0; wanted > 0 && pass < 4; ++pass) {
         const int shift = 24 - 8 * pass;
         uint32_t* hist = s.hist[pass & 1];
-        uint32_t* counts = s.counts + (lane & (kCopies - 1));
         if (pass == 0) {
             for (int k0 = threadIdx.x; k0 < mine; k0 += kLoadsAhead * kSelectThreads) {
                 float x[kLoadsAhead];
@@ -178,7 +174,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
                     const int k = k0 + u * kSelectThreads;
                     if (k < mine) {
                         if (k < held) s.held[k] = x[u];
-                        atomicAdd(&counts[(ordered(x[u]) >> 24) * kCopies], 1u);
+                        atomicAdd(&hist[ordered(x[u]) >> 24], 1u);
                     }
                 }
             }
@@ -190,18 +186,11 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     const uint32_t key = ordered(x[u]);
-                    if (k + u < mine && (key ^ prefix) >> (shift + 8) == 0) atomicAdd(&counts[(key >> shift & (kBins - 1)) * kCopies], 1u);
+                    if (k + u < mine && (key ^ prefix) >> (shift + 8) == 0) atomicAdd(&hist[key >> shift & (kBins - 1)], 1u);
                 }
             }
         }
-        __syncthreads();
-        if (threadIdx.x < kBins) {
-            uint4* own = reinterpret_cast<uint4*>(s.counts + threadIdx.x * kCopies);
-            const uint4 a = own[0], b = own[1];
-            hist[threadIdx.x] = ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
-            own[0] = own[1] = make_uint4(0u, 0u, 0u, 0u);
-        }
-        cluster.sync();   // (also: nobody reads the digit's before the last any more)
+        cluster.sync();   // (also: nobody reads the histogram of the pass before any more)
         if (threadIdx.x < kBins) {
             uint32_t n[kMaxRanks], all = 0, before = 0;   // all in flight at once
 #pragma unroll
@@ -213,6 +202,8 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
             }
             s.all[threadIdx.x] = all;
             s.before[threadIdx.x] = before;
+        } else {
+            s.hist[~pass & 1][threadIdx.x - kBins] = 0;
         }
         __syncthreads();
         if (threadIdx.x < 32) {   // eight neighbouring bins a lane, from the highest down
