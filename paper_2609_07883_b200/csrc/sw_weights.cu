@@ -18,7 +18,8 @@ constexpr int kWeightThreads = 256, kWeightBlocksPerSm = 4;
 // cost the launches 7 us of 147.
 __global__ void __launch_bounds__(kWeightThreads, kWeightBlocksPerSm) sw_key_weights_kernel(const WeightParams p) {
     grid_launch_dependents();
-    // The batch was there before the attention launch started: where the warp's stretch lies is found while that ends.
+    // The batch was there before the attention launch started: where the warp's stretch lies is found while that ends (64 contexts of 256-2048
+    // tokens 68.4 -> 60.9 us; with the request's other words as well 63.4).
     const int lane = threadIdx.x & 31, warps = gridDim.x * (kWeightThreads / 32), w = blockIdx.x * (kWeightThreads / 32) + threadIdx.x / 32;
     const int64_t total = __ldcg(p.page_indptr + p.n);
     const int begin = (int)(total * w / warps), end = (int)(total * (w + 1) / warps);
@@ -28,7 +29,7 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocksPerSm) sw_key_wei
         if (__ldcg(p.page_indptr + mid) <= begin) i = mid; else hi = mid;
     }
     grid_dependency_wait();
-    if (ld_relaxed_gpu(&p.ctrl[kCtrStatus]) == SW_ERR_DEVICE_TIMEOUT) return;   // some scores may not have been written
+    const int status = ld_relaxed_gpu(&p.ctrl[kCtrStatus]);   // (looked at with the first request's words)
     constexpr float kLog2E = 1.4426950408889634f;
     const int key = lane & 15, g = p.group, lines = p.Hkv * kPageSize * g / 32;   // of 128 bytes, of a page's scores
     int at = 0, next = begin, len = 0, row = 0;
@@ -42,6 +43,7 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocksPerSm) sw_key_wei
             row = p.row_of[i];
             const int pages = len > 0 ? (len - 1) / kPageSize + 1 : 0;
             ok = pages <= next - at;   // (reported by the attention launch)
+            ok = ok && status != SW_ERR_DEVICE_TIMEOUT;   // some scores may not have been written
             if (ok && len > 0 && (row < 0 || (int64_t)row >= p.rows || len > p.capacity)) {
                 if (lane == 0) report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteWeights, i);
                 ok = false;
