@@ -19,16 +19,16 @@
 namespace sw {
 namespace cg = cooperative_groups;
 
-constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kManyThreads = 512, kFewThreads = 256;   // of a selecting CTA
 constexpr int kBins = 256, kHeldKeys = 16384, kMaxRanks = 8, kLoadsAhead = 8;
 constexpr int kMoveThreads = 256;
 
 struct SelectShared {
     uint32_t hist[2][kBins];          // keys of each digit, by the parity of the pass (eight words a digit, by lane: no faster)
     alignas(16) uint32_t all[kBins], before[kBins];   // summed over the cluster; over the CTAs before this one
-    uint32_t scan[2][kSelectWarps];   // by the parity of the use
+    uint32_t above[kManyThreads / 32], equal[kManyThreads / 32];
     alignas(16) uint32_t found[4];                // the digit, keys above it in the cluster and in the CTAs before, keys of it in those
-    alignas(16) float held[];
+    alignas(16) uint32_t held[];                  // ordered()
 };
 
 // Floats as integers of the same order; NaN as the lowest.
@@ -36,30 +36,6 @@ __device__ __forceinline__ uint32_t ordered(float w) {
     if (w != w) return 0u;
     const uint32_t u = __float_as_uint(w + 0.f);   // -0 as 0
     return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-
-// Block-wide exclusive prefix sum of one value per thread; `total` is the block's.  `use` counts the calls: two in a row have different words, and
-// every call has a barrier, so the words of the call before last are free.
-__device__ __forceinline__ uint32_t block_prefix(uint32_t v, SelectShared& s, int& use, uint32_t* total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    uint32_t inc = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t t = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += t;
-    }
-    uint32_t* words = s.scan[use++ & 1];
-    if (lane == 31) words[warp] = inc;
-    __syncthreads();
-    uint32_t sum = lane < kSelectWarps ? words[lane] : 0u;
-#pragma unroll
-    for (int o = 1; o < kSelectWarps; o <<= 1) {
-        const uint32_t t = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= o) sum += t;
-    }
-    *total = __shfl_sync(0xffffffffu, sum, kSelectWarps - 1);
-    const uint32_t before = warp == 0 ? 0u : __shfl_sync(0xffffffffu, sum, warp - 1);
-    return before + inc - v;
 }
 
 // The rows of one new page of a pair that keeps `kept` keys (list: p.kept).  Lane groups of D / 8 lanes copy a row each, 16 bytes a lane; all loads of
@@ -99,16 +75,17 @@ __device__ __forceinline__ void move_page(const EvictParams& p, int i, int h, in
 }
 
 // D: head size where the cluster copies its pair's rows as well, 0 where a launch of its own does.
-template <int D>
-__global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(const EvictParams p) {
+template <int D, int kSelectThreads>
+__global__ void __launch_bounds__(kSelectThreads, 1024 / kSelectThreads) sw_evict_select_kernel(const EvictParams p) {
+    constexpr int kSelectWarps = kSelectThreads / 32;
     extern __shared__ __align__(16) unsigned char select_raw[];
     SelectShared& s = *reinterpret_cast<SelectShared*>(select_raw);
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int pair = blockIdx.x / ranks, i = pair / p.Hkv, h = pair % p.Hkv;
-    const int lane = threadIdx.x & 31;
-    s.hist[0][threadIdx.x] = 0;   // (both)
-    static_assert(kSelectThreads == 2 * kBins, "a thread per word");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    static_assert(kSelectThreads >= kBins, "a thread per bin");
+    if (threadIdx.x < kBins) s.hist[0][threadIdx.x] = s.hist[1][threadIdx.x] = 0;
     grid_launch_dependents();
     grid_dependency_wait();
 
@@ -123,10 +100,14 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
         if (!fits) report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteEvict, i);
     }
     if (!fits || kept == 0) return;
+    auto all_here = [&] {
+        if (ranks > 1) cluster.sync();
+        else __syncthreads();
+    };
     auto move = [&](int count, bool listed_already = false) {   // (in step with the cluster's other CTAs, which write parts of the list)
         if constexpr (D > 0) {
-            if (!listed_already) cluster.sync();
-            for (int pg = rank * kSelectWarps + (int)threadIdx.x / 32; pg * kPageSize < count; pg += ranks * kSelectWarps) move_page<D>(p, i, h, pg, count);
+            if (!listed_already) all_here();
+            for (int pg = rank * kSelectWarps + warp; pg * kPageSize < count; pg += ranks * kSelectWarps) move_page<D>(p, i, h, pg, count);
         }
     };
     const float* w = p.weights + ((int64_t)row * p.Hkv + h) * p.capacity;
@@ -147,13 +128,13 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
     const float* x0 = w + p.sinks + begin;
     const int held = min(mine, p.held);
     // four neighbours from k on (a multiple of four), zeros past the end
-    auto weights_of = [&](int k, float (&x)[4]) {
+    auto keys_of = [&](int k, uint32_t (&x)[4]) {
         if (k + 4 <= held) {
-            const float4 v = *reinterpret_cast<const float4*>(s.held + k);
+            const uint4 v = *reinterpret_cast<const uint4*>(s.held + k);
             x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
         } else {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) x[u] = k + u >= mine ? 0.f : (k + u < held ? s.held[k + u] : __ldg(x0 + k + u));
+            for (int u = 0; u < 4; ++u) x[u] = k + u >= mine ? 0u : (k + u < held ? s.held[k + u] : ordered(__ldg(x0 + k + u)));
         }
     };
 
@@ -173,24 +154,23 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
                 for (int u = 0; u < kLoadsAhead; ++u) {
                     const int k = k0 + u * kSelectThreads;
                     if (k < mine) {
-                        if (k < held) s.held[k] = x[u];
-                        atomicAdd(&hist[ordered(x[u]) >> 24], 1u);
+                        const uint32_t key = ordered(x[u]);
+                        if (k < held) s.held[k] = key;
+                        atomicAdd(&hist[key >> 24], 1u);
                     }
                 }
             }
         } else {
 #pragma unroll 2
             for (int k = 4 * threadIdx.x; k < mine; k += 4 * kSelectThreads) {
-                float x[4];
-                weights_of(k, x);
+                uint32_t x[4];
+                keys_of(k, x);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const uint32_t key = ordered(x[u]);
-                    if (k + u < mine && (key ^ prefix) >> (shift + 8) == 0) atomicAdd(&hist[key >> shift & (kBins - 1)], 1u);
-                }
+                for (int u = 0; u < 4; ++u)
+                    if (k + u < mine && x[u] - prefix < 256u << shift) atomicAdd(&hist[x[u] >> shift & (kBins - 1)], 1u);
             }
         }
-        cluster.sync();   // (also: nobody reads the histogram of the pass before any more)
+        all_here();   // (also: nobody reads the histogram of the pass before any more)
         if (threadIdx.x < kBins) {
             uint32_t n[kMaxRanks], all = 0, before = 0;   // all in flight at once
 #pragma unroll
@@ -202,8 +182,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
             }
             s.all[threadIdx.x] = all;
             s.before[threadIdx.x] = before;
-        } else {
-            s.hist[~pass & 1][threadIdx.x - kBins] = 0;
+            s.hist[~pass & 1][threadIdx.x] = 0;
         }
         __syncthreads();
         if (threadIdx.x < 32) {   // eight neighbouring bins a lane, from the highest down
@@ -225,17 +204,23 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
 #pragma unroll
             for (int b = 0; b < 8; ++b) {
                 if (n_sum < rest && n_sum + n[b] >= rest)   // exactly one bin of one lane
-                    *reinterpret_cast<uint4*>(s.found) = make_uint4((uint32_t)(top + 7 - b), n_sum, m_sum, m[b]);
+                    *reinterpret_cast<uint4*>(s.found) = make_uint4((uint32_t)(top + 7 - b) | (n_sum + n[b] == rest ? kBins : 0u), n_sum, m_sum, m[b]);
                 n_sum += n[b];
                 m_sum += m[b];
             }
         }
         __syncthreads();   // (also: the sums are read before they are written again)
         const uint4 found = *reinterpret_cast<const uint4*>(s.found);
-        prefix |= found.x << shift;
+        prefix |= (found.x & (kBins - 1)) << shift;
         rest -= found.y;
         above_before += found.z;
         equal_before = found.w;
+        if (found.x >= kBins && prefix > 0) {   // all keys that share these digits stay: the threshold is the number below them.  For most weights two or three digits do.
+            prefix -= 1;
+            above_before += equal_before;
+            rest = equal_before = 0;
+            break;
+        }
     }
     // the keys that stay without asking
     for (int k = everything; k < fixed; k += step) {
@@ -247,31 +232,52 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
         move(kept);
         return;
     }
-    int use = 0;
-    // In order of position, four neighbours per thread and round.  (Put side by side in shared memory first, to leave in whole lines: no faster.)
-    constexpr int kEach = 4;
-#pragma unroll 1
-    for (int k0 = 0; k0 < mine; k0 += kEach * kSelectThreads) {
-        const int first = k0 + kEach * (int)threadIdx.x;
-        float x[kEach];
-        weights_of(first, x);
-        uint32_t flags = 0, counts = 0;   // bit u: above, bit 4 + u: equal; two counts of at most 2048
+    // Each warp lists the keys of a stretch of its own: it counts them, adds those of the warps before, and goes over them again in order of position.
+    // (In one pass, with a prefix sum over the CTA per 2048 keys: 81 against 69 us for 224 contexts of 928 to 4230 tokens to 43 keys.)
+    const int stretch = ((mine - 1) / (kSelectWarps * 128) + 1) * 128, end = min(mine, (warp + 1) * stretch);
+    uint32_t above = 0, equal = 0;
+    for (int k = warp * stretch + 4 * lane; k < end; k += 128) {
+        uint32_t x[4];
+        keys_of(k, x);
 #pragma unroll
-        for (int u = 0; u < kEach; ++u) {
-            const uint32_t key = ordered(x[u]);
-            if (first + u < mine && key > prefix) flags |= 1u << u, counts += 1u << 16;
-            if (first + u < mine && key == prefix) flags |= 16u << u, counts += 1u;
+        for (int u = 0; u < 4; ++u) {
+            above += k + u < mine && x[u] > prefix;
+            equal += k + u < mine && x[u] == prefix;
         }
-        uint32_t tile;
-        const uint32_t b = block_prefix(counts, s, use, &tile);
-        uint32_t my_above = above_before + (b >> 16), my_equal = equal_before + (b & 0xffffu);
+    }
+    above = __reduce_add_sync(0xffffffffu, above);
+    equal = __reduce_add_sync(0xffffffffu, equal);
+    if (lane == 0) s.above[warp] = above, s.equal[warp] = equal;
+    __syncthreads();
+    above_before += __reduce_add_sync(0xffffffffu, lane < warp ? s.above[lane] : 0u);
+    equal_before += __reduce_add_sync(0xffffffffu, lane < warp ? s.equal[lane] : 0u);
+#pragma unroll 1
+    for (int k0 = warp * stretch; k0 < end; k0 += 128) {
+        const int first = k0 + 4 * lane;
+        uint32_t x[4], flags = 0, counts = 0;   // bit u: above, bit 4 + u: equal; two counts of at most 128
+        keys_of(first, x);
 #pragma unroll
-        for (int u = 0; u < kEach; ++u) {
+        for (int u = 0; u < 4; ++u) {
+            if (first + u < mine && x[u] > prefix) flags |= 1u << u, counts += 1u << 16;
+            if (first + u < mine && x[u] == prefix) flags |= 16u << u, counts += 1u;
+        }
+        if (!__any_sync(0xffffffffu, flags)) continue;
+        uint32_t sum = counts;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t c = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += c;
+        }
+        const uint32_t tile = __shfl_sync(0xffffffffu, sum, 31);
+        uint32_t my_above = above_before + (sum - counts >> 16), my_equal = equal_before + (sum - counts & 0xffffu);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
             const bool is_above = flags >> u & 1, is_equal = flags >> (4 + u) & 1;
             if (is_above || (is_equal && my_equal < rest)) {
                 const int slot = p.sinks + (int)(my_above + min(my_equal, rest));
                 list[slot] = p.sinks + begin + first + u;
-                new_w[slot] = x[u];
+                // the weight itself where its key stands for several: NaN, zeros
+                new_w[slot] = x[u] == 0u || x[u] == 0x80000000u ? __ldg(x0 + first + u) : __uint_as_float(x[u] & 0x80000000u ? x[u] ^ 0x80000000u : ~x[u]);
             }
             my_above += is_above;
             my_equal += is_equal;
@@ -279,7 +285,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) sw_evict_select_kernel(cons
         above_before += tile >> 16;
         equal_before += tile & 0xffffu;
     }
-    cluster.sync();   // a CTA's last histogram is read by the others
+    all_here();   // a CTA's last histogram is read by the others
     if constexpr (D > 0) move(kept, true);
 }
 
@@ -297,9 +303,10 @@ __global__ void __launch_bounds__(kMoveThreads) sw_evict_move_kernel(const Evict
 
 template <class F>
 cudaError_t for_each_select(F f) {
-    cudaError_t e = f(sw_evict_select_kernel<0>);
-    if (e == cudaSuccess) e = f(sw_evict_select_kernel<64>);
-    return e == cudaSuccess ? f(sw_evict_select_kernel<128>) : e;
+    for (auto* kernel : {sw_evict_select_kernel<0, kManyThreads>, sw_evict_select_kernel<64, kManyThreads>, sw_evict_select_kernel<128, kManyThreads>,
+                         sw_evict_select_kernel<0, kFewThreads>, sw_evict_select_kernel<64, kFewThreads>, sw_evict_select_kernel<128, kFewThreads>})
+        if (const cudaError_t e = f(kernel)) return e;
+    return cudaSuccess;
 }
 cudaError_t configure_evict_kernels() {
     return for_each_select([](auto* kernel) {
@@ -310,11 +317,18 @@ cudaError_t configure_evict_kernels() {
 cudaError_t launch_evict(const EvictParams& params, int head_dim, int num_sms, cudaStream_t stream) {
     EvictParams p = params;
     const int64_t pairs = (int64_t)p.n * p.Hkv;
-    // as many CTAs per pair as keep the launch within two CTAs an SM
+    // As many CTAs per pair as keep the launch within two CTAs an SM, and as hold the longest row of weights in shared memory (61 contexts of 40606 to 131072
+    // tokens, 4 KV heads: 148 us with eight, 173 us with one).
     int ranks = kMaxRanks;
-    while (ranks > 1 && pairs * ranks > 2 * (int64_t)num_sms) ranks /= 2;
+    while (ranks > 1 && pairs * ranks > 2 * (int64_t)num_sms && p.capacity <= ranks / 2 * kHeldKeys) ranks /= 2;
     p.held = std::min(kHeldKeys, (p.capacity + ranks - 1) / ranks);
-    const bool fused = pairs * ranks >= num_sms;
+    // Smaller CTAs where there is little for each one to do.  Pairs for more than two large CTAs an SM: 128 contexts of 2048 to 4096 tokens to 64 keys, 8 KV heads,
+    // 32 against 43 us; 64 of 8192 to 16384 to 1024, though, 183 against 124.  Fewer pairs: one context of 8192 to 1024 12.6 against 14.4, of 32768 to 8192 25.7 against 24.7.
+    const bool few = p.capacity <= (pairs > 2 * (int64_t)num_sms ? 8192 : 1024 * ranks);
+    const int threads = few ? kFewThreads : kManyThreads;
+    // One launch where the selecting CTAs fill the SMs or have a page a warp at most to copy (2 contexts of 524 to 584 tokens to 18: 10.8 against 12.4 us; one
+    // of 32768 to 8192, which has more, 32.7 against 24.4).
+    const bool fused = pairs * ranks >= num_sms || (p.budget - 1) / kPageSize < ranks * (threads / 32);
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -323,15 +337,15 @@ cudaError_t launch_evict(const EvictParams& params, int head_dim, int num_sms, c
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(pairs * ranks));
-    cfg.blockDim = dim3(kSelectThreads);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = sizeof(SelectShared) + (size_t)p.held * sizeof(float);
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    if (fused)
-        return head_dim == 64 ? cudaLaunchKernelEx(&cfg, sw_evict_select_kernel<64>, p) : cudaLaunchKernelEx(&cfg, sw_evict_select_kernel<128>, p);
-    cudaError_t e = cudaLaunchKernelEx(&cfg, sw_evict_select_kernel<0>, p);
-    if (e != cudaSuccess) return e;
+    auto* select = few ? (!fused ? sw_evict_select_kernel<0, kFewThreads> : head_dim == 64 ? sw_evict_select_kernel<64, kFewThreads> : sw_evict_select_kernel<128, kFewThreads>)
+                       : (!fused ? sw_evict_select_kernel<0, kManyThreads> : head_dim == 64 ? sw_evict_select_kernel<64, kManyThreads> : sw_evict_select_kernel<128, kManyThreads>);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, select, p);
+    if (e != cudaSuccess || fused) return e;
     const int64_t tasks = pairs * ((p.budget - 1) / kPageSize + 1), blocks = (tasks + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
     cfg.gridDim = dim3((unsigned)(blocks < 8 * (int64_t)num_sms ? blocks : 8 * (int64_t)num_sms));
     cfg.blockDim = dim3(kMoveThreads);

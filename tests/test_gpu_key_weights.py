@@ -169,7 +169,8 @@ def test_evict_ties_and_special_weights():
     check_evict(c2, w2, 101, 2, 5)
 
 
-@pytest.mark.parametrize("lens,budget", [([60000], 1000), ([120000, 3000], 40000), ([20000] * 60, 64)])   # keys beyond those held in shared memory; every cluster size
+# keys beyond those held in shared memory; every cluster size; CTAs of both sizes
+@pytest.mark.parametrize("lens,budget", [([60000], 1000), ([120000, 3000], 40000), ([20000] * 60, 64), ([150000], 900), ([9000] * 60, 64), ([1900, 40] * 30, 64)])
 def test_evict_long(lens, budget):
     c = U.Case((4, 1, 64) if len(lens) < 3 else (8, 8, 64), lens, seed=3, spare=sum(-(-min(n, budget) // U.PAGE) for n in lens) + 8)
     w = weights_of(c, 2 * len(lens), max(lens))
@@ -199,6 +200,22 @@ def test_evict_long(lens, budget):
             j = torch.arange(m, device=c.dev)
             to = to_dev(new_pages[new_indptr[i]:new_indptr[i + 1]]).long()[j // U.PAGE]
             assert torch.equal(c.pool[to, :, h, j % U.PAGE].view(torch.int16), c.pool[src, :, h, keep % U.PAGE].view(torch.int16))
+
+
+@pytest.mark.parametrize("n,capacity", [(1, 300), (1, 9000), (60, 300), (60, 9000)])   # CTAs of both sizes, alone and in clusters
+@pytest.mark.parametrize("budget", [17, 101])
+def test_evict_special_weights_in_every_form(n, capacity, budget):
+    """Thresholds among NaN, infinities, zeros of both signs, numbers one step apart and numbers that share their first 16 bits."""
+    c = U.Case((8, 8, 64), [300] * n, seed=n, spare=n * 7 + 8)
+    gen = torch.Generator(device=c.dev)
+    gen.manual_seed(budget)
+    near = torch.randint(0, 9, (2 * n, 8, capacity), device=c.dev, generator=gen, dtype=torch.int32)
+    w = (near + 0x3F800000).view(torch.float32).clone()
+    w[::5] = torch.tensor([math.nan, math.inf, -math.inf, 0.0, -0.0, 1e-45, -1e-45, 3.0, -3.0], device=c.dev)[near[::5].long()]
+    w[1::5] = -w[1::5]
+    w[2::5] = math.nan
+    w[2::5, :, 40:70] = -math.inf
+    check_evict(c, w, budget, 1, 3)
 
 
 def test_evict_what_does_not_fit_is_reported():
