@@ -209,7 +209,7 @@ sw_status sw_decode_attn_weights_run(sw_ctx* ctx, const void* kv_pool, const sw_
  * int32).  What lies behind these is left as it is.  The old pages and rows are left as they are too; no new page or row may be among those that the
  * call reads, nor twice among the new ones.  1 <= budget <= capacity, sinks + recent <= budget.  A request that does not fit (page list too
  * short, row outside the weights, context longer than a row) is reported by sw_check_status, gets new_len 0 and nothing else; a page id outside the
- * pool is reported, and that page's rows of that head are not copied.  Asynchronous (two launches). */
+ * pool is reported, and that page's rows of that head are not copied.  Asynchronous (one or two launches). */
 sw_status sw_kv_evict(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const sw_key_weights* weights, const int32_t* new_page_indptr,
                       const int32_t* new_pages, const int32_t* new_row_of, int32_t budget, int32_t sinks, int32_t recent, int32_t* kept,
                       int32_t* new_len, void* stream);
