@@ -1,0 +1,64 @@
+"""When sw_decode_attn_weights_run leaves the accumulated weights alone, and batches whose page lists do not start at the first entry."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_07883_b200 import binding as B
+from tests import op_util as U
+from tests.test_gpu_key_weights import check_weights, weigh, weights_of
+
+pytestmark = pytest.mark.gpu
+
+
+def rows_of(c, rows):
+    return torch.tensor(list(rows), dtype=torch.int32, device=c.dev)
+
+
+def status(c):
+    return B.sw_check_status(c.ctx, raise_on_error=False)[0]
+
+
+def test_expired_wait_behind_another_problem_leaves_the_weights_alone():
+    """The status words keep the first problem: one that was reported before and not yet asked for must not hide an expired wait."""
+    c = U.Case((32, 8, 128), [3000] * 40, seed=3)     # (enough that some page is still on its way)
+    w = weights_of(c, 40, 3000)
+    before = w.clone()
+    kw = B.KeyWeights(w, rows_of(c, range(40)))
+    page = int(c.batch.decode_pages[7])
+    c.batch.decode_pages[7] = c.pages
+    c.renew()
+    B.sw_mixed_attn_run(c.ctx, c.pool, c.db, c.q, c.out, c.lse)      # reports a page outside the pool
+    c.batch.decode_pages[7] = page
+    c.renew()
+    torch.cuda.synchronize()
+    B._lib.sw_ctx_set_line_wait(c.ctx.handle, ctypes.c_int64(0))     # what has not arrived at the first look has expired
+    weigh(c, kw)
+    torch.cuda.synchronize()
+    assert torch.equal(w, before)
+    assert status(c) == B.SW_ERR_OUT_OF_RANGE and status(c) == B.SW_OK
+
+
+@pytest.mark.parametrize("heads,lens", [((8, 2, 64), [40, 100, 30]), ((8, 1, 128), [700] * 40), ((8, 2, 64), [90] * 500)])
+def test_bad_page_leaves_the_weights_alone(heads, lens):
+    """The request's log-sum-exps are those of page 0's keys then.  Once the problem has been asked for, weights are written again."""
+    c = U.Case(heads, lens, seed=4)
+    n = len(lens)
+    w = weights_of(c, n, max(lens))
+    before = w.clone()
+    kw = B.KeyWeights(w, rows_of(c, range(n)))
+    page = int(c.batch.decode_pages[2])
+    for bad in (c.pages, -1):
+        c.batch.decode_pages[2] = bad
+        c.renew()
+        weigh(c, kw)
+        c.batch.decode_pages[2] = page
+        c.renew()
+        weigh(c, kw)                          # (not asked for yet)
+        torch.cuda.synchronize()
+        assert torch.equal(w, before)
+        assert status(c) == B.SW_ERR_OUT_OF_RANGE
+    weigh(c, kw)
+    c.ok()
+    check_weights(c, before, w, list(range(n)), c.check(c.pool.double()))
