@@ -196,7 +196,9 @@ typedef struct {
  * lse must be given, on a 16-byte boundary.  scratch: 128-byte aligned device memory of sw_attn_weights_scratch_bytes(layout,
  * decode_page_indptr[num_decode]) bytes, of no use between calls.  A request that does not fit (row outside the weights, context longer than a
  * row, pages beyond the scratch) is reported by sw_check_status; its output is written, its weights are not (nor, beyond the scratch, those of
- * the pages there).  Where a wait of the attention expires no weights are written.  The sums do not depend on any order.  SW_ERR_UNSUPPORTED for batches with chunks.  Asynchronous (two launches). */
+ * the pages there).  Where a wait of the attention expires or a page id lies outside the pool no weights are written, by that call and those
+ * after it, until sw_check_status has returned the problem.  The sums do not depend on any order.  SW_ERR_UNSUPPORTED for batches with chunks.
+ * Asynchronous (two launches). */
 size_t sw_attn_weights_scratch_bytes(const sw_layout* layout, int64_t decode_pages);
 sw_status sw_decode_attn_weights_run(sw_ctx* ctx, const void* kv_pool, const sw_batch* batch, const void* q, void* out, float* lse,
                                      const sw_key_weights* weights, void* scratch, size_t scratch_bytes, void* stream);

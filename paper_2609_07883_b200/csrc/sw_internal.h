@@ -24,8 +24,10 @@ constexpr int kMaxChunk = 65536;        // chunk tokens per iteration (256-row g
 constexpr long long kLineWaitCycles = 2000000000LL;   // limit of a wait in the line of decode stages (about a second)
 
 // Control words at the start of the workspace.
+// kCtrSpoiled: a wait expired, or an attention that leaves its scores behind could not work them all out, since the status was last asked for.  (A word of
+// its own: the status keeps the first problem only.)
 // kCtrArrived counts the CTAs that have ended, modulo two grids; launches use the two counter sets at kCtrSets in turn.
-enum CtrlWord { kCtrArrived = 0, kCtrStatus = 2, kCtrDetail = 3, kCtrSets = 16, kCtrWords = 64 };
+enum CtrlWord { kCtrArrived = 0, kCtrStatus = 2, kCtrDetail = 3, kCtrSpoiled = 4, kCtrSets = 16, kCtrWords = 64 };
 // Words of a counter set: decode units handed out by the counter, chunk-prefill entries likewise, and (fused launches with
 // chunks) CTAs that have written their share of the new K/V rows; decode units of the launch + 1 once they are known.
 enum SetWord { kSetWork = 0, kSetPrefill = 1, kSetAppend = 2, kSetItems = 3, kSetWords = 16 };

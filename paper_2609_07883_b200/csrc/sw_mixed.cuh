@@ -53,7 +53,14 @@ __device__ __forceinline__ int page_of(const Span& v, int j) { return j < v.head
 // device status: first problem wins
 // ---------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void report(int32_t* ctrl, int code, int site, int index) {
+    if (code == SW_ERR_DEVICE_TIMEOUT) ctrl[kCtrSpoiled] = 1;
     if (atomicCAS(&ctrl[kCtrStatus], 0, code) == 0) ctrl[kCtrDetail] = (site << 24) | (index & 0xFFFFFF);
+}
+// The same for problems that leave scores unwritten or wrong (kScored: nobody may add up weights from them).
+template <Option O>
+__device__ __forceinline__ void report_spoiled(int32_t* ctrl, int code, int site, int index) {
+    if (O == kScored) ctrl[kCtrSpoiled] = 1;
+    report(ctrl, code, site, index);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -476,7 +483,7 @@ __device__ __forceinline__ Line make_line(const MixedParams& p, int* prefix, int
     line.prefix = prefix;
     int before = block_exclusive_scan(here, scratch + 16, &line.stages);
     if (line.stages < 0 || (int64_t)line.stages * p.Hkv > kLineMaxStages) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) report(p.ctrl, SW_ERR_WORKSPACE, kSiteScratch, line.stages);
+        if (blockIdx.x == 0 && threadIdx.x == 0) report_spoiled<O>(p.ctrl, SW_ERR_WORKSPACE, kSiteScratch, line.stages);
         line.stages = 0;
     }
     const int few = min(line_whole_max(D), kLineWhole + line.stages * p.Hkv / ((int)gridDim.x * 4));
@@ -979,7 +986,7 @@ __device__ bool run_unit(const CUtensorMap* kvp_map, const MixedParams& p, const
         if (page < 0 || (int64_t)page >= p.num_pages) {
             // a bad id never reaches the copy engine: the problem is reported and page 0 is fetched in its place, so
             // the barrier still receives the bytes it expects
-            if (lane == 0) report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteAttnPage, u.q_row);
+            if (lane == 0) report_spoiled<O>(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteAttnPage, u.q_row);
             page = 0;
         }
         // the request's last page holds the row this iteration appends
@@ -1226,7 +1233,7 @@ __device__ __forceinline__ void run_line(const CUtensorMap* kvp_map, const Mixed
                 if constexpr (O == kWindow) page = page_of(span_of<O>(p, line.len[i]), page);
                 id = p.decode_pages[line.indptr[i] + page];
                 if (id < 0 || (int64_t)id >= p.num_pages) {   // never reaches the copy engine
-                    report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteAttnPage, p.C + i);
+                    report_spoiled<O>(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteAttnPage, p.C + i);
                     id = 0;
                 }
             }
@@ -1591,7 +1598,7 @@ __global__ void __launch_bounds__(kThreads, 1) sw_mixed_attn_kernel(const __grid
     const Plan plan = make_plan<O>(p, unit_prefix, lens, indptr, scratch, late, p.stages_per_us);
     if ((int)blockIdx.x == prefill_ctas && threadIdx.x == 0) atomicExch(p.ctrl + misc[kMiscSet] + kSetItems, plan.total_items + 1);
     if (plan.total_items > p.max_items) {
-        if (threadIdx.x == 0) report(p.ctrl, SW_ERR_WORKSPACE, kSiteScratch, plan.total_items);
+        if (threadIdx.x == 0) report_spoiled<O>(p.ctrl, SW_ERR_WORKSPACE, kSiteScratch, plan.total_items);
     } else {
         if (!tensor_prefill && p.append_last) list_last_pages<D>(p, plan.len, plan.indptr, base, sets);
         int32_t* work = p.ctrl + lds_s32(base + Geo<D>::kSetOffset) + kSetWork;

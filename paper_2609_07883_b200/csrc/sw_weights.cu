@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocksPerSm) sw_key_wei
         if (__ldcg(p.page_indptr + mid) <= begin) i = mid; else hi = mid;
     }
     grid_dependency_wait();
-    const int status = ld_relaxed_gpu(&p.ctrl[kCtrStatus]);   // (looked at with the first request's words)
+    const int spoiled = ld_relaxed_gpu(&p.ctrl[kCtrSpoiled]);   // (looked at with the first request's words)
     constexpr float kLog2E = 1.4426950408889634f;
     const int key = lane & 15, g = p.group, lines = p.Hkv * kPageSize * g / 32;   // of 128 bytes, of a page's scores
     int at = 0, next = begin, len = 0, row = 0;
@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocksPerSm) sw_key_wei
             row = p.row_of[i];
             const int pages = len > 0 ? (len - 1) / kPageSize + 1 : 0;
             ok = pages <= next - at;   // (reported by the attention launch)
-            ok = ok && status != SW_ERR_DEVICE_TIMEOUT;   // some scores may not have been written
+            ok = ok && spoiled == 0;   // some scores may not have been written
             if (ok && len > 0 && (row < 0 || (int64_t)row >= p.rows || len > p.capacity)) {
                 if (lane == 0) report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteWeights, i);
                 ok = false;
