@@ -21,8 +21,9 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocksPerSm) sw_key_wei
     // The batch was there before the attention launch started: where the warp's stretch lies is found while that ends (64 contexts of 256-2048
     // tokens 68.4 -> 60.9 us; with the request's other words as well 63.4).
     const int lane = threadIdx.x & 31, warps = gridDim.x * (kWeightThreads / 32), w = blockIdx.x * (kWeightThreads / 32) + threadIdx.x / 32;
-    const int64_t total = __ldcg(p.page_indptr + p.n);
-    const int begin = (int)(total * w / warps), end = (int)(total * (w + 1) / warps);
+    const int first = __ldcg(p.page_indptr);   // (the batch may be the later requests of a longer list)
+    const int64_t total = (int64_t)__ldcg(p.page_indptr + p.n) - first;
+    const int begin = first + (int)(total * w / warps), end = first + (int)(total * (w + 1) / warps);
     int i = 0;
     for (int hi = p.n; hi - i > 1;) {   // largest i with page_indptr[i] <= begin
         const int mid = (i + hi) >> 1;
@@ -42,7 +43,7 @@ __global__ void __launch_bounds__(kWeightThreads, kWeightBlocksPerSm) sw_key_wei
             len = p.kv_len[i];
             row = p.row_of[i];
             const int pages = len > 0 ? (len - 1) / kPageSize + 1 : 0;
-            ok = pages <= next - at;   // (reported by the attention launch)
+            ok = pages <= next - at && at <= e;   // (reported by the attention launch; offsets that decrease have no entry of theirs here)
             ok = ok && spoiled == 0;   // some scores may not have been written
             if (ok && len > 0 && (row < 0 || (int64_t)row >= p.rows || len > p.capacity)) {
                 if (lane == 0) report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteWeights, i);

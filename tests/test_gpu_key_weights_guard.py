@@ -62,3 +62,18 @@ def test_bad_page_leaves_the_weights_alone(heads, lens):
     weigh(c, kw)
     c.ok()
     check_weights(c, before, w, list(range(n)), c.check(c.pool.double()))
+
+
+@pytest.mark.parametrize("heads,lens", [((8, 2, 64), [300, 40, 1000, 17]), ((32, 8, 128), [2000, 100]), ((8, 1, 128), [500] * 40)])
+def test_lists_that_start_behind_the_first_entry(heads, lens):
+    """The later requests of a longer batch: decode_page_indptr starts above zero.  Weights in front of the rows in use stay as they are."""
+    c = U.Case(heads, lens, seed=5)
+    n, at = len(lens), 70
+    c.batch.decode_pages = np.concatenate([np.full(at, -1, dtype=np.int32), c.batch.decode_pages])
+    c.batch.decode_page_indptr = c.batch.decode_page_indptr + np.int32(at)
+    c.renew()
+    w = weights_of(c, n + 2, max(lens) + 3)
+    before = w.clone()
+    weigh(c, B.KeyWeights(w, rows_of(c, range(2, n + 2))))
+    c.ok()
+    check_weights(c, before, w, list(range(2, n + 2)), c.check(c.pool.double()))
