@@ -164,6 +164,15 @@ __global__ void __launch_bounds__(kKv8Threads) sw_kv8_expand_kernel(const Kv8Par
                 asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(x[e]) : "r"(x[e]), "r"(factor));
                 if (rest != 1.f) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(x[e]) : "r"(x[e]), "r"(more));
             }
+            // the codes 0x7f and 0xff, which this made 480 times the scale, stand for NaN
+            if ((((w[i].x & 0x7f7f7f7fu) + 0x01010101u) | ((w[i].y & 0x7f7f7f7fu) + 0x01010101u)) & 0x80808080u) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t two = (e < 2 ? w[i].x : w[i].y) >> 16 * (e & 1);
+                    if ((two & 0x7fu) == 0x7fu) x[e] |= 0x7fffu;
+                    if ((two & 0x7f00u) == 0x7f00u) x[e] |= 0x7fff0000u;
+                }
+            }
             dst[i * 32] = (i * 32 + lane) / kRowLanes < valid ? make_uint4(x[0], x[1], x[2], x[3]) : make_uint4(0u, 0u, 0u, 0u);
         }
         if (hs == 0 && lane == 0) p.list[b] = b;

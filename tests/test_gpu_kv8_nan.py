@@ -51,12 +51,16 @@ def test_pages_that_no_list_names_may_hold_anything(heads, chunks, lens, scratch
 @pytest.mark.parametrize("heads,chunk,page", [((8, 2, 64), (1000, 300), 75), ((32, 8, 128), (1000, 300), 80), ((8, 1, 128), (0, 200), 3), ((4, 4, 64), (37, 500), 20),
                                               ((32, 8, 128), (700, 1500), 100)])
 @pytest.mark.parametrize("scratch", [False, True])
-def test_nan_keys_reach_the_rows_that_attend_them(heads, chunk, page, scratch):
+@pytest.mark.parametrize("how", ["scale", "codes"])
+def test_nan_keys_reach_the_rows_that_attend_them(heads, chunk, page, scratch, how):
     """K of one block, some way into the chunk: the rows in front of it do not attend it, and the other heads have nothing to do with it."""
     c = U.Case(heads, [], [chunk], seed=page)
     codes, scales = U.quantise(c.pool)
     want = U.dequantise(codes, scales)
-    scales[int(c.batch.prefill_pages[page]), 0, 0] = math.nan
+    if how == "scale":
+        scales[int(c.batch.prefill_pages[page]), 0, 0] = math.nan
+    else:
+        codes.view(torch.uint8)[int(c.batch.prefill_pages[page]), 0, 0] = 0x7F
     attend(c, codes, scales, scratch)
     g, (P, C) = c.shape.group, chunk
     behind = (page + 1) * U.PAGE - 1 - P         # the row that attends the whole block
@@ -64,3 +68,30 @@ def test_nan_keys_reach_the_rows_that_attend_them(heads, chunk, page, scratch):
     assert bool(torch.isnan(c.out[behind:, :g]).all()) and bool(torch.isnan(c.lse[behind:, :g]).all())
     assert not bool(torch.isnan(c.out[:, g:]).any()) and not bool(torch.isnan(c.lse[:, g:]).any())
     c.check(want, rows=slice(0, page * U.PAGE - P), floor=FLOOR)
+
+
+@pytest.mark.parametrize("scratch", [False, True])
+@pytest.mark.parametrize("how", ["scale", "codes", "one code"])
+def test_nan_values_reach_the_rows_that_attend_them(scratch, how):
+    """V of one block, or one element of it.  Rows in front whose last 128 keys hold the block may be reached too, as by the V rows of a 16-bit pool; those
+    before them are not, nor is any log-sum-exp."""
+    heads, (P, C), page = (32, 8, 128), (704, 1500), 100
+    c = U.Case(heads, [100], [(P, C)], seed=2)
+    codes, scales = U.quantise(c.pool)
+    want = U.dequantise(codes, scales)
+    at = int(c.batch.prefill_pages[page])
+    columns = slice(None)
+    if how == "scale":
+        scales[at, 1, 0] = math.nan
+    elif how == "codes":
+        codes.view(torch.uint8)[at, 1, 0] = 0xFF
+    else:
+        codes.view(torch.uint8)[at, 1, 0, 0, 37] = 0x7F
+        columns = slice(37, 38)
+    attend(c, codes, scales, scratch)
+    assert bool(torch.isnan(c.out[page * U.PAGE - P:C, :4, columns]).all())
+    assert not bool(torch.isnan(c.out[:, 4:]).any()) and not bool(torch.isnan(c.lse).any())
+    if how == "one code":
+        assert not bool(torch.isnan(c.out[:, :, :37]).any()) and not bool(torch.isnan(c.out[:, :, 38:]).any())
+    # a tile of 128 rows is 32 tokens; those that reach into the block's 128 keys start at token 1536 - P
+    c.check(want, rows=list(range(page * U.PAGE // 128 * 128 - P)) + [C], floor=FLOOR)
