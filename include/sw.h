@@ -209,7 +209,8 @@ sw_status sw_decode_attn_weights_run(sw_ctx* ctx, const void* kv_pool, const sw_
  * new_pages[new_page_indptr[i] ..] (device, CSR like the batch's), their weights to the front of row new_row_of[i] (device int32 [num_decode]); the
  * positions they came from to kept[i][head][0 ..] (device int32 [num_decode][num_kv_heads][budget]), their number to new_len[i] (device
  * int32).  What lies behind these is left as it is.  The old pages and rows are left as they are too; no new page or row may be among those that the
- * call reads, nor twice among the new ones.  1 <= budget <= capacity, sinks + recent <= budget.  A request that does not fit (page list too
+ * call reads, nor twice among the new ones.  kept and new_len overlap neither each other nor an array that the call reads
+ * (lengths are not updated in place: SW_ERR_INVALID_ARG).  1 <= budget <= capacity, sinks + recent <= budget.  A request that does not fit (page list too
  * short, row outside the weights, context longer than a row) is reported by sw_check_status, gets new_len 0 and nothing else; a page id outside the
  * pool is reported, and that page's rows of that head are not copied.  Asynchronous (one or two launches). */
 sw_status sw_kv_evict(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const sw_key_weights* weights, const int32_t* new_page_indptr,

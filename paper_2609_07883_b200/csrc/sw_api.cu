@@ -657,6 +657,29 @@ sw_status check_weights(const sw_key_weights* w, const char* who) {
     if (w->rows < 1 || w->capacity < 1) return sw_fail(SW_ERR_INVALID_ARG, "%s: %lld rows of %d weights", who, (long long)w->rows, w->capacity);
     return SW_OK;
 }
+// The CTAs of an eviction read the batch's and the lists' words while others already write what it returns (lengths updated in place would be read as
+// old ones by some of a request's CTAs and as new ones by others, which wait for one another).  The page lists' own lengths are on the device.
+sw_status check_evict_arrays(const sw_batch* b, const sw_key_weights* w, int num_kv_heads, const int32_t* new_page_indptr, const int32_t* new_pages,
+                             const int32_t* new_row_of, int32_t budget, const int32_t* kept, const int32_t* new_len, const char* who) {
+    struct Words {
+        const int32_t* at;
+        int64_t count;
+        const char* name;
+    };
+    const int64_t n = b->num_decode;
+    const Words out[2] = {{new_len, n, "new_len"}, {kept, n * num_kv_heads * std::max(budget, 1), "kept"}};
+    const Words in[] = {{b->decode_kv_len, n, "decode_kv_len"}, {b->decode_page_indptr, n + 1, "decode_page_indptr"}, {b->decode_pages, 1, "decode_pages"},
+                        {w ? w->row_of : nullptr, n, "row_of"}, {new_page_indptr, n + 1, "new_page_indptr"}, {new_pages, 1, "new_pages"},
+                        {new_row_of, n, "new_row_of"}, out[0]};
+    auto overlap = [](const Words& a, const Words& c) {   // (as numbers: the arrays need not be parts of one)
+        const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.at), c0 = reinterpret_cast<uintptr_t>(c.at);
+        return a.at && c.at && a0 < c0 + (uintptr_t)c.count * 4 && c0 < a0 + (uintptr_t)a.count * 4;
+    };
+    for (const Words& o : out)
+        for (const Words& i : in)
+            if (o.name != i.name && overlap(o, i)) return sw_fail(SW_ERR_INVALID_ARG, "%s: %s overlaps %s", who, o.name, i.name);
+    return SW_OK;
+}
 }  // namespace
 
 size_t sw_attn_weights_scratch_bytes(const sw_layout* layout, int64_t decode_pages) {
@@ -710,7 +733,10 @@ sw_status sw_kv_evict(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const s
                       int32_t* new_len, void* stream) {
     const char* who = "sw_kv_evict";
     Chunks ch;
-    sw_status st = check_batch(ctx, batch, who, &ch);
+    sw_status st = SW_OK;
+    if (batch && batch->num_decode > 0)
+        st = check_evict_arrays(batch, weights, ctx ? ctx->layout.num_kv_heads : 1, new_page_indptr, new_pages, new_row_of, budget, kept, new_len, who);
+    if (st == SW_OK) st = check_batch(ctx, batch, who, &ch);
     if (st != SW_OK) return st;
     if (ch.rows > 0) return sw_fail(SW_ERR_UNSUPPORTED, "%s: decode requests only (no chunks)", who);
     if (batch->num_decode == 0) return SW_OK;

@@ -39,3 +39,24 @@ def test_window_is_checked_before_anything_else():
     for window, sinks in [(0, 0), (-3, 0), (1, -1)]:
         assert B._lib.sw_mixed_attn_window_run(None, None, None, window, sinks, None, None, None, None) == B.SW_ERR_INVALID_ARG
         assert "window" in B.sw_last_error()
+
+
+@pytest.mark.parametrize("new_len,kept,name", [
+    (0x10000, 0x90000, "decode_kv_len"), (0x1000C, 0x90000, "decode_kv_len"), (0xFFF4, 0x90000, "decode_kv_len"),   # the same; its last word; from in front
+    (0x20010, 0x90000, "decode_page_indptr"), (0x30000, 0x90000, "decode_pages"), (0x40000, 0x90000, "row_of"), (0x50010, 0x90000, "new_page_indptr"),
+    (0x60000, 0x90000, "new_pages"), (0x70004, 0x90000, "new_row_of"), (0x80000, 0x10000, "decode_kv_len"), (0x80000, 0x80000 - 4 * 4 * 8 + 4, "new_len"),
+    (0x80000, 0x70000 - 4 * 4 * 8 + 4, "new_row_of")])
+def test_evict_refuses_outputs_over_inputs(new_len, kept, name):
+    """Four requests, a budget of 8: lengths are not updated in place, nor anything else that the call still reads."""
+    batch = B.sw_batch(0, 0, None, 0, 4, 0x10000, 0x20000, 0x30000, 0, None, None, None)
+    weights = B.sw_key_weights(0x1000000, 8, 64, 0x40000)
+    assert B._lib.sw_kv_evict(None, 0x2000000, batch, weights, 0x50000, 0x60000, 0x70000, 8, 0, 0, kept, new_len, None) == B.SW_ERR_INVALID_ARG
+    assert "overlaps " + name in B.sw_last_error()
+
+
+def test_evict_takes_neighbouring_arrays():
+    batch = B.sw_batch(0, 0, None, 0, 4, 0x10000, 0x20000, 0x30000, 0, None, None, None)
+    weights = B.sw_key_weights(0x1000000, 8, 64, 0x40000)
+    for new_len, kept in [(0x10010, 0x90000), (0xFFF0, 0x90000), (0x80000, 0x70010), (0x80000, 0x80000 - 4 * 4 * 8)]:
+        assert B._lib.sw_kv_evict(None, 0x2000000, batch, weights, 0x50000, 0x60000, 0x70000, 8, 0, 0, kept, new_len, None) == B.SW_ERR_INVALID_ARG
+        assert "null context" in B.sw_last_error()
