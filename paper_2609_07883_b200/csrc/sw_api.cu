@@ -734,11 +734,11 @@ sw_status sw_kv_evict(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const s
     const char* who = "sw_kv_evict";
     Chunks ch;
     sw_status st = SW_OK;
+    if (batch && (batch->chunk_len > 0 || batch->num_chunks > 0)) return sw_fail(SW_ERR_UNSUPPORTED, "%s: decode requests only (no chunks)", who);
     if (batch && batch->num_decode > 0)
         st = check_evict_arrays(batch, weights, ctx ? ctx->layout.num_kv_heads : 1, new_page_indptr, new_pages, new_row_of, budget, kept, new_len, who);
     if (st == SW_OK) st = check_batch(ctx, batch, who, &ch);
     if (st != SW_OK) return st;
-    if (ch.rows > 0) return sw_fail(SW_ERR_UNSUPPORTED, "%s: decode requests only (no chunks)", who);
     if (batch->num_decode == 0) return SW_OK;
     if (!kv_pool || !new_page_indptr || !new_pages || !new_row_of || !kept || !new_len) return sw_fail(SW_ERR_INVALID_ARG, "%s: null tensor", who);
     st = check_weights(weights, who);
