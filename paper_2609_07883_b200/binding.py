@@ -285,6 +285,8 @@ class KeyWeights:
 
         if weights.dtype != torch.float32 or weights.dim() != 3 or not weights.is_contiguous():
             raise ValueError("weights must be a contiguous fp32 tensor [rows][num_kv_heads][capacity]")
+        if weights.shape[2] > 2 ** 31 - 1:
+            raise ValueError("a row holds 2^31 - 1 weights at most")
         if row_of.dtype != torch.int32 or row_of.dim() != 1 or not row_of.is_contiguous():
             raise ValueError("row_of must be a contiguous int32 tensor")
         self.weights, self.row_of = weights, row_of

@@ -321,7 +321,7 @@ cudaError_t launch_evict(const EvictParams& params, int head_dim, int num_sms, c
     // tokens, 4 KV heads: 148 us with eight, 173 us with one).
     int ranks = kMaxRanks;
     while (ranks > 1 && pairs * ranks > 2 * (int64_t)num_sms && p.capacity <= ranks / 2 * kHeldKeys) ranks /= 2;
-    p.held = std::min(kHeldKeys, (p.capacity + ranks - 1) / ranks);
+    p.held = std::min(kHeldKeys, (p.capacity - 1) / ranks + 1);
     // Smaller CTAs where there is little for each one to do.  Pairs for more than two large CTAs an SM: 128 contexts of 2048 to 4096 tokens to 64 keys, 8 KV heads,
     // 32 against 43 us; 64 of 8192 to 16384 to 1024, though, 183 against 124.  Fewer pairs: one context of 8192 to 1024 12.6 against 14.4, of 32768 to 8192 25.7 against 24.7.
     const bool few = p.capacity <= (pairs > 2 * (int64_t)num_sms ? 8192 : 1024 * ranks);

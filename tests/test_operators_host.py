@@ -60,3 +60,11 @@ def test_evict_takes_neighbouring_arrays():
     for new_len, kept in [(0x10010, 0x90000), (0xFFF0, 0x90000), (0x80000, 0x70010), (0x80000, 0x80000 - 4 * 4 * 8)]:
         assert B._lib.sw_kv_evict(None, 0x2000000, batch, weights, 0x50000, 0x60000, 0x70000, 8, 0, 0, kept, new_len, None) == B.SW_ERR_INVALID_ARG
         assert "null context" in B.sw_last_error()
+
+
+def test_rows_of_weights_that_are_too_long():
+    import torch
+
+    rows = torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        B.KeyWeights(torch.empty(1, 1, 2 ** 31, device="meta"), rows)      # (would wrap to a negative capacity)
