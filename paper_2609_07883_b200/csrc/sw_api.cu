@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -219,6 +220,36 @@ sw_status check_batch(const sw_ctx* ctx, const sw_batch* b, const char* who, Chu
 }  // namespace
 
 namespace {
+// What a context asks of its device.  The driver takes 1.2 ms for each clock rate (and 2.5 for all properties at once, which are not asked for), so a process asks
+// once per device: a context is created in 35 us (80 where it gets the streams of host-buffer iterations) instead of 5 ms.
+struct DeviceFacts {
+    int major, minor, sms, mem_khz, bus_bits, sm_khz;
+};
+sw_status device_facts(int device, DeviceFacts* out) {
+    constexpr int kMost = 64;
+    static DeviceFacts kept[kMost];
+    static std::atomic<int> state[kMost];   // 0: nothing; 1: being written; 2: there
+    const bool keeps = device >= 0 && device < kMost;
+    if (keeps && state[device].load(std::memory_order_acquire) == 2) {
+        *out = kept[device];
+        return SW_OK;
+    }
+    DeviceFacts f{};
+    const struct {
+        cudaDeviceAttr attr;
+        int* to;
+    } asked[] = {{cudaDevAttrComputeCapabilityMajor, &f.major}, {cudaDevAttrComputeCapabilityMinor, &f.minor}, {cudaDevAttrMultiProcessorCount, &f.sms},
+                 {cudaDevAttrMemoryClockRate, &f.mem_khz}, {cudaDevAttrGlobalMemoryBusWidth, &f.bus_bits}, {cudaDevAttrClockRate, &f.sm_khz}};
+    for (const auto& a : asked) SW_CUDA(cudaDeviceGetAttribute(a.to, a.attr, device));
+    int nothing = 0;
+    if (keeps && state[device].compare_exchange_strong(nothing, 1, std::memory_order_relaxed)) {   // (of several threads one keeps what all have found)
+        kept[device] = f;
+        state[device].store(2, std::memory_order_release);
+    }
+    *out = f;
+    return SW_OK;
+}
+
 sw_status make_copy_stream(sw_ctx* ctx) {
     SW_CUDA(cudaStreamCreateWithFlags(&ctx->copies, cudaStreamNonBlocking));
     SW_CUDA(cudaEventCreateWithFlags(&ctx->ev_start, cudaEventDisableTiming));
@@ -250,11 +281,12 @@ sw_status sw_create(const sw_layout* layout, int device, void* workspace, size_t
     const WsLayout w = ws_layout(*layout, max_chunk, max_decode, max_pages);
     if (!workspace || workspace_bytes < w.total || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0)
         return sw_fail(SW_ERR_WORKSPACE, "sw_create: workspace must be 256-byte aligned and hold %zu bytes", w.total);
-    cudaDeviceProp prop;
-    SW_CUDA(cudaGetDeviceProperties(&prop, device));
-    if (prop.major != 10)
+    DeviceFacts facts;
+    const sw_status known = device_facts(device, &facts);
+    if (known != SW_OK) return known;
+    if (facts.major != 10)
         return sw_fail(SW_ERR_UNSUPPORTED, "sw_create: device %d is compute capability %d.%d; this library is sm_100a only",
-                       device, prop.major, prop.minor);
+                       device, facts.major, facts.minor);
     // the set-up below runs with `device` current; the caller's current device is put back before returning
     int caller_device = device;
     SW_CUDA(cudaGetDevice(&caller_device));
@@ -265,17 +297,13 @@ sw_status sw_create(const sw_layout* layout, int device, void* workspace, size_t
         }
     } restore{caller_device, device};
     if (caller_device != device) SW_CUDA(cudaSetDevice(device));
-    int mem_khz = 0, bus_bits = 0, sm_khz = 0;
-    SW_CUDA(cudaDeviceGetAttribute(&mem_khz, cudaDevAttrMemoryClockRate, device));
-    SW_CUDA(cudaDeviceGetAttribute(&bus_bits, cudaDevAttrGlobalMemoryBusWidth, device));
-    SW_CUDA(cudaDeviceGetAttribute(&sm_khz, cudaDevAttrClockRate, device));
     sw_ctx* ctx = new (std::nothrow) sw_ctx();
     if (!ctx) return sw_fail(SW_ERR_INVALID_ARG, "sw_create: out of host memory");
     ctx->layout = *layout;
     if (ctx->layout.sm_scale <= 0.f) ctx->layout.sm_scale = 1.0f / std::sqrt((float)layout->head_dim);
     ctx->device = device;
-    ctx->num_sms = std::min(prop.multiProcessorCount, sw::kMaxCtas);
-    sw::device_timing(mem_khz, bus_bits, sm_khz, layout->head_dim, &ctx->stage_us, &ctx->step_us);
+    ctx->num_sms = std::min(facts.sms, sw::kMaxCtas);
+    sw::device_timing(facts.mem_khz, facts.bus_bits, facts.sm_khz, layout->head_dim, &ctx->stage_us, &ctx->step_us);
     ctx->max_chunk = max_chunk;
     ctx->max_decode = max_decode;
     ctx->max_pages = max_pages;
@@ -298,11 +326,11 @@ sw_status sw_create(const sw_layout* layout, int device, void* workspace, size_t
     int per_sm = 0, window_per_sm = 0;
     if (e == cudaSuccess) e = sw::mixed_attn_resident_ctas_per_sm(layout->head_dim, &per_sm);
     if (e == cudaSuccess) e = sw::window_attn_resident_ctas_per_sm(layout->head_dim, &window_per_sm);
-    ctx->window_grid_resident = (int64_t)window_per_sm * prop.multiProcessorCount >= ctx->num_sms;
+    ctx->window_grid_resident = (int64_t)window_per_sm * facts.sms >= ctx->num_sms;
     // The fused launch lets CTAs wait for one another's share of the KV append, so the whole grid has to be resident.
     // Where it would not be (fewer SMs than the properties promise cannot be seen here, but a smaller shared-memory
     // or register budget can) sw_mixed_iteration_run issues the append as a launch of its own.
-    ctx->grid_resident = (int64_t)per_sm * prop.multiProcessorCount >= ctx->num_sms;
+    ctx->grid_resident = (int64_t)per_sm * facts.sms >= ctx->num_sms;
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) {
         delete ctx;
