@@ -167,13 +167,19 @@ sw_status sw_mixed_iteration_window_run(sw_ctx* ctx, void* kv_pool, const sw_bat
  * sw_kv8_append writes the iteration's rows (bf16, as sw_kv_append's).  A block's scale is the smallest power of two, 2^-100 at least, that
  * brings the largest magnitude of its rows to 448 or less; rows are divided by it and rounded to the nearest e4m3 value.  Rows that join
  * others in a page may raise the scale (it never falls): the older rows are then rounded again at the new one, which changes only values that
- * become subnormal.  A row at a page's first slot starts the page anew.  A non-finite element makes its block's scale NaN, and NaN of all that is read
- * from the block.  Rows of different chunks or requests must lie on different pages, or the shared page holds anything afterwards
+ * become subnormal.  A row at a page's first slot starts the page anew.  A non-finite element makes its block's scale NaN, and the block's values with
+ * it.  Rows of different chunks or requests must lie on different pages, or the shared page holds anything afterwards
  * (append such rows by calls of their own).  Slots behind the new rows are left as they are.
  *
  * sw_kv8_attn_run is sw_mixed_attn_run over such a pool.  The scales must be powers of two (between 2^-100 and 2^120) or NaN.  Its products see the
- * values that the pool stands for exactly; queries are rounded at 2^-18 of their row's largest element, softmax weights at 2^-32 of
- * their row's largest, and V at 2^-33 of the largest magnitude that the scales of the 128 keys around it allow.
+ * values that the pool stands for exactly.  What is rounded beside the output, relative to the row's largest:
+ *   decode rows: queries at 2^-31, softmax weights at 2^-40 times the largest scale of V so far over that of the key's page (2^16 at most; beyond
+ *     that the weights follow);
+ *   chunk rows: queries at 2^-18, softmax weights at 2^-32, and V at 2^-33 of the largest magnitude that the scales of the 128 keys around it allow;
+ *   chunk rows that read a copy (scratch): as sw_mixed_attn_run, softmax weights to bf16 and 2^x to 7.5e-5.
+ * Rows that attend a NaN key or value are NaN, and no others, with two exceptions in chunks: a NaN value also reaches the rows in front of it whose
+ * last 128 keys hold it (with those of the same 128 / group tokens), as in sw_mixed_attn_run; and in a copy, rows that attend no more than the first four keys of
+ * a NaN block may leave these out.
  * scratch (optional; 256-byte aligned device memory of sw_kv8_scratch_bytes(layout, sum over the chunks of ceil((P + C) / 16)) bytes, of no use
  * between calls): where it is large enough and that is faster, long chunks read a copy of their prompts in 16 bits, made there first.
  * Both calls are asynchronous. */

@@ -4,12 +4,13 @@
 // weights the ones at the lowest positions; NaN counts as the lightest).  The kept keys keep their order.  They go to other pages and
 // another row of weights: pages that requests share stay as they are, and no thread reads what another one writes.
 //
-// Selection (sw_evict_select_kernel): a cluster of 1 to 8 CTAs per pair finds the threshold by radix, four digits of 8 bits of the weights as ordered
-// integers.  Each CTA has an equal stretch of the pair's keys, the first ones of it in shared memory, so the weights are read from memory once, and a
+// Selection (sw_evict_select_kernel): a cluster of 1 to 8 CTAs per pair finds the threshold by radix, digits of 8 bits of the weights as ordered
+// integers: four at most, and none after one whose keys all stay.  Each CTA has an equal stretch of the pair's keys, the first ones of it in shared memory, so the weights are read from memory once, and a
 // histogram per digit that the cluster's CTAs read from one another.  That traffic is what a pass costs beside its barrier: with digits of 11
 // bits (three passes, 64 KB into every CTA of a cluster of eight) a 32768-token context took 22 us.  From the same histograms every CTA
 // knows how many keys the CTAs before it keep, so a last round writes the kept positions in order.
-// Copy (sw_evict_move_kernel): one warp per (request, new page, KV head); bound by memory.
+// Copy: one warp per (request, new page, KV head); bound by memory.  The selecting CTAs do it themselves where they fill the SMs or have little to copy,
+// a launch of its own (sw_evict_move_kernel) otherwise.
 #include <cooperative_groups.h>
 
 #include <algorithm>

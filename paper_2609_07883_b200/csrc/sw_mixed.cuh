@@ -25,8 +25,8 @@ using namespace swptx;
 // What a launch does beside the plain iteration, fixed at compile time like the form (below): every option is a kernel of its own, so
 // the plain kernels keep their code.
 //   kWindow   rows attend the last `window` keys and the first `sinks` ones; pages and key tiles without such a key are passed over
-//   kKv8      the decode requests' pages hold e4m3 values with a scale per (page, K|V, KV head); the chunks' prompts are read from a copy
-//             in 16 bits (sw_kv8.cu)
+//   kKv8      the pages hold e4m3 values with a scale per (page, K|V, KV head), chunks' prompts too; where that is faster and there is room for it,
+//             the chunks read a copy of their prompts in 16 bits and their part of the kernel is the plain one (sw_kv8.cu)
 //   kScored   decode-only launches that also leave every score behind (sw_weights.cu)
 enum Option { kPlain, kWindow, kKv8, kScored };
 

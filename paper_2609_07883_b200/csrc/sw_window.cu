@@ -1,8 +1,9 @@
 // The mixed iteration inside a sliding window with sinks: the kernels of sw_mixed.cuh with kWindow.
 //
-// The row at position t attends key k when k <= t and (k > t - window or k < sinks).  A decode request's pages, and a chunk's 128-key tiles,
-// that hold no such key are passed over when the work is laid out (span_of, pf_passed), so plan, line and pieces see only what is read;
-// inside the pages at the window's edges the scores of unattended keys are masked.
+// The row at position t attends key k when k <= t and (k > t - window or k < sinks).  Pages that hold no such key are passed over when the work
+// is laid out: a decode request's visible pages are numbered without gaps (span_of), and the 128-key tiles of a chunk's item are made of the pages that
+// its rows attend (pf_passed), so plan, line and pieces see only what is read.  In the pages at the window's edges the scores of unattended
+// keys are masked.
 #include "sw_mixed.cuh"
 
 namespace sw {
