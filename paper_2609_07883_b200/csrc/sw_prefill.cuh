@@ -156,18 +156,7 @@ struct PfPlan {
     uint32_t table;     // several chunks: shared address of the chunk table (k of chunk j is field 4)
 };
 
-// kWindow: page j of an item is page j of the prompt below `head` (pages with sinks), j + skip from there on.  (Not members of the other options' items: two more
-// words of an array that is indexed at run time cost the plain kernel 8 bytes of spills.)
-template <Option O>
-struct PfPassed {
-    static constexpr int head = 0, skip = 0;
-};
-template <>
-struct PfPassed<kWindow> {
-    int head, skip;
-};
-template <Option O>
-struct PfItem : PfPassed<O> {
+struct PfItem {
     int item;        // number of the item among all chunks' items; within its chunk: rank * Hkv + kvh
     int kvh;
     int chunk;       // which chunk of the iteration the item belongs to (its descriptors are in the shared table)
@@ -177,6 +166,7 @@ struct PfItem : PfPassed<O> {
     int j0, j1;      // this entry's piece of the item: KV tiles [j0, j1)
     int piece;       // index of the piece (0 when the item is whole)
     int slot0;       // scratch slot of the item's piece 0 (tail items only)
+    int head, skip;  // kWindow: page j of the item is page j of the prompt below `head` (pages with sinks), j + skip from there on
     int pieces;      // pieces the item is cut into (several chunks: each chunk has its own count)
 };
 
@@ -492,8 +482,8 @@ __device__ __forceinline__ PfPlan pf_make_plan(uint32_t table) {  // worked out 
 }
 
 template <bool kMulti, Option O>
-__device__ __forceinline__ PfItem<O> pf_entry(const MixedParams& p, const PfPlan& plan, int entry) {
-    PfItem<O> it;
+__device__ __forceinline__ PfItem pf_entry(const MixedParams& p, const PfPlan& plan, int entry) {
+    PfItem it;
     it.pieces = plan.pieces;
     it.slot0 = 0;
     it.chunk = 0;
@@ -538,7 +528,7 @@ __device__ __forceinline__ PfItem<O> pf_entry(const MixedParams& p, const PfPlan
     it.kvh = local % p.Hkv;
     const int tt = 128 / p.group;
     const int tp = pf_num_groups(p.group, cC) - 1 - rank;
-    if constexpr (O == kWindow) pf_passed<O>(p, cP, tp * 2 * tt, it.head, it.skip);
+    pf_passed<O>(p, cP, tp * 2 * tt, it.head, it.skip);
     for (int t = 0; t < 2; ++t) {
         it.tok0[t] = (tp * 2 + t) * tt;
         it.nkv[t] = pf_tiles_of(p.group, cP, cC, it.tok0[t], it.skip);
@@ -557,7 +547,7 @@ __device__ __forceinline__ PfItem<O> pf_entry(const MixedParams& p, const PfPlan
 // ---- role: TMA producer (one warp) ----------------------------------------------------------------------------
 template <int D, bool kMulti, Option O>
 __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUtensorMap* q_map, const MixedParams& p,
-                                           const PfShared& sh, const PfItem<O>& it, uint32_t& kv_it) {
+                                           const PfShared& sh, const PfItem& it, uint32_t& kv_it) {
     using G = PfGeo<D>;
     // The whole warp runs the role: lane i owns page i of every 128-key tile (its page id, its TMA boxes), so the
     // eight pages of a tile are issued by one instruction instead of a loop of one thread.
@@ -654,7 +644,7 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
 // Keys at or past P + C are never attended, but their V rows still enter the P V product with weight zero; zero them
 // so that whatever an unwritten page slot (or a stale buffer) holds cannot turn 0 * x into NaN.
 template <int D, bool kMulti, Option O>
-__device__ __forceinline__ bool pf_sanitize(const MixedParams& p, const PfShared& sh, const PfItem<O>& it, uint32_t& kv_it) {
+__device__ __forceinline__ bool pf_sanitize(const MixedParams& p, const PfShared& sh, const PfItem& it, uint32_t& kv_it) {
     using G = PfGeo<D>;
     const int lane = threadIdx.x & 31;
     const int kv_total = pf_chunk<D, kMulti>(p, sh, 0, it.chunk) + pf_chunk<D, kMulti>(p, sh, 1, it.chunk);
@@ -825,7 +815,7 @@ __device__ __forceinline__ void pf_issue_pv_half(const PfShared& sh, int t, uint
 
 // The entry's Q tiles are there (kKv8: split in two parts by their softmax warps).
 template <Option O>
-__device__ __forceinline__ bool pf_wait_q(const MixedParams& p, const PfShared& sh, const PfItem<O>& it, PfMmaState& st) {
+__device__ __forceinline__ bool pf_wait_q(const MixedParams& p, const PfShared& sh, const PfItem& it, PfMmaState& st) {
     if constexpr (O == kKv8) {
         for (int t = 0; t < 2; ++t)
             if (it.nkv[t] > it.j0) {
@@ -839,7 +829,7 @@ __device__ __forceinline__ bool pf_wait_q(const MixedParams& p, const PfShared& 
 }
 
 template <int D, Option O>
-__device__ __forceinline__ bool pf_mma(const MixedParams& p, const PfShared& sh, const PfItem<O>& it, PfMmaState& st) {
+__device__ __forceinline__ bool pf_mma(const MixedParams& p, const PfShared& sh, const PfItem& it, PfMmaState& st) {
     const bool leader = elect_one();
     auto act = [&](int t, int j) { return j < it.j1 && j < it.nkv[t]; };
     auto last_active = [&](int j) { return act(1, j) ? 1 : 0; };
@@ -892,7 +882,7 @@ __device__ __forceinline__ bool pf_mma(const MixedParams& p, const PfShared& sh,
 // in the plain order, both in one kernel: 23.4, but 256 + 128 beside four contexts 13.1 -> 14.4.  One rolled loop over (step, tile)
 // with the same order: 76.7 -> 86.)
 template <int D, Option O>
-__device__ __forceinline__ bool pf_mma_ahead(const MixedParams& p, const PfShared& sh, const PfItem<O>& it, PfMmaState& st) {
+__device__ __forceinline__ bool pf_mma_ahead(const MixedParams& p, const PfShared& sh, const PfItem& it, PfMmaState& st) {
     const bool leader = elect_one();
     auto act = [&](int t, int j) { return j < it.j1 && j < it.nkv[t]; };
     auto commit = [&](int bar) {
@@ -1031,7 +1021,7 @@ struct PfScratch {
 
 template <int D, bool kMulti, Option O>
 __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const MixedParams& p, const PfShared& sh,
-                                           const PfPlan& plan, const PfScratch& scr, const PfItem<O>& it, int t,
+                                           const PfPlan& plan, const PfScratch& scr, const PfItem& it, int t,
                                            PfSoftmaxState& st) {
     using G = PfGeo<D>;
     if (it.j1 <= it.j0) return true;  // an empty piece (more pieces than steps)
@@ -1409,7 +1399,7 @@ __device__ __forceinline__ void prefill_phase(const CUtensorMap* kv_map, const C
         setmaxnreg_dec<kPfRegsLight>();
         int entry = first_entry;
         for (int iter = 0; entry < plan.n_entries; ++iter) {
-            const PfItem<O> it = pf_entry<kMulti, O>(p, plan, entry);
+            const PfItem it = pf_entry<kMulti, O>(p, plan, entry);
             if (warp == 0) {
                 if (it.j1 > it.j0) pf_produce<D, kMulti, O>(kv_map, q_map, p, sh, it, prod_kv_it);
             } else if (warp == 1) {
@@ -1440,7 +1430,7 @@ __device__ __forceinline__ void prefill_phase(const CUtensorMap* kv_map, const C
         setmaxnreg_inc<kPfRegsHeavy>();
         int entry = first_entry;
         for (int iter = 0; entry < plan.n_entries; ++iter) {
-            const PfItem<O> it = pf_entry<kMulti, O>(p, plan, entry);
+            const PfItem it = pf_entry<kMulti, O>(p, plan, entry);
             pf_softmax<D, kMulti, O>(out_map, p, sh, plan, scr, it, (warp - 4) >> 2, sm_state);
             if (O == kKv8 && it.j1 > it.j0) {
                 sm_state.kv_it += it.j1 - it.j0;
