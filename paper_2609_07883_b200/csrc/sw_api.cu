@@ -573,7 +573,7 @@ size_t kv8_scratch(const sw_layout& l, int64_t pages) { return (size_t)pages * p
 // Whether an iteration's chunks read a 16-bit copy of their prompts, made by a launch of its own, rather than the 8-bit pool.  Measured with
 // 32/8/128: a 128-key step of an entry is up to 0.9 us longer over the 8-bit pool (the widened V tiles go through a shared memory that the
 // tensor cores' operands keep busy), a copy costs 4 us and 0.6 us a megabyte of the prompts, and most of the rest is the same.  Over the
-// pool | with a copy, us: 1024 tokens at prefix 4096 104 | 81, 512 at 512 28 | 26, 4096 at 28672 2060 | 1600; 128 at 28672 94 | 110.
+// pool | with a copy, us: 1024 tokens at prefix 4096 104 | 78, 512 at 512 31 | 27, 4096 at 28672 2040 | 1575; 128 at 28672 94 | 110.
 bool chunks_copied(const sw_layout& l, const Chunks& ch, int num_sms) {
     const int group = l.num_q_heads / l.num_kv_heads;
     double steps = 0., megabytes = 0.;
