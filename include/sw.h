@@ -223,6 +223,54 @@ sw_status sw_kv_evict(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const s
                       const int32_t* new_pages, const int32_t* new_row_of, int32_t budget, int32_t sinks, int32_t recent, int32_t* kept,
                       int32_t* new_len, void* stream);
 
+/* ---- in front of the iteration, beside it and behind it (no counterparts in the paper) ---------------------------- */
+
+/* Rotary positions.  Pair i (of rotary_dim / 2) of every query and key head is turned by t = position * turns[i] turns: its elements (a, b) become
+ * m (a cos t - b sin t) and m (b cos t + a sin t), m = magnitude.  The pair's elements are i and i + rotary_dim / 2, or, interleaved, 2i and 2i + 1; those
+ * from rotary_dim on are left as they are.  rotary_dim: a multiple of 16, the head size at most.  Angles are worked out in 64 bits, rotations in 32.
+ * positions: NULL for the batch's own (P + j for chunk row j, decode_kv_len[i] - 1 for request i), or one int32 per row, where a row's place in the
+ * cache is not its position (after an eviction, say).
+ * Strides: elements between rows, multiples of 8; 0 for dense rows.  So q, k and v can be slices of one projection's rows; what is written is dense. */
+typedef struct {
+    const double* turns;      /* device [rotary_dim / 2], see sw_rope_frequencies */
+    int32_t rotary_dim;
+    int32_t interleaved;
+    float magnitude;          /* 1 where nothing else is asked for */
+    const int32_t* positions; /* device [C + n] or NULL */
+    int64_t q_stride, k_stride, v_stride;
+} sw_rope;
+
+/* Fills turns (HOST array, rotary_dim / 2 values, to be copied to the device) and *magnitude.  Pair i has w = base^(-2i / rotary_dim) radians a position, and
+ *   SW_ROPE_PLAIN   w / 2 pi turns;
+ *   SW_ROPE_LINEAR  w / factor: positions stretched by `factor`;
+ *   SW_ROPE_BASE    the base times factor^(rotary_dim / (rotary_dim - 2)): the slowest pair stretched by `factor`, the fastest kept;
+ *   SW_ROPE_BANDS   pairs that turn `high` times or more over original_len positions are kept, those that turn `low` times or less are stretched by `factor`,
+ *                   and between them the frequency goes over linearly in their turns;
+ *   SW_ROPE_RAMP    likewise, but linearly in i, between the pairs that turn `high` and `low` times, these rounded outward; and the
+ *                   magnitude is 0.1 ln(factor) + 1 (1 with all others).
+ * factor >= 1; original_len, low and high are of the last two only, 0 < low < high. */
+typedef enum { SW_ROPE_PLAIN = 0, SW_ROPE_LINEAR = 1, SW_ROPE_BASE = 2, SW_ROPE_BANDS = 3, SW_ROPE_RAMP = 4 } sw_rope_scaling;
+sw_status sw_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double original_len, double low, double high,
+                              double* turns, float* magnitude);
+
+/* sw_kv_append of keys that are rotated on the way, with the queries: q [C+n][num_q_heads][head_dim] goes to q_out, k_new rotated and v_new as it is to
+ * their places in the pool.  Places and problems as sw_kv_append's (of a row that has no place the queries are rotated all the same).  Followed by
+ * sw_mixed_attn_run or one of its kind on q_out.  q_out may be q where q is dense; it overlaps no other input. */
+sw_status sw_rope_append(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const sw_rope* rope, const void* q, const void* k_new, const void* v_new,
+                         void* q_out, void* stream);
+
+/* The same without a pool: k goes to k_out, [C+n][num_kv_heads][head_dim], for the calls that append by themselves (sw_mixed_iteration_run,
+ * sw_mixed_iteration_window_run, sw_kv8_append).  q_out may be q and k_out may be k, where these are dense.  v_stride is ignored, and so are
+ * decode page lists (their arrays must be there).  Both calls are asynchronous, one launch. */
+sw_status sw_rope_run(sw_ctx* ctx, const sw_batch* batch, const sw_rope* rope, const void* q, const void* k, void* q_out, void* k_out, void* stream);
+
+/* Cross attention: sw_mixed_attn_run over the cached states of an encoder, whose number has nothing to do with the rows'.  prefix_len (or
+ * chunk_prefix_lens[j]) is the number of keys of a chunk's source, 0 or more, and every row of the chunk attends all of them; its page list needs
+ * ceil(P / 16) entries.  decode_kv_len[i], 0 or more, likewise (where no list has an entry the lists may be NULL).  Rows without keys are zero, with a log-sum-exp of minus infinity.  The keys and values are
+ * written once, by sw_kv_append with a batch of their own (prefix_len 0, chunk_len the number of states).  List the chunk with the longest items
+ * (keys) first.  One launch, and one more for each chunk without keys.  Asynchronous. */
+sw_status sw_cross_attn_run(sw_ctx* ctx, const void* kv_pool, const sw_batch* batch, const void* q, void* out, float* lse, void* stream);
+
 /* Profiler step (Sec. 5.1; Sec. 6.4): time the attention of one iteration over a stack of `layers` pools
  * (kv_pools: HOST array of `layers` device pool pointers, used round-robin so that successive launches do
  * not hit the same cache lines).  Runs `warmup` untimed and `reps` timed iterations of `layers` launches

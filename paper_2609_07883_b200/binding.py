@@ -67,13 +67,19 @@ class sw_key_weights(C.Structure):
     _fields_ = [("weights", C.c_void_p), ("rows", C.c_int64), ("capacity", C.c_int32), ("row_of", C.c_void_p)]
 
 
+class sw_rope(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float),
+                ("positions", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
+
+
 EXPORTS = ["sw_workspace_bytes", "sw_create", "sw_destroy", "sw_kv_append", "sw_mixed_attn_run", "sw_mixed_iteration_run",
            "sw_mixed_iteration_host", "sw_cost_probe", "sw_cost_probe_iteration", "sw_check_status", "sw_cost_table_create",
            "sw_cost_table_destroy", "sw_cost_table_lookup", "sw_choose_chunk", "sw_choose_chunks", "sw_last_error",
            "sw_decode_attn_static", "sw_selftest_wait_timeout", "sw_telemetry_create", "sw_telemetry_destroy",
            "sw_telemetry_record", "sw_telemetry_margin", "sw_telemetry_exceeds", "sw_telemetry_get_totals",
            "sw_telemetry_reset", "sw_mixed_attn_window_run", "sw_mixed_iteration_window_run", "sw_kv8_scratch_bytes", "sw_kv8_append",
-           "sw_kv8_attn_run", "sw_attn_weights_scratch_bytes", "sw_decode_attn_weights_run", "sw_kv_evict"]
+           "sw_kv8_attn_run", "sw_attn_weights_scratch_bytes", "sw_decode_attn_weights_run", "sw_kv_evict", "sw_rope_frequencies",
+           "sw_rope_append", "sw_rope_run", "sw_cross_attn_run"]
 
 _vp, _i32, _i64 = C.c_void_p, C.c_int32, C.c_int64
 _lib.sw_workspace_bytes.restype = C.c_size_t
@@ -95,6 +101,10 @@ _lib.sw_attn_weights_scratch_bytes.restype = C.c_size_t
 _lib.sw_attn_weights_scratch_bytes.argtypes = [C.POINTER(sw_layout), _i64]
 _lib.sw_decode_attn_weights_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, C.POINTER(sw_key_weights), _vp, C.c_size_t, _vp]
 _lib.sw_kv_evict.argtypes = [_vp, _vp, C.POINTER(sw_batch), C.POINTER(sw_key_weights), _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp]
+_lib.sw_rope_frequencies.argtypes = [_i32, C.c_double, _i32, C.c_double, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_double), C.POINTER(C.c_float)]
+_lib.sw_rope_append.argtypes = [_vp, _vp, C.POINTER(sw_batch), C.POINTER(sw_rope), _vp, _vp, _vp, _vp, _vp]
+_lib.sw_rope_run.argtypes = [_vp, C.POINTER(sw_batch), C.POINTER(sw_rope), _vp, _vp, _vp, _vp, _vp]
+_lib.sw_cross_attn_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, _vp]
 _lib.sw_cost_probe.argtypes = [_vp, C.POINTER(_vp), _i32, C.POINTER(sw_batch), _vp, _vp, _i32, _i32,
                                C.POINTER(_i64), C.POINTER(_i64), C.POINTER(_i64), _vp]
 _lib.sw_cost_probe_iteration.argtypes = [_vp, C.POINTER(_vp), _i32, C.POINTER(sw_batch), _vp, _vp, _vp, _vp, _i32, _i32,
@@ -325,6 +335,80 @@ def sw_kv_evict(ctx: Context, kv_pool, batch: DeviceBatch, weights: KeyWeights, 
     _check(_lib.sw_kv_evict(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), C.byref(weights.struct), _ptr(new_page_indptr),
                             _ptr(new_pages), _ptr(new_weights.row_of), budget, sinks, recent, _ptr(kept), _ptr(new_len),
                             _stream_handle(stream)), "sw_kv_evict")
+
+
+# ---- rotary positions, cross attention, sampling ----------------------------------------------------------------------
+SW_ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+
+def sw_rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, original_len: float = 0.0,
+                        low: float = 0.0, high: float = 0.0):
+    """Turns per position of every pair (float64, on the host) and the magnitude of the rotation."""
+    turns = np.zeros(max(rotary_dim // 2, 0), dtype=np.float64)
+    magnitude = C.c_float(0.0)
+    _check(_lib.sw_rope_frequencies(rotary_dim, base, SW_ROPE_SCALINGS[scaling], factor, original_len, low, high,
+                                    turns.ctypes.data_as(C.POINTER(C.c_double)), C.byref(magnitude)), "sw_rope_frequencies")
+    return turns, float(magnitude.value)
+
+
+class Rope:
+    """Frequencies on the device, how the pairs of a head lie, and (optional) the rows' positions (int32, one per row of the batch)."""
+
+    def __init__(self, turns, interleaved: bool = False, magnitude: float = 1.0, positions=None, device=None):
+        import torch
+
+        turns = torch.as_tensor(turns)
+        if turns.dtype != torch.float64 or turns.dim() != 1:
+            raise ValueError("turns must be float64, one per pair")
+        if positions is not None and (positions.dtype != torch.int32 or positions.dim() != 1 or not positions.is_contiguous()):
+            raise ValueError("positions must be a contiguous int32 tensor")
+        self.turns = turns.to("cuda" if device is None else device).contiguous()
+        self.interleaved, self.magnitude, self.positions = bool(interleaved), float(magnitude), positions
+
+    def struct(self, rows: int, q, k, v=None) -> sw_rope:
+        if self.positions is not None and self.positions.numel() < rows:
+            raise ValueError(f"positions names {self.positions.numel()} rows, the batch has {rows}")
+        return sw_rope(self.turns.data_ptr(), 2 * self.turns.numel(), int(self.interleaved), self.magnitude, _ptr(self.positions), q.stride(0), k.stride(0),
+                       0 if v is None else v.stride(0))
+
+
+def _check_rows(name: str, t, rows: int, heads: int, head_dim: int, dense: bool) -> None:
+    # what the library cannot see from a pointer
+    import torch
+
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[0] < rows or tuple(t.shape[1:]) != (heads, head_dim):
+        raise ValueError(f"{name} must be bf16 [{rows}][{heads}][{head_dim}]")
+    if t.stride(2) != 1 or t.stride(1) != head_dim or (dense and t.stride(0) != heads * head_dim):
+        raise ValueError(f"{name}: {'rows' if dense else 'heads of a row'} must lie side by side")
+
+
+def _rope_rows(ctx: Context, batch: DeviceBatch, rope: Rope, q, k, v, q_out, k_out) -> sw_rope:
+    sh, rows = ctx.shape, batch.host.num_rows
+    for name, t, heads, dense in (("q", q, sh.num_q_heads, False), ("k", k, sh.num_kv_heads, False), ("v", v, sh.num_kv_heads, False),
+                                  ("q_out", q_out, sh.num_q_heads, True), ("k_out", k_out, sh.num_kv_heads, True)):
+        if t is not None:
+            _check_rows(name, t, rows, heads, sh.head_dim, dense)
+    return rope.struct(rows, q, k, v)
+
+
+def sw_rope_append(ctx: Context, kv_pool, batch: DeviceBatch, rope: Rope, q, k_new, v_new, q_out, stream=None) -> None:
+    """Rotated queries to ``q_out``, rotated keys and the values to their pages.  ``q``, ``k_new``, ``v_new`` may be slices of one projection's rows."""
+    s = _rope_rows(ctx, batch, rope, q, k_new, v_new, q_out, None)
+    _check(_lib.sw_rope_append(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), C.byref(s), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(q_out),
+                               _stream_handle(stream)), "sw_rope_append")
+
+
+def sw_rope_run(ctx: Context, batch: DeviceBatch, rope: Rope, q, k, q_out, k_out, stream=None) -> None:
+    """Rotated queries and keys, for the calls that append by themselves; ``q_out`` may be ``q`` and ``k_out`` ``k``."""
+    s = _rope_rows(ctx, batch, rope, q, k, None, q_out, k_out)
+    _check(_lib.sw_rope_run(ctx.handle, C.byref(batch.struct), C.byref(s), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _stream_handle(stream)),
+           "sw_rope_run")
+
+
+def sw_cross_attn_run(ctx: Context, kv_pool, batch: DeviceBatch, q, out, lse=None, stream=None) -> None:
+    """As ``sw_mixed_attn_run``, but the rows of a chunk attend the ``prefix_len`` keys of its page list, all of them; no keys: zeros."""
+    _check(_lib.sw_cross_attn_run(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), _ptr(q), _ptr(out), _ptr(lse), _stream_handle(stream)),
+           "sw_cross_attn_run")
 
 
 def sw_cost_probe_iteration(ctx: Context, kv_pools, batch: DeviceBatch, k_new, v_new, q, out, warmup: int = 3,

@@ -194,7 +194,8 @@ sw_status chunks_of(const sw_batch* b, const char* who, Chunks* out) {
     return SW_OK;
 }
 
-sw_status check_batch(const sw_ctx* ctx, const sw_batch* b, const char* who, Chunks* chunks) {
+// cross: a chunk's keys are its prefix alone, and there may be none, nor pages.
+sw_status check_batch(const sw_ctx* ctx, const sw_batch* b, const char* who, Chunks* chunks, bool cross = false) {
     if (!ctx || !b) return sw_fail(SW_ERR_INVALID_ARG, "%s: null context or batch", who);
     if (b->prefix_len < 0 || b->chunk_len < 0 || b->num_decode < 0 || b->num_prefill_pages < 0)
         return sw_fail(SW_ERR_INVALID_ARG, "%s: negative size in batch", who);
@@ -206,13 +207,13 @@ sw_status check_batch(const sw_ctx* ctx, const sw_batch* b, const char* who, Chu
     if (b->num_decode > sw::kMaxDecode)
         return sw_fail(SW_ERR_UNSUPPORTED, "%s: at most %d decode requests per iteration", who, sw::kMaxDecode);
     for (int j = 0; j < chunks->n; ++j) {
-        const int64_t need = ((int64_t)chunks->P[j] + chunks->C[j] + sw::kPageSize - 1) / sw::kPageSize;
+        const int64_t need = ((int64_t)chunks->P[j] + (cross ? 0 : chunks->C[j]) + sw::kPageSize - 1) / sw::kPageSize;
         const int have = chunks->page0[j + 1] - chunks->page0[j];
-        if (!b->prefill_pages || have < need)
-            return sw_fail(SW_ERR_OUT_OF_RANGE, "%s: prefill page list has %d entries, P+C needs %lld", who, have,
+        if ((!b->prefill_pages && need > 0) || have < need)
+            return sw_fail(SW_ERR_OUT_OF_RANGE, "%s: prefill page list has %d entries, %s needs %lld", who, have, cross ? "P" : "P+C",
                            (long long)need);
     }
-    if (b->num_decode > 0 && (!b->decode_kv_len || !b->decode_page_indptr || !b->decode_pages))
+    if (b->num_decode > 0 && (!b->decode_kv_len || !b->decode_page_indptr || (!b->decode_pages && !cross)))
         return sw_fail(SW_ERR_INVALID_ARG, "%s: decode arrays missing", who);
     return SW_OK;
 }
@@ -323,6 +324,7 @@ sw_status sw_create(const sw_layout* layout, int device, void* workspace, size_t
     if (e == cudaSuccess) e = sw::configure_kv8_kernels(layout->head_dim);
     if (e == cudaSuccess) e = sw::configure_scored_kernels(layout->head_dim);
     if (e == cudaSuccess) e = sw::configure_evict_kernels();
+    if (e == cudaSuccess) e = sw::configure_cross_kernels(layout->head_dim);
     int per_sm = 0, window_per_sm = 0;
     if (e == cudaSuccess) e = sw::mixed_attn_resident_ctas_per_sm(layout->head_dim, &per_sm);
     if (e == cudaSuccess) e = sw::window_attn_resident_ctas_per_sm(layout->head_dim, &window_per_sm);
@@ -557,6 +559,137 @@ sw_status sw_mixed_iteration_window_run(sw_ctx* ctx, void* kv_pool, const sw_bat
     if (st != SW_OK) return st;
     if (!k_new || !v_new) return sw_fail(SW_ERR_INVALID_ARG, "sw_mixed_iteration_window_run: null tensor");
     return run_iteration(ctx, kv_pool, batch, k_new, v_new, q, out, lse, stream, "sw_mixed_iteration_window_run", w);
+}
+
+// ---- cross attention -------------------------------------------------------------------------------------------------
+sw_status sw_cross_attn_run(sw_ctx* ctx, const void* kv_pool, const sw_batch* batch, const void* q, void* out, float* lse, void* stream) {
+    const char* who = "sw_cross_attn_run";
+    Chunks ch;
+    sw_status st = check_batch(ctx, batch, who, &ch, true);
+    if (st != SW_OK) return st;
+    if (ch.rows + batch->num_decode == 0) return SW_OK;
+    if (!kv_pool || !q || !out) return sw_fail(SW_ERR_INVALID_ARG, "%s: null tensor", who);
+    st = check_current_device(ctx, who);
+    if (st != SW_OK) return st;
+    if (!aligned16(q, out)) return sw_fail(SW_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
+    const sw::KvMaps* kv_maps = nullptr;
+    st = kv_map_for(ctx, const_cast<void*>(kv_pool), &kv_maps);
+    if (st != SW_OK) return st;
+    const sw_layout& l = ctx->layout;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    // The rows of chunks without keys are written here, and the launch sees the other chunks.
+    const int64_t heads = l.num_q_heads;
+    int kept = 0;
+    for (int j = 0; j < ch.n; ++j) {
+        if (ch.P[j] == 0) {
+            SW_CUDA(sw::launch_keyless_rows(static_cast<__nv_bfloat16*>(out) + ch.row0[j] * heads * l.head_dim, ch.C[j] * heads * l.head_dim,
+                                            lse ? lse + ch.row0[j] * heads : nullptr, ch.C[j] * heads, ctx->num_sms, s));
+            continue;
+        }
+        ch.P[kept] = ch.P[j];
+        ch.C[kept] = ch.C[j];
+        ch.row0[kept] = ch.row0[j];
+        ch.page0[kept] = ch.page0[j];
+        ++kept;
+    }
+    if (kept == 0 && batch->num_decode == 0) return SW_OK;
+    sw_batch rest = *batch;
+    int64_t skipped = 0;
+    if (kept < ch.n) {   // (a launch's first chunk begins at its first row and page)
+        skipped = kept > 0 ? ch.row0[0] : 0;
+        const int pages = kept > 0 ? ch.page0[0] : 0;
+        for (int j = 0; j < kept; ++j) {
+            ch.row0[j] -= (int)skipped;
+            ch.page0[j] -= pages;
+        }
+        for (int j = kept; j < ch.n; ++j) ch.P[j] = ch.C[j] = ch.row0[j] = 0;
+        ch.n = kept;
+        ch.rows -= (int)skipped;
+        rest.prefill_pages += pages;
+        rest.num_prefill_pages -= pages;
+        for (int j = kept; j <= sw::kMaxChunks; ++j) ch.page0[j] = rest.num_prefill_pages;
+    }
+    const sw::MixedParams p = mixed_params(ctx, &rest, ch, static_cast<const __nv_bfloat16*>(q) + skipped * heads * l.head_dim,
+                                           static_cast<__nv_bfloat16*>(out) + skipped * heads * l.head_dim, lse ? lse + skipped * heads : nullptr);
+    CUtensorMap q_map = kv_maps->half, out_map = kv_maps->half;
+    st = encode_row_maps(ctx, p, &q_map, &out_map);
+    if (st != SW_OK) return st;
+    SW_CUDA(sw::launch_cross_attn(l.head_dim, *kv_maps, q_map, out_map, p, ctx->num_sms, s));
+    return SW_OK;
+}
+
+// ---- rotary positions ------------------------------------------------------------------------------------------------
+namespace {
+// Rows of `width` elements, `stride` apart.
+struct Rows {
+    const void* at;
+    int64_t stride, width;
+    const char* name;
+};
+bool rows_overlap(const Rows& a, const Rows& b, int64_t rows) {   // by their extents, as numbers
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.at), b0 = reinterpret_cast<uintptr_t>(b.at);
+    const uintptr_t a1 = a0 + (uintptr_t)((rows - 1) * a.stride + a.width) * 2, b1 = b0 + (uintptr_t)((rows - 1) * b.stride + b.width) * 2;
+    return a0 < b1 && b0 < a1;
+}
+
+// pool: the keys and values go there; null: the keys go to k_out.
+sw_status run_rope(sw_ctx* ctx, void* kv_pool, bool append, const sw_batch* batch, const sw_rope* rope, const void* q, const void* k, const void* v,
+                   void* q_out, void* k_out, void* stream, const char* who) {
+    Chunks ch;
+    sw_status st = check_batch(ctx, batch, who, &ch);
+    if (st != SW_OK) return st;
+    const sw_layout& l = ctx->layout;
+    if (!rope || !rope->turns) return sw_fail(SW_ERR_INVALID_ARG, "%s: null rope or frequencies", who);
+    if (rope->rotary_dim < 16 || rope->rotary_dim % 16 != 0 || rope->rotary_dim > l.head_dim)
+        return sw_fail(SW_ERR_UNSUPPORTED, "%s: rotary_dim %d (multiples of 16 up to the head size, %d)", who, rope->rotary_dim, l.head_dim);
+    const int64_t q_width = (int64_t)l.num_q_heads * l.head_dim, kv_width = (int64_t)l.num_kv_heads * l.head_dim;
+    const int64_t q_stride = rope->q_stride ? rope->q_stride : q_width, k_stride = rope->k_stride ? rope->k_stride : kv_width,
+                  v_stride = rope->v_stride ? rope->v_stride : kv_width;
+    if (q_stride < q_width || k_stride < kv_width || (append && v_stride < kv_width) || ((q_stride | k_stride | (append ? v_stride : 0)) & 7) != 0 ||
+        std::max(q_stride, std::max(k_stride, v_stride)) > (int64_t)1 << 40)
+        return sw_fail(SW_ERR_INVALID_ARG, "%s: strides of %lld, %lld, %lld elements (multiples of 8, a row's width at least)", who, (long long)q_stride,
+                       (long long)k_stride, (long long)v_stride);
+    const int64_t rows = ch.rows + batch->num_decode;
+    if (rows == 0) return SW_OK;
+    if (!q || !k || !q_out || (append ? !kv_pool || !v : !k_out)) return sw_fail(SW_ERR_INVALID_ARG, "%s: null tensor", who);
+    if (!aligned16(q, k, v, q_out) || !aligned16(kv_pool, k_out)) return sw_fail(SW_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
+    if ((reinterpret_cast<uintptr_t>(rope->turns) & 7) != 0) return sw_fail(SW_ERR_INVALID_ARG, "%s: frequencies must be 8-byte aligned", who);
+    // A row is read by the warps that write it, so dense rows can be rotated where they are; any other overlap would be read too late.
+    const Rows in[] = {{q, q_stride, q_width, "q"}, {k, k_stride, kv_width, "k"}, {v, v_stride, kv_width, "v"}};
+    const Rows out[] = {{q_out, q_width, q_width, "q_out"}, {k_out, kv_width, kv_width, "k_out"}};
+    for (int o = 0; o < (append ? 1 : 2); ++o)
+        for (int i = 0; i < (append ? 3 : 2); ++i)
+            if (rows_overlap(out[o], in[i], rows) && !(o == i && out[o].at == in[i].at && out[o].stride == in[i].stride))
+                return sw_fail(SW_ERR_INVALID_ARG, "%s: %s overlaps %s", who, out[o].name, in[i].name);
+    if (!append && rows_overlap(out[0], out[1], rows)) return sw_fail(SW_ERR_INVALID_ARG, "%s: q_out overlaps k_out", who);
+    st = check_current_device(ctx, who);
+    if (st != SW_OK) return st;
+    sw::RopeParams p{};
+    p.append = append_params(ctx, batch, ch, append ? kv_pool : nullptr, k, v);
+    p.Hq = l.num_q_heads;
+    p.rotary = rope->rotary_dim;
+    p.interleaved = rope->interleaved != 0;
+    p.magnitude = rope->magnitude;
+    p.turns = rope->turns;
+    p.positions = rope->positions;
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.q_stride = q_stride;
+    p.k_stride = k_stride;
+    p.v_stride = v_stride;
+    p.q_out = static_cast<__nv_bfloat16*>(q_out);
+    p.k_out = static_cast<__nv_bfloat16*>(k_out);
+    SW_CUDA(sw::launch_rope(p, l.head_dim, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+    return SW_OK;
+}
+}  // namespace
+
+sw_status sw_rope_append(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const sw_rope* rope, const void* q, const void* k_new, const void* v_new,
+                         void* q_out, void* stream) {
+    return run_rope(ctx, kv_pool, true, batch, rope, q, k_new, v_new, q_out, nullptr, stream, "sw_rope_append");
+}
+
+sw_status sw_rope_run(sw_ctx* ctx, const sw_batch* batch, const sw_rope* rope, const void* q, const void* k, void* q_out, void* k_out, void* stream) {
+    return run_rope(ctx, nullptr, false, batch, rope, q, k, nullptr, q_out, k_out, stream, "sw_rope_run");
 }
 
 // ---- the pool in 8 bits --------------------------------------------------------------------------------------------

@@ -109,6 +109,20 @@ struct AppendParams {
     int32_t* ctrl;
 };
 
+// Rotary positions.  append.k_new and v_new are the rows to rotate and to store; append.pool is null where k goes to k_out and v is not touched.
+struct RopeParams {
+    AppendParams append;
+    int Hq, rotary;
+    int interleaved;
+    int parts, part_heads;   // units that a row is cut into, heads (of q, k and v) of each: the launcher's
+    float magnitude;
+    const double* turns;         // [rotary / 2]
+    const int32_t* positions;    // [C + n], or null: from the batch
+    const __nv_bfloat16* q;
+    int64_t q_stride, k_stride, v_stride;   // elements between rows
+    __nv_bfloat16 *q_out, *k_out;
+};
+
 // Weights of a decode-only iteration's keys from its scores (scores, lse: of the attention launch before it).
 struct WeightParams {
     int n, Hkv, group, capacity;
@@ -214,6 +228,13 @@ cudaError_t launch_window_attn(int head_dim, const KvMaps& kv_maps, const CUtens
                                int num_sms, cudaStream_t stream);
 cudaError_t configure_window_kernels(int head_dim);
 cudaError_t window_attn_resident_ctas_per_sm(int head_dim, int* out);
+// cross attention (sw_cross.cu)
+cudaError_t launch_cross_attn(int head_dim, const KvMaps& kv_maps, const CUtensorMap& q_map, const CUtensorMap& out_map, const MixedParams& p,
+                              int num_sms, cudaStream_t stream);
+cudaError_t launch_keyless_rows(__nv_bfloat16* out, int64_t elements, float* lse, int64_t values, int num_sms, cudaStream_t stream);
+cudaError_t configure_cross_kernels(int head_dim);
+// rotary positions (sw_rope.cu)
+cudaError_t launch_rope(const RopeParams& p, int head_dim, int num_sms, cudaStream_t stream);
 // 8-bit pools (sw_kv8.cu)
 cudaError_t launch_kv8_append(const AppendParams& a, const int* cC, uint8_t* pool, float* scales, int num_sms, cudaStream_t stream);
 cudaError_t launch_kv8_expand(const AppendParams& a, const int* cC, const uint8_t* pool, const float* scales, __nv_bfloat16* copy, int32_t* list,

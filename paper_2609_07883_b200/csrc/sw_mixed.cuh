@@ -28,7 +28,8 @@ using namespace swptx;
 //   kKv8      the pages hold e4m3 values with a scale per (page, K|V, KV head), chunks' prompts too; where that is faster and there is room for it,
 //             the chunks read a copy of their prompts in 16 bits and their part of the kernel is the plain one (sw_kv8.cu)
 //   kScored   decode-only launches that also leave every score behind (sw_weights.cu)
-enum Option { kPlain, kWindow, kKv8, kScored };
+//   kCross    the rows of a chunk attend the keys in front of it, all of them, and not its own (sw_cross.cu); requests may have no keys
+enum Option { kPlain, kWindow, kKv8, kScored, kCross };
 
 // Pages of a decode request that hold a key its row attends, numbered without gaps: visible page j is page j of the list up to the
 // `head` pages of the sinks, and j + skip behind them.
@@ -48,6 +49,14 @@ __device__ __forceinline__ Span span_of(const MixedParams& p, int len) {
     return v;
 }
 __device__ __forceinline__ int page_of(const Span& v, int j) { return j < v.head ? j : j + v.skip; }
+
+// kCross: the row of a request without keys, by the thread that finds it while the CTAs plan.
+template <int D>
+__device__ __forceinline__ void zero_row(const MixedParams& p, int row) {
+    uint4* out = reinterpret_cast<uint4*>(p.out + (int64_t)row * p.Hq * D);
+    for (int k = 0; k < p.Hq * D / 8; ++k) out[k] = make_uint4(0, 0, 0, 0);
+    for (int h = 0; p.lse && h < p.Hq; ++h) p.lse[(int64_t)row * p.Hq + h] = -INFINITY;
+}
 
 // ---------------------------------------------------------------------------------------------------------------
 // device status: first problem wins
@@ -354,7 +363,7 @@ struct LateJoin {
 // run them, so that no warp starts a second unit.  If the early warps are nearly done by the time the late ones arrive,
 // the plan is sized for the early warps alone; if the early CTAs are few, their head start is small or there are many
 // requests per warp, it falls back to units of one size pulled by everybody.
-template <Option O>
+template <int D, Option O, bool kChunks>
 __device__ __forceinline__ Plan make_plan(const MixedParams& p, int* unit_prefix, int* len_s, int* indptr_s, int* scratch,
                                           LateJoin late, float pages_per_us) {
     Plan plan;
@@ -372,6 +381,8 @@ __device__ __forceinline__ Plan make_plan(const MixedParams& p, int* unit_prefix
         const int pg = span_of<O>(p, len).pages;
         pages_local += pg;
         long_local |= pg >= kLongPages;
+        // (with chunks, the one CTA that surely plans: the others may leave before)
+        if (O == kCross && len <= 0 && (kChunks ? (int)gridDim.x - 1 : i % (int)gridDim.x) == (int)blockIdx.x) zero_row<D>(p, p.C + i);
         len_s[i] = len;                              // the units read these from shared memory later
         indptr_s[i] = p.decode_page_indptr[i];
     }
@@ -474,6 +485,7 @@ __device__ __forceinline__ Line make_line(const MixedParams& p, int* prefix, int
         indptr_s[i] = at;
         prefix[i] = stages_of(len, listed);
         here += prefix[i];
+        if (O == kCross && len <= 0 && i % (int)gridDim.x == (int)blockIdx.x) zero_row<D>(p, p.C + i);
         if (i == p.n - 1) indptr_s[p.n] = at + listed;
         if (len > 0 && prefix[i] == 0 && blockIdx.x == 0) report(p.ctrl, SW_ERR_OUT_OF_RANGE, kSiteAttnLen, p.C + i);
     }
@@ -1595,7 +1607,7 @@ __global__ void __launch_bounds__(kThreads, 1) sw_mixed_attn_kernel(const __grid
         if (threadIdx.x == 0) atomicInc(reinterpret_cast<unsigned*>(&p.ctrl[kCtrArrived]), 2 * gridDim.x - 1);
         return;
     }
-    const Plan plan = make_plan<O>(p, unit_prefix, lens, indptr, scratch, late, p.stages_per_us);
+    const Plan plan = make_plan<D, O, tensor_prefill>(p, unit_prefix, lens, indptr, scratch, late, p.stages_per_us);
     if ((int)blockIdx.x == prefill_ctas && threadIdx.x == 0) atomicExch(p.ctrl + misc[kMiscSet] + kSetItems, plan.total_items + 1);
     if (plan.total_items > p.max_items) {
         if (threadIdx.x == 0) report_spoiled<O>(p.ctrl, SW_ERR_WORKSPACE, kSiteScratch, plan.total_items);

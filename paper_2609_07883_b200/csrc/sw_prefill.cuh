@@ -89,6 +89,12 @@ __device__ __forceinline__ int pf_chunk(const MixedParams& p, const PfShared& sh
     }
 }
 
+// Keys that some row of the chunk attends: its prefix and its own, or (kCross) the prefix alone.
+template <int D, bool kMulti, Option O>
+__device__ __forceinline__ int pf_keys(const MixedParams& p, const PfShared& sh, int chunk) {
+    return pf_chunk<D, kMulti>(p, sh, 0, chunk) + (O == kCross ? 0 : pf_chunk<D, kMulti>(p, sh, 1, chunk));
+}
+
 template <Option O>
 __device__ __forceinline__ void pf_init_barriers(uint32_t bars) {
     // arrivals: four softmax warps of a tile; kKv8: all eight, which convert V
@@ -170,9 +176,11 @@ struct PfItem {
     int pieces;      // pieces the item is cut into (several chunks: each chunk has its own count)
 };
 
+template <Option O>
 __device__ __forceinline__ int pf_tiles_of(int group, int P, int C, int tok0, int skip = 0) {
     const int tt = 128 / group;  // tokens per tile
     if (tok0 >= C) return 0;
+    if (O == kCross) return (P - 1) / 128 + 1;   // (chunks without keys have no items)
     return (P + min(tok0 + tt, C) - 1 - skip * kPageSize) / 128 + 1;
 }
 __device__ __forceinline__ int pf_num_groups(int group, int C) {
@@ -198,7 +206,7 @@ __device__ __forceinline__ int pf_steps_of_rank(const MixedParams& p, int P, int
     const int tp = n_tp - 1 - r;
     int head, skip;
     pf_passed<O>(p, P, tp * 2 * tt, head, skip);
-    return max(pf_tiles_of(p.group, P, C, (tp * 2) * tt, skip), pf_tiles_of(p.group, P, C, (tp * 2 + 1) * tt, skip));
+    return max(pf_tiles_of<O>(p.group, P, C, (tp * 2) * tt, skip), pf_tiles_of<O>(p.group, P, C, (tp * 2 + 1) * tt, skip));
 }
 // first KV tile of piece i when nk steps are cut into k pieces
 __device__ __forceinline__ int pf_piece_begin(int nk, int k, int i) { return (int)(((long long)nk * i) / k); }
@@ -531,7 +539,7 @@ __device__ __forceinline__ PfItem pf_entry(const MixedParams& p, const PfPlan& p
     pf_passed<O>(p, cP, tp * 2 * tt, it.head, it.skip);
     for (int t = 0; t < 2; ++t) {
         it.tok0[t] = (tp * 2 + t) * tt;
-        it.nkv[t] = pf_tiles_of(p.group, cP, cC, it.tok0[t], it.skip);
+        it.nkv[t] = pf_tiles_of<O>(p.group, cP, cC, it.tok0[t], it.skip);
     }
     it.nk = max(it.nkv[0], it.nkv[1]);
     if (entry < plan.n_whole) {
@@ -570,7 +578,7 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
         }
         return false;
     }
-    const int npages = (pf_chunk<D, kMulti>(p, sh, 0, it.chunk) + pf_chunk<D, kMulti>(p, sh, 1, it.chunk) + kPageSize - 1) / kPageSize;
+    const int npages = (pf_keys<D, kMulti, O>(p, sh, it.chunk) + kPageSize - 1) / kPageSize;
     auto id_of = [&](int step) {
         int page = step * 8 + lane;
         if (O == kWindow && page >= it.head) page += it.skip;
@@ -641,13 +649,13 @@ __device__ __forceinline__ bool pf_produce(const CUtensorMap* kv_map, const CUte
 }
 
 // ---- role: V sanitizer (one warp) -------------------------------------------------------------------------------
-// Keys at or past P + C are never attended, but their V rows still enter the P V product with weight zero; zero them
+// Keys at or past P + C (kCross: P) are never attended, but their V rows still enter the P V product with weight zero; zero them
 // so that whatever an unwritten page slot (or a stale buffer) holds cannot turn 0 * x into NaN.
 template <int D, bool kMulti, Option O>
 __device__ __forceinline__ bool pf_sanitize(const MixedParams& p, const PfShared& sh, const PfItem& it, uint32_t& kv_it) {
     using G = PfGeo<D>;
     const int lane = threadIdx.x & 31;
-    const int kv_total = pf_chunk<D, kMulti>(p, sh, 0, it.chunk) + pf_chunk<D, kMulti>(p, sh, 1, it.chunk);
+    const int kv_total = pf_keys<D, kMulti, O>(p, sh, it.chunk);
     for (int j = it.j0; j < it.j1; ++j, ++kv_it) {
         const uint32_t s = kv_it & 1, n = kv_it >> 1;
         if (!pf_wait(sh, kBarVLanded + s, n & 1, p.ctrl, 3)) return false;
@@ -1048,7 +1056,7 @@ __device__ __forceinline__ bool pf_softmax(const CUtensorMap* out_map, const Mix
     if (j_end <= it.j0) return true;  // this tile has no step in this piece
     const int tok = it.tok0[t] + row / p.group;
     const int head = it.kvh * p.group + row % p.group;
-    const int pos = pf_chunk<D, kMulti>(p, sh, 0, it.chunk) + tok;
+    const int pos = pf_chunk<D, kMulti>(p, sh, 0, it.chunk) + (O == kCross ? -1 : tok);   // the last key that the row attends
     const uint32_t lane_addr = sh.tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t s_addr = lane_addr + t * 128;
     const uint32_t p_addr = lane_addr + G::kPColumn + t * G::kPStride;
