@@ -271,6 +271,33 @@ sw_status sw_rope_run(sw_ctx* ctx, const sw_batch* batch, const sw_rope* rope, c
  * (keys) first.  One launch, and one more for each chunk without keys.  Asynchronous. */
 sw_status sw_cross_attn_run(sw_ctx* ctx, const void* kv_pool, const sw_batch* batch, const void* q, void* out, float* lse, void* stream);
 
+/* The next tokens: one draw a row from device logits [rows][vocab], row_stride elements apart.  Arrays are device memory, one value per row;
+ * all but uniform may be NULL (temperature 1, nothing cut off).
+ *   The weight of logit x is exp((x - largest) / temperature), rounded to 2^-44 of the largest one's.  Minus infinity and NaN have none; of rows with
+ *   plus infinity, the infinite ones have equal weights and no other has any.
+ *   temperature 0 (or less, or NaN): the token is the largest logit, and the rest is not looked at.
+ *   Of the logits in falling order, equal ones by their index, top_k (0 or less: off) keeps the first k; of the total weight of these, top_p (1 or more,
+ *   or NaN: off) keeps those in front of which less than that share lies, the first one always; min_p (0 or less, or NaN: off) keeps those whose weight is at
+ *   least that share of the largest.
+ *   tokens[r] is the first index up to which the kept weights sum to more than uniform[r] (in [0, 1); others count as the nearest such) times their total;
+ *   log_probs[r] (NULL: not asked for) the logarithm of its share of that total, 0 at temperature 0.
+ * A row without any weight gets token -1 and minus infinity.  Sums are exact: the result depends on no order, and is the same in every batch.
+ * vocab: at most 393216.  One launch, asynchronous; it uses nothing of the context but its device, so calls on several streams may overlap. */
+typedef enum { SW_DTYPE_F32 = 0, SW_DTYPE_BF16 = 1, SW_DTYPE_F16 = 2 } sw_dtype;
+#define SW_SAMPLE_MAX_ROWS 65536
+typedef struct {
+    const void* logits;
+    int32_t dtype; /* sw_dtype */
+    int32_t rows, vocab;
+    int64_t row_stride;
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    const float* uniform;
+} sw_sampling;
+sw_status sw_sample_run(sw_ctx* ctx, const sw_sampling* sampling, int32_t* tokens, float* log_probs, void* stream);
+
 /* Profiler step (Sec. 5.1; Sec. 6.4): time the attention of one iteration over a stack of `layers` pools
  * (kv_pools: HOST array of `layers` device pool pointers, used round-robin so that successive launches do
  * not hit the same cache lines).  Runs `warmup` untimed and `reps` timed iterations of `layers` launches

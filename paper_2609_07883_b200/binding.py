@@ -72,6 +72,11 @@ class sw_rope(C.Structure):
                 ("positions", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
 
 
+class sw_sampling(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("dtype", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32), ("row_stride", C.c_int64),
+                ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("uniform", C.c_void_p)]
+
+
 EXPORTS = ["sw_workspace_bytes", "sw_create", "sw_destroy", "sw_kv_append", "sw_mixed_attn_run", "sw_mixed_iteration_run",
            "sw_mixed_iteration_host", "sw_cost_probe", "sw_cost_probe_iteration", "sw_check_status", "sw_cost_table_create",
            "sw_cost_table_destroy", "sw_cost_table_lookup", "sw_choose_chunk", "sw_choose_chunks", "sw_last_error",
@@ -79,7 +84,7 @@ EXPORTS = ["sw_workspace_bytes", "sw_create", "sw_destroy", "sw_kv_append", "sw_
            "sw_telemetry_record", "sw_telemetry_margin", "sw_telemetry_exceeds", "sw_telemetry_get_totals",
            "sw_telemetry_reset", "sw_mixed_attn_window_run", "sw_mixed_iteration_window_run", "sw_kv8_scratch_bytes", "sw_kv8_append",
            "sw_kv8_attn_run", "sw_attn_weights_scratch_bytes", "sw_decode_attn_weights_run", "sw_kv_evict", "sw_rope_frequencies",
-           "sw_rope_append", "sw_rope_run", "sw_cross_attn_run"]
+           "sw_rope_append", "sw_rope_run", "sw_cross_attn_run", "sw_sample_run"]
 
 _vp, _i32, _i64 = C.c_void_p, C.c_int32, C.c_int64
 _lib.sw_workspace_bytes.restype = C.c_size_t
@@ -105,6 +110,7 @@ _lib.sw_rope_frequencies.argtypes = [_i32, C.c_double, _i32, C.c_double, C.c_dou
 _lib.sw_rope_append.argtypes = [_vp, _vp, C.POINTER(sw_batch), C.POINTER(sw_rope), _vp, _vp, _vp, _vp, _vp]
 _lib.sw_rope_run.argtypes = [_vp, C.POINTER(sw_batch), C.POINTER(sw_rope), _vp, _vp, _vp, _vp, _vp]
 _lib.sw_cross_attn_run.argtypes = [_vp, _vp, C.POINTER(sw_batch), _vp, _vp, _vp, _vp]
+_lib.sw_sample_run.argtypes = [_vp, C.POINTER(sw_sampling), _vp, _vp, _vp]
 _lib.sw_cost_probe.argtypes = [_vp, C.POINTER(_vp), _i32, C.POINTER(sw_batch), _vp, _vp, _i32, _i32,
                                C.POINTER(_i64), C.POINTER(_i64), C.POINTER(_i64), _vp]
 _lib.sw_cost_probe_iteration.argtypes = [_vp, C.POINTER(_vp), _i32, C.POINTER(sw_batch), _vp, _vp, _vp, _vp, _i32, _i32,
@@ -409,6 +415,24 @@ def sw_cross_attn_run(ctx: Context, kv_pool, batch: DeviceBatch, q, out, lse=Non
     """As ``sw_mixed_attn_run``, but the rows of a chunk attend the ``prefix_len`` keys of its page list, all of them; no keys: zeros."""
     _check(_lib.sw_cross_attn_run(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), _ptr(q), _ptr(out), _ptr(lse), _stream_handle(stream)),
            "sw_cross_attn_run")
+
+
+def sw_sample_run(ctx: Context, logits, uniform, tokens, log_probs=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None) -> None:
+    """One token a row of ``logits`` (fp32, bf16 or f16 [rows][vocab]) by the row's ``uniform`` number; settings are tensors of one value a row."""
+    import torch
+
+    dtype = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(logits.dtype)
+    if dtype is None or logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise ValueError("logits must be an fp32, bf16 or f16 tensor [rows][vocab] with the logits of a row side by side")
+    rows, vocab = logits.shape
+    f32, i32 = torch.float32, torch.int32
+    for name, t, kind in (("uniform", uniform, f32), ("tokens", tokens, i32), ("log_probs", log_probs, f32), ("temperature", temperature, f32),
+                          ("top_k", top_k, i32), ("top_p", top_p, f32), ("min_p", min_p, f32)):
+        if t is not None and (t.dtype != kind or t.dim() != 1 or t.shape[0] < rows or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {kind} tensor of one value per row")
+    s = sw_sampling(logits.data_ptr(), dtype, rows, vocab, logits.stride(0) if rows > 1 else vocab, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                    _ptr(uniform))
+    _check(_lib.sw_sample_run(ctx.handle, C.byref(s), _ptr(tokens), _ptr(log_probs), _stream_handle(stream)), "sw_sample_run")
 
 
 def sw_cost_probe_iteration(ctx: Context, kv_pools, batch: DeviceBatch, k_new, v_new, q, out, warmup: int = 3,

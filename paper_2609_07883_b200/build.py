@@ -17,7 +17,7 @@ LIB = HERE / "libsloweave.so"
 LIB_SANITIZED = HERE / "libsloweave_asan.so"
 HOST_SOURCES = ["sw_error.cpp", "sw_controller.cpp", "sw_telemetry.cpp", "sw_rope_frequencies.cpp"]
 DEVICE_SOURCES = ["sw_api.cu", "sw_kernels.cu", "sw_static.cu", "sw_window.cu", "sw_kv8.cu", "sw_weights.cu", "sw_evict.cu",
-                  "sw_cross.cu", "sw_rope.cu"]
+                  "sw_cross.cu", "sw_rope.cu", "sw_sample.cu"]
 SOURCES = HOST_SOURCES + DEVICE_SOURCES
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 SANITIZE = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer", "-g", "-O1"]

@@ -325,6 +325,7 @@ sw_status sw_create(const sw_layout* layout, int device, void* workspace, size_t
     if (e == cudaSuccess) e = sw::configure_scored_kernels(layout->head_dim);
     if (e == cudaSuccess) e = sw::configure_evict_kernels();
     if (e == cudaSuccess) e = sw::configure_cross_kernels(layout->head_dim);
+    if (e == cudaSuccess) e = sw::configure_sample_kernels();
     int per_sm = 0, window_per_sm = 0;
     if (e == cudaSuccess) e = sw::mixed_attn_resident_ctas_per_sm(layout->head_dim, &per_sm);
     if (e == cudaSuccess) e = sw::window_attn_resident_ctas_per_sm(layout->head_dim, &window_per_sm);
@@ -690,6 +691,38 @@ sw_status sw_rope_append(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, cons
 
 sw_status sw_rope_run(sw_ctx* ctx, const sw_batch* batch, const sw_rope* rope, const void* q, const void* k, void* q_out, void* k_out, void* stream) {
     return run_rope(ctx, nullptr, false, batch, rope, q, k, nullptr, q_out, k_out, stream, "sw_rope_run");
+}
+
+// ---- sampling ----------------------------------------------------------------------------------------------------------
+sw_status sw_sample_run(sw_ctx* ctx, const sw_sampling* sampling, int32_t* tokens, float* log_probs, void* stream) {
+    const char* who = "sw_sample_run";
+    if (!ctx || !sampling) return sw_fail(SW_ERR_INVALID_ARG, "%s: null context or sampling", who);
+    const sw_sampling& a = *sampling;
+    if (a.dtype != SW_DTYPE_F32 && a.dtype != SW_DTYPE_BF16 && a.dtype != SW_DTYPE_F16) return sw_fail(SW_ERR_UNSUPPORTED, "%s: dtype %d", who, a.dtype);
+    if (a.rows < 0 || a.vocab < 1 || a.row_stride < a.vocab)
+        return sw_fail(SW_ERR_INVALID_ARG, "%s: %d rows of %d logits, %lld apart", who, a.rows, a.vocab, (long long)a.row_stride);
+    if (a.vocab > sw::kMaxVocab || a.rows > SW_SAMPLE_MAX_ROWS)
+        return sw_fail(SW_ERR_UNSUPPORTED, "%s: %d rows of %d logits (at most %d of %d)", who, a.rows, a.vocab, SW_SAMPLE_MAX_ROWS, sw::kMaxVocab);
+    if (a.rows == 0) return SW_OK;
+    if (!a.logits || !a.uniform || !tokens) return sw_fail(SW_ERR_INVALID_ARG, "%s: null tensor", who);
+    if (reinterpret_cast<uintptr_t>(a.logits) % (a.dtype == SW_DTYPE_F32 ? 4 : 2) != 0)
+        return sw_fail(SW_ERR_INVALID_ARG, "%s: logits must be aligned to their size", who);
+    const sw_status st = check_current_device(ctx, who);
+    if (st != SW_OK) return st;
+    sw::SampleParams p{};
+    p.logits = a.logits;
+    p.rows = a.rows;
+    p.vocab = a.vocab;
+    p.row_stride = a.row_stride;
+    p.temperature = a.temperature;
+    p.top_k = a.top_k;
+    p.top_p = a.top_p;
+    p.min_p = a.min_p;
+    p.uniform = a.uniform;
+    p.tokens = tokens;
+    p.log_probs = log_probs;
+    SW_CUDA(sw::launch_sample(p, a.dtype, ctx->num_sms, static_cast<cudaStream_t>(stream)));
+    return SW_OK;
 }
 
 // ---- the pool in 8 bits --------------------------------------------------------------------------------------------

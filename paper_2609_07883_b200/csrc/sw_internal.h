@@ -19,6 +19,7 @@ constexpr int kMaxGroup = 8;            // query heads per KV head
 constexpr int kMaxCtas = 192;           // persistent CTAs (one per SM) the scratch is sized for
 constexpr int kPfRoundSlots = 3 * kMaxCtas;  // partial results of chunk-prefill pieces that run in several rounds
 constexpr int kMaxChunks = 8;           // prefill chunks (of different prompts) in one iteration
+constexpr int kMaxVocab = 393216;       // logits of a row that a token is drawn from: eight CTAs' shared memory
 constexpr int kMaxChunk = 65536;        // chunk tokens per iteration (256-row groups are planned in shared memory)
 
 constexpr long long kLineWaitCycles = 2000000000LL;   // limit of a wait in the line of decode stages (about a second)
@@ -121,6 +122,18 @@ struct RopeParams {
     const __nv_bfloat16* q;
     int64_t q_stride, k_stride, v_stride;   // elements between rows
     __nv_bfloat16 *q_out, *k_out;
+};
+
+// One token a row from logits.  Every array but logits, uniform and tokens may be null.
+struct SampleParams {
+    const void* logits;   // [rows], row_stride elements apart
+    int rows, vocab;
+    int stretch;          // logits of a CTA: the launcher's
+    int64_t row_stride;
+    const float *temperature, *top_p, *min_p, *uniform;
+    const int32_t* top_k;
+    int32_t* tokens;
+    float* log_probs;
 };
 
 // Weights of a decode-only iteration's keys from its scores (scores, lse: of the attention launch before it).
@@ -235,6 +248,9 @@ cudaError_t launch_keyless_rows(__nv_bfloat16* out, int64_t elements, float* lse
 cudaError_t configure_cross_kernels(int head_dim);
 // rotary positions (sw_rope.cu)
 cudaError_t launch_rope(const RopeParams& p, int head_dim, int num_sms, cudaStream_t stream);
+// sampling (sw_sample.cu)
+cudaError_t launch_sample(const SampleParams& p, int dtype, int num_sms, cudaStream_t stream);
+cudaError_t configure_sample_kernels();
 // 8-bit pools (sw_kv8.cu)
 cudaError_t launch_kv8_append(const AppendParams& a, const int* cC, uint8_t* pool, float* scales, int num_sms, cudaStream_t stream);
 cudaError_t launch_kv8_expand(const AppendParams& a, const int* cC, const uint8_t* pool, const float* scales, __nv_bfloat16* copy, int32_t* list,

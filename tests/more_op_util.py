@@ -10,6 +10,7 @@ Tolerances are sums of the roundings that a result goes through, taken at their 
 from __future__ import annotations
 
 import math
+from fractions import Fraction
 
 import numpy as np
 import torch
@@ -102,3 +103,36 @@ def rotate(x, pos, turns, interleaved, magnitude):
     for part in (a, b):
         tol[..., part] = 2.0 ** -8 * y[..., part].abs() + (2.0 ** -21 + slack) * (xa.abs() + xb.abs()) * abs(magnitude)
     return y, tol
+
+
+# ---- sampling --------------------------------------------------------------------------------------------------------------------
+UNIT = 2.0 ** 44
+
+
+def draw(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """Token, log-probability and the kept indices of one row; x float64 (numpy).  Weights are whole units, as the header says, so sums are exact."""
+    x = np.where(np.isnan(x), -np.inf, x)
+    top = x.max()
+    if top == -np.inf:
+        return -1, -math.inf, np.zeros(0, dtype=np.int64)
+    best = int(np.argmax(x))
+    if not temperature > 0:
+        return best, 0.0, np.array([best])
+    with np.errstate(invalid="ignore", over="ignore", under="ignore"):
+        w = np.where(x == top, 1.0, np.where(x == -np.inf, 0.0, np.exp((x - top) / temperature) if top < np.inf else 0.0))
+    w = np.rint(w * UNIT).astype(np.int64)
+    order = np.argsort(-x, kind="stable")
+    live = x[order] > -np.inf
+    order = order[live]
+    if 0 < top_k < len(x):
+        order = order[:top_k]
+    if top_p < 1:
+        sums = np.cumsum(w[order])
+        order = order[: 1 + int(np.sum(sums[:-1] < math.ceil(Fraction(max(top_p, 0.0)) * int(sums[-1]))))]
+    if min_p > 0:
+        order = order[w[order] >= min(min_p, 1.0) * UNIT]
+    kept = np.sort(order)
+    sums = np.cumsum(w[kept])
+    drawn = min(math.floor(Fraction(min(max(u, 0.0), 1.0)) * int(sums[-1])) if u == u else 0, int(sums[-1]) - 1)
+    at = int(np.searchsorted(sums, drawn, side="right"))
+    return int(kept[at]), math.log(int(w[kept[at]]) / int(sums[-1])), kept

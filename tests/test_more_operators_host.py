@@ -80,6 +80,7 @@ def test_frequencies_null_and_unknown():
     lambda: B._lib.sw_rope_append(None, None, None, None, None, None, None, None, None),
     lambda: B._lib.sw_rope_run(None, None, None, None, None, None, None, None),
     lambda: B._lib.sw_cross_attn_run(None, None, None, None, None, None, None),
+    lambda: B._lib.sw_sample_run(None, None, None, None, None),
 ])
 def test_null_context(call):
     assert call() == B.SW_ERR_INVALID_ARG
