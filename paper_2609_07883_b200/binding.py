@@ -217,6 +217,7 @@ class DeviceBatch:
         import torch
 
         self.host = batch
+        self.rows = batch.num_rows
         to = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(device)
         self.prefill_pages = to(batch.prefill_pages)
         self.decode_kv_len = to(batch.decode_kv_len)
@@ -370,31 +371,40 @@ class Rope:
             raise ValueError("positions must be a contiguous int32 tensor")
         self.turns = turns.to("cuda" if device is None else device).contiguous()
         self.interleaved, self.magnitude, self.positions = bool(interleaved), float(magnitude), positions
+        self.num_positions = None if positions is None else positions.numel()
+        self._structs = {}
 
-    def struct(self, rows: int, q, k, v=None) -> sw_rope:
-        if self.positions is not None and self.positions.numel() < rows:
-            raise ValueError(f"positions names {self.positions.numel()} rows, the batch has {rows}")
-        return sw_rope(self.turns.data_ptr(), 2 * self.turns.numel(), int(self.interleaved), self.magnitude, _ptr(self.positions), q.stride(0), k.stride(0),
-                       0 if v is None else v.stride(0))
+    def struct(self, rows: int, strides) -> sw_rope:
+        if self.num_positions is not None and self.num_positions < rows:
+            raise ValueError(f"positions names {self.num_positions} rows, the batch has {rows}")
+        s = self._structs.get(strides)
+        if s is None:
+            s = self._structs[strides] = sw_rope(self.turns.data_ptr(), 2 * self.turns.numel(), int(self.interleaved), self.magnitude,
+                                                 _ptr(self.positions), *strides)
+        return s
 
 
-def _check_rows(name: str, t, rows: int, heads: int, head_dim: int, dense: bool) -> None:
+def _row_stride(name: str, t, rows: int, heads: int, head_dim: int, bf16, dense: bool = False) -> int:
     # what the library cannot see from a pointer
-    import torch
-
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[0] < rows or tuple(t.shape[1:]) != (heads, head_dim):
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not bf16 or len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != head_dim:
         raise ValueError(f"{name} must be bf16 [{rows}][{heads}][{head_dim}]")
-    if t.stride(2) != 1 or t.stride(1) != head_dim or (dense and t.stride(0) != heads * head_dim):
+    width = heads * head_dim
+    if stride[2] != 1 or (stride[1] != head_dim and heads > 1) or (dense and stride[0] != width and rows > 1):
         raise ValueError(f"{name}: {'rows' if dense else 'heads of a row'} must lie side by side")
+    return stride[0] if rows > 1 else width
 
 
 def _rope_rows(ctx: Context, batch: DeviceBatch, rope: Rope, q, k, v, q_out, k_out) -> sw_rope:
-    sh, rows = ctx.shape, batch.host.num_rows
-    for name, t, heads, dense in (("q", q, sh.num_q_heads, False), ("k", k, sh.num_kv_heads, False), ("v", v, sh.num_kv_heads, False),
-                                  ("q_out", q_out, sh.num_q_heads, True), ("k_out", k_out, sh.num_kv_heads, True)):
-        if t is not None:
-            _check_rows(name, t, rows, heads, sh.head_dim, dense)
-    return rope.struct(rows, q, k, v)
+    import torch
+
+    sh, rows, bf16 = ctx.shape, batch.rows, torch.bfloat16
+    hq, hkv, d = sh.num_q_heads, sh.num_kv_heads, sh.head_dim
+    strides = (_row_stride("q", q, rows, hq, d, bf16), _row_stride("k", k, rows, hkv, d, bf16), 0 if v is None else _row_stride("v", v, rows, hkv, d, bf16))
+    _row_stride("q_out", q_out, rows, hq, d, bf16, True)
+    if k_out is not None:
+        _row_stride("k_out", k_out, rows, hkv, d, bf16, True)
+    return rope.struct(rows, strides)
 
 
 def sw_rope_append(ctx: Context, kv_pool, batch: DeviceBatch, rope: Rope, q, k_new, v_new, q_out, stream=None) -> None:
@@ -426,10 +436,9 @@ def sw_sample_run(ctx: Context, logits, uniform, tokens, log_probs=None, tempera
         raise ValueError("logits must be an fp32, bf16 or f16 tensor [rows][vocab] with the logits of a row side by side")
     rows, vocab = logits.shape
     f32, i32 = torch.float32, torch.int32
-    for name, t, kind in (("uniform", uniform, f32), ("tokens", tokens, i32), ("log_probs", log_probs, f32), ("temperature", temperature, f32),
-                          ("top_k", top_k, i32), ("top_p", top_p, f32), ("min_p", min_p, f32)):
-        if t is not None and (t.dtype != kind or t.dim() != 1 or t.shape[0] < rows or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous {kind} tensor of one value per row")
+    for t, kind in ((uniform, f32), (tokens, i32), (log_probs, f32), (temperature, f32), (top_k, i32), (top_p, f32), (min_p, f32)):
+        if t is not None and (t.dtype is not kind or t.numel() < rows or not t.is_contiguous()):
+            raise ValueError("uniform, log_probs, temperature, top_p, min_p (fp32), tokens and top_k (int32) must be contiguous, one value per row")
     s = sw_sampling(logits.data_ptr(), dtype, rows, vocab, logits.stride(0) if rows > 1 else vocab, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
                     _ptr(uniform))
     _check(_lib.sw_sample_run(ctx.handle, C.byref(s), _ptr(tokens), _ptr(log_probs), _stream_handle(stream)), "sw_sample_run")

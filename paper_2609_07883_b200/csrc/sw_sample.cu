@@ -8,13 +8,17 @@
 // Weights are worked out in 64 bits (2^x from a table of 32 powers and a polynomial of degree four, 8e-14 off) and rounded to 2^-44 of the
 // largest; their sums are integers, exact in any order, and equal logits have equal weights.
 //
-// A cluster of 1 to 8 CTAs has a row; each CTA keeps an equal stretch in shared memory as fp32, so logits are read from memory once.  Then
-//   - the row's largest logit, and a cut below which most logits lie: a quantile of the threads' largest ones (its median over warps and CTAs).  It
-//     only has to be about right;
-//   - top-k, top-p: the threshold by radix, 256 bins a pass with their number of logits and weight, over the logits above the cut; the CTAs read
-//     one another's bins.  Where the threshold lies lower, 256 bins of equal width over the rest come first;
-//   - the sums of the kept weights of every warp's run of logits; the CTA and the warp that the draw falls into look for the token.
-// Bound by the logits' bytes, and by 64-bit arithmetic where all weights are needed (nine operations a logit).
+// A cluster of 1 to 8 CTAs has a row; each CTA copies an equal stretch to shared memory, so logits are read from memory once.  Then
+//   - the row's largest logit, and a cut above which some hundreds of logits lie: a quantile of the threads' largest ones (its median over warps and
+//     CTAs).  It only has to be about right;
+//   - without top-k and top-p, the sums of the weights of every warp's run of logits; the warp that the draw falls into looks for the token;
+//   - with them, the logits above the cut are collected in one CTA (another one for the next row; top-p: and all weights summed).  If the threshold lies among
+//     them, that CTA has the rest to itself: it keeps them in registers, finds the threshold by radix, 256 bins a pass with their number of logits and
+//     weight, and the token likewise, by index.  The others end;
+//   - if it does not (a large k, or weights spread over thousands of tokens), all CTAs search their stretches, and read one another's bins: first those
+//     above the cut, then 256 bins of equal width over the rest, then the bin that the threshold lies in.
+// Bound by the logits' bytes, by the instructions of a weight where all are needed (19 a logit, nine of them in 64 bits), and for a few rows by the
+// chain of two cluster barriers and the passes.
 #include <cfloat>
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
@@ -24,29 +28,38 @@
 namespace sw {
 namespace cg = cooperative_groups;
 
-constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kSampleBins = 256, kSampleRanks = 8;
+constexpr int kSampleThreads = 256, kSampleWarps = kSampleThreads / 32, kSampleBins = 256, kSampleRanks = 8;
+constexpr int kSampleCtasPerSm = 3;
 constexpr int kBlock = 128;   // logits that a warp takes at once
-constexpr uint32_t kLowestKey = 0x00800000u;   // ordered() of the lowest finite number
+constexpr int kListed = 144, kHeld = (kListed * kSampleRanks + kSampleThreads - 1) / kSampleThreads;   // collected from a CTA; by a thread of the collecting one
+constexpr uint32_t kLowestKey = 0x00800000u;   // key_of() of the lowest finite number
 constexpr int kUnitBits = 44;                  // the largest weight is 2^44 units: sums of up to 2^19 of them fit 63 bits
+static_assert(kSampleThreads == kSampleBins, "a thread per bin");
 
 struct SampleShared {
-    uint32_t count[2][kSampleBins], low[2][kSampleBins], high[2][kSampleBins];   // by the parity of the pass: logits, and units in two halves
-    uint64_t weight[kSampleBins];                                                // summed over the cluster
-    uint32_t number[kSampleBins], before[kSampleBins];                           // likewise; of the CTAs before this one
-    double power[32];                                                            // 2^(j / 32)
-    uint64_t rank_total[kSampleRanks], rank_kept[kSampleRanks], warp_sum[kSampleWarps];
+    union {
+        uint2 listed[kSampleRanks][kListed];   // the collecting CTA: logits above the cut, as bits, and their indices
+        struct {
+            uint32_t count[2][kSampleBins], low[2][kSampleBins], high[2][kSampleBins];   // by the parity of the pass: logits, and units in two halves
+            uint64_t weight[kSampleBins];                                                // summed over the cluster
+            uint32_t number[kSampleBins];                                                // likewise
+        } bins;
+    };
+    uint2 mine[kListed];
+    double power[32];   // 2^(44 + j / 32)
+    uint64_t rank_total[kSampleRanks], rank_above[kSampleRanks], rank_kept[kSampleRanks], warp_sum[kSampleWarps];
     float rank_top[kSampleRanks], rank_cut[kSampleRanks], warp_top[kSampleWarps], warp_cut[kSampleWarps];
-    uint32_t rank_first[kSampleRanks], warp_word[kSampleWarps];
-    struct {
-        uint64_t above_w, w;
-        uint32_t above_n, n, before;
-        int bin;
+    uint32_t rank_listed[kSampleRanks], warp_word[kSampleWarps];
+    struct Found {
+        uint64_t above_w, w;   // units of what lies above the bin, and in it
+        uint32_t above_n, n;
+        int bin;               // -1: the target is not reached
     } found;
-    uint32_t edge[2];
-    alignas(16) float x[];
+    uint32_t edge[2], num_mine;
+    alignas(16) unsigned char x[];
 };
 
-// Floats as integers of the same order (no NaN gets here); -0 as 0.
+// Floats as integers of the same order; -0 as 0.  (Of a NaN it may be anything: comparisons of the floats come first.)
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
@@ -58,16 +71,17 @@ struct Weigh {
     double c, mc;        // 32 / ln 2 / temperature, and times the largest logit
     float floor;         // weights below 2^-64 are none
     const double* power;
-    __device__ __forceinline__ uint64_t operator()(float x) const {
-        const double magic = 6755399441055744.0;   // 1.5 2^52: a sum with it is rounded to an integer, which its low word holds
-        const double t = fma((double)fmaxf(x, floor), c, -mc), r = t + magic, f = t - (r - magic);
+    static constexpr uint64_t kZero = 0x4330000000000000ull;   // bits of 2^52: a sum with it is rounded to an integer, which its low bits hold
+    __device__ __forceinline__ uint64_t bits(float x) const {  // kZero + units
+        const double magic = 6755399441055744.0;   // 1.5 2^52: likewise, of either sign
+        const double t = fma((double)fmaxf(x, floor), c, -mc), r = t + magic, f = t - (r - magic);   // (NaN: the floor)
         const int n = __double2loint(r);
         const double q = fma(fma(fma(fma(9.172517872816247e-09, f, 1.6938633901956802e-06), f, 0.00023459619822185958), f, 0.021660849391722196), f,
                              0.9999999999999993);   // 2^(f / 32), |f| <= 1/2
         const double s = power[n & 31];
-        const double scale = __hiloint2double(__double2hiint(s) + ((n >> 5) + kUnitBits) * 0x100000, __double2loint(s));
-        return (uint64_t)__double_as_longlong(fma(q, scale, 4503599627370496.0)) - 0x4330000000000000ull;   // (2^52 likewise)
+        return (uint64_t)__double_as_longlong(fma(q, __hiloint2double(__double2hiint(s) + (n & ~31) * 0x8000, __double2loint(s)), 4503599627370496.0));
     }
+    __device__ __forceinline__ uint64_t operator()(float x) const { return bits(x) - kZero; }
 };
 
 // share * total, rounded down or up from the exact product (a share of 24 bits times 63); share in [0, 1).
@@ -101,50 +115,38 @@ __device__ __forceinline__ uint64_t warp_scan_u64(uint64_t v, int lane) {   // i
     }
     return v;
 }
-// the value that `half` of the first n lanes' values lie above
-__device__ __forceinline__ float lanes_median(float v, int n, int lane) {
+// the value of one of the first n lanes that `rank` of theirs lie above
+__device__ __forceinline__ float lanes_rank(float v, int n, int rank, int lane) {
     int above = 0;
     for (int j = 0; j < n; ++j) {
         const float o = __shfl_sync(0xffffffffu, v, j);
         above += o > v || (o == v && j < lane);
     }
-    const unsigned at = __ballot_sync(0xffffffffu, lane < n && above == n / 2);
+    const unsigned at = __ballot_sync(0xffffffffu, lane < n && above == rank);
     return __shfl_sync(0xffffffffu, v, __ffs(at) - 1);
 }
 
-template <class T>
-struct Vec;   // 16 bytes of logits as fp32
-template <>
-struct Vec<float> {
-    static constexpr int kN = 4;
-    static __device__ __forceinline__ void widen(uint4 v, float (&f)[4]) {
-        f[0] = __uint_as_float(v.x), f[1] = __uint_as_float(v.y), f[2] = __uint_as_float(v.z), f[3] = __uint_as_float(v.w);
-    }
-    static __device__ __forceinline__ float one(float x) { return x; }
-};
-template <>
-struct Vec<__nv_bfloat16> {
-    static constexpr int kN = 8;
-    static __device__ __forceinline__ void widen(uint4 v, float (&f)[8]) {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[2 * i] = __uint_as_float(w[i] << 16), f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-    static __device__ __forceinline__ float one(__nv_bfloat16 x) { return __bfloat162float(x); }
-};
-template <>
-struct Vec<__half> {
-    static constexpr int kN = 8;
-    static __device__ __forceinline__ void widen(uint4 v, float (&f)[8]) {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-            f[2 * i] = h.x, f[2 * i + 1] = h.y;
-        }
-    }
-    static __device__ __forceinline__ float one(__half x) { return __half2float(x); }
-};
+// Four neighbouring logits in shared memory as fp32.
+__device__ __forceinline__ void quad_of(const float* x, float (&v)[4]) {
+    const float4 q = *reinterpret_cast<const float4*>(x);
+    v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+}
+__device__ __forceinline__ void quad_of(const __nv_bfloat16* x, float (&v)[4]) {
+    const uint2 q = *reinterpret_cast<const uint2*>(x);
+    v[0] = __uint_as_float(q.x << 16), v[1] = __uint_as_float(q.x & 0xffff0000u), v[2] = __uint_as_float(q.y << 16), v[3] = __uint_as_float(q.y & 0xffff0000u);
+}
+__device__ __forceinline__ void quad_of(const __half* x, float (&v)[4]) {
+    const uint2 q = *reinterpret_cast<const uint2*>(x);
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&q.x)), b = __half22float2(*reinterpret_cast<const __half2*>(&q.y));
+    v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+}
+__device__ __forceinline__ float max4(const float (&v)[4]) { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])); }   // (NaN does not count)
+__device__ __forceinline__ void store_logit(float* x, float v) { *x = v; }
+__device__ __forceinline__ void store_logit(__nv_bfloat16* x, float v) { *x = __float2bfloat16(v); }
+__device__ __forceinline__ void store_logit(__half* x, float v) { *x = __float2half(v); }
+__device__ __forceinline__ float load_logit(const float* x) { return *x; }
+__device__ __forceinline__ float load_logit(const __nv_bfloat16* x) { return __bfloat162float(*x); }
+__device__ __forceinline__ float load_logit(const __half* x) { return __half2float(*x); }
 
 // Logits whose keys lie in [lo, hi], in 256 bins: of 2^shift keys each, or (linear) of equal width from x_lo on.
 struct Interval {
@@ -161,15 +163,52 @@ struct Interval {
     }
 };
 
+// The bin in which what lies above it, from above_n logits and above_w units on, reaches the target.  One warp; number(i) and weight(i) of bin i.
+template <class N, class W>
+__device__ __forceinline__ SampleShared::Found pick_bin(N number, W weight, uint64_t above_n, uint64_t above_w, bool by_weight, uint64_t target, int lane) {
+    // lane l has bins 255 - 8 l down to 248 - 8 l
+    uint64_t n = 0, w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        n += number(kSampleBins - 1 - lane * 8 - i);
+        w += weight(kSampleBins - 1 - lane * 8 - i);
+    }
+    const uint64_t n_to = above_n + warp_scan_u64(n, lane), w_to = above_w + warp_scan_u64(w, lane);
+    const unsigned reached = __ballot_sync(0xffffffffu, (by_weight ? w_to : n_to) >= target);
+    n = n_to - n;
+    w = w_to - w;
+    SampleShared::Found f;
+    f.bin = -1;
+    f.n = 0;
+    f.w = 0;
+    const int last = reached ? __ffs(reached) - 1 : 31;
+    if (lane == last) {
+        for (int i = 0; i < 8 && f.bin < 0; ++i) {
+            const int at = kSampleBins - 1 - lane * 8 - i;
+            const uint64_t n1 = number(at), w1 = weight(at);
+            if (reached && (by_weight ? w + w1 : n + n1) >= target) {
+                f.bin = at;
+                f.n = (uint32_t)n1;
+                f.w = w1;
+            } else {
+                n += n1;
+                w += w1;
+            }
+        }
+        f.above_n = (uint32_t)n;
+        f.above_w = w;
+    }
+    return f;   // (of lane `last`; the caller keeps that one's)
+}
+
 template <class T>
-__global__ void __launch_bounds__(kSampleThreads, 2) sw_sample_kernel(const SampleParams p) {
+__global__ void __launch_bounds__(kSampleThreads, kSampleCtasPerSm) sw_sample_kernel(const SampleParams p) {
     extern __shared__ __align__(16) unsigned char sample_raw[];
     SampleShared& s = *reinterpret_cast<SampleShared*>(sample_raw);
+    T* const x = reinterpret_cast<T*>(s.x);
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int row = (int)blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid < 32) s.power[tid] = exp2((double)tid / 32.);
-    for (int i = tid; i < 2 * kSampleBins; i += kSampleThreads) (&s.count[0][0])[i] = (&s.low[0][0])[i] = (&s.high[0][0])[i] = 0;
     grid_launch_dependents();
     grid_dependency_wait();
     auto all_here = [&] {
@@ -177,36 +216,42 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sw_sample_kernel(const Samp
         else __syncthreads();
     };
 
-    // ---- the row's settings, and its logits to shared memory ----
-    const float temperature = p.temperature ? p.temperature[row] : 1.f;
-    const int top_k = p.top_k ? p.top_k[row] : 0;
-    const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
-    const bool greedy = !(temperature > 0.f), by_count = !greedy && top_k > 0 && top_k < p.vocab, by_share = !greedy && top_p < 1.f;
-    // Position i of the stretch is logit first + i; the row's first logit lies `first` past a 16-byte boundary in CTA 0.
-    constexpr int kN = Vec<T>::kN;
+    // ---- the row's logits to shared memory, and its settings ----
+    // Position i of the stretch is logit first + i; the row's first logit lies `-first` past a 16-byte boundary in CTA 0.
+    constexpr int kN = 16 / sizeof(T);
     const T* logits = static_cast<const T*>(p.logits) + row * p.row_stride;
     const int first = rank * p.stretch - (int)((reinterpret_cast<uintptr_t>(logits) & 15) / sizeof(T));
-    float top = -INFINITY;
-#pragma unroll 4
     for (int v = tid; v < p.stretch / kN; v += kSampleThreads) {
         const int e = first + v * kN;
-        float f[kN];
         if (e >= 0 && e + kN <= p.vocab) {
-            Vec<T>::widen(__ldcs(reinterpret_cast<const uint4*>(logits + e)), f);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(x + v * kN)), "l"(logits + e) : "memory");
         } else {
 #pragma unroll
-            for (int i = 0; i < kN; ++i) f[i] = e + i >= 0 && e + i < p.vocab ? Vec<T>::one(logits[e + i]) : -INFINITY;
+            for (int i = 0; i < kN; ++i) {
+                if (e + i >= 0 && e + i < p.vocab) x[v * kN + i] = logits[e + i];
+                else store_logit(&x[v * kN + i], -INFINITY);
+            }
         }
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            f[i] = fmaxf(f[i], -INFINITY);   // NaN counts as minus infinity
-            top = fmaxf(top, f[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < kN; i += 4) *reinterpret_cast<float4*>(&s.x[v * kN + i]) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (tid < 32) s.power[tid] = exp2((double)kUnitBits + (double)tid / 32.);
+    if (tid == 0) s.num_mine = 0;
+    const float temperature = p.temperature ? p.temperature[row] : 1.f;
+    const int top_k = p.top_k ? p.top_k[row] : 0;
+    const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f, uniform = p.uniform[row];
+    const bool greedy = !(temperature > 0.f), by_count = !greedy && top_k > 0 && top_k < p.vocab, by_share = !greedy && top_p < 1.f;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    const int blocks = p.stretch / kBlock, block0 = blocks * warp / kSampleWarps, block1 = blocks * (warp + 1) / kSampleWarps;   // of this warp
 
     // ---- the largest logit, and the cut ----
+    float top = -INFINITY;
+#pragma unroll 4
+    for (int b = block0; b < block1; ++b) {
+        float v[4];
+        quad_of(x + b * kBlock + lane * 4, v);
+        top = max3(max3(top, v[0], v[1]), v[2], v[3]);
+    }
     if (by_count || by_share) {
         // the warp's 32 tops in falling order
 #pragma unroll
@@ -216,19 +261,20 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sw_sample_kernel(const Samp
                 const float o = __shfl_xor_sync(0xffffffffu, top, j);
                 top = ((lane & j) == 0) == ((lane & k) == 0) ? fmaxf(top, o) : fminf(top, o);
             }
-        // above its q-th lie about q / 32 of the cluster's threads' tops, and a logit each at least
-        const int q = by_count ? min(31, (2 * min(top_k, 1 << 16) + 64) * 32 / (ranks * kSampleThreads) + 1) : 4;
+        // With `want` logits above the cut, a share of 1 - exp(-want / threads) of the threads' tops is.
+        const float want = by_count ? fmaxf(256.f, 1.5f * (float)top_k + 64.f) : 512.f;
+        const int q = min(31, (int)(32.f * (1.f - __expf(-want / (float)(ranks * kSampleThreads)))));
         const float cut = __shfl_sync(0xffffffffu, top, q);
         if (lane == 0) s.warp_top[warp] = top, s.warp_cut[warp] = cut;
     } else {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (lane == 0) s.warp_top[warp] = top, s.warp_cut[warp] = top;
+        if (lane == 0) s.warp_top[warp] = s.warp_cut[warp] = top;
     }
     __syncthreads();
     if (warp == 0) {
         float t = lane < kSampleWarps ? s.warp_top[lane] : -INFINITY;
-        const float cut = lanes_median(lane < kSampleWarps ? s.warp_cut[lane] : -INFINITY, min(kSampleWarps, (p.stretch / kN + 31) / 32), lane);
+        const float cut = lanes_rank(lane < kSampleWarps ? s.warp_cut[lane] : -INFINITY, kSampleWarps, min(kSampleWarps, blocks) / 2, lane);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
         if (lane < ranks) {
@@ -238,11 +284,11 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sw_sample_kernel(const Samp
         }
     }
     all_here();
-    float m = lane < ranks ? s.rank_top[lane] : -INFINITY;
+    const float rank_top = lane < ranks ? s.rank_top[lane] : -INFINITY;
+    float m = rank_top;
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     m = __shfl_sync(0xffffffffu, m, 0);
-    float cut = lanes_median(lane < ranks ? s.rank_cut[lane] : -INFINITY, ranks, lane);
     if (m == -INFINITY) {   // nothing to draw from
         if (rank == 0 && tid == 0) {
             p.tokens[row] = -1;
@@ -250,40 +296,33 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sw_sample_kernel(const Samp
         }
         return;
     }
-    const float4* x4 = reinterpret_cast<const float4*>(s.x);
-    if (m == INFINITY) {   // the infinite ones share the draw
-        for (int i = tid; i < p.stretch; i += kSampleThreads) s.x[i] = s.x[i] == INFINITY ? 0.f : -INFINITY;
-        m = cut = 0.f;
-        __syncthreads();
-    }
-    const int blocks = p.stretch / kBlock, block0 = blocks * warp / kSampleWarps, block1 = blocks * (warp + 1) / kSampleWarps;   // of this warp
-
-    if (greedy) {
+    if (greedy) {   // the first CTA with that logit has the token
+        if (__ffs(__ballot_sync(0xffffffffu, rank_top == m)) - 1 != rank) return;
         uint32_t at = 0xffffffffu;
         for (int b = block0; b < block1; ++b) {
-            const float4 v = x4[b * 32 + lane];
-            const uint32_t i = (uint32_t)(first + b * kBlock + lane * 4);
-            if (v.w == m) at = min(at, i + 3);
-            if (v.z == m) at = min(at, i + 2);
-            if (v.y == m) at = min(at, i + 1);
-            if (v.x == m) at = min(at, i);
+            float v[4];
+            quad_of(x + b * kBlock + lane * 4, v);
+#pragma unroll
+            for (int i = 3; i >= 0; --i)
+                if (v[i] == m) at = min(at, (uint32_t)(first + b * kBlock + lane * 4 + i));
         }
         at = __reduce_min_sync(0xffffffffu, at);
         if (lane == 0) s.warp_word[warp] = at;
         __syncthreads();
         if (warp == 0) {
             at = __reduce_min_sync(0xffffffffu, lane < kSampleWarps ? s.warp_word[lane] : 0xffffffffu);
-            if (lane < ranks) cluster.map_shared_rank(&s, lane)->rank_first[rank] = at;
-        }
-        all_here();
-        if (rank == 0 && warp == 0) {
-            at = __reduce_min_sync(0xffffffffu, lane < ranks ? s.rank_first[lane] : 0xffffffffu);
             if (lane == 0) {
                 p.tokens[row] = (int32_t)at;
                 if (p.log_probs) p.log_probs[row] = 0.f;
             }
         }
         return;
+    }
+    float cut = lanes_rank(lane < ranks ? s.rank_cut[lane] : -INFINITY, ranks, ranks / 2, lane);
+    if (m == INFINITY) {   // the infinite ones share the draw
+        for (int i = tid; i < p.stretch; i += kSampleThreads) store_logit(&x[i], load_logit(&x[i]) == INFINITY ? 0.f : -INFINITY);
+        m = cut = 0.f;
+        __syncthreads();
     }
 
     // Temperatures at which no number but the largest logit has a weight are all alike.
@@ -293,201 +332,321 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sw_sample_kernel(const Samp
     weigh.c = 32. * 1.4426950408889634 / (double)t;
     weigh.mc = (double)m * weigh.c;
     weigh.floor = fmaxf(fminf(below, m - 44.3614f * t), -FLT_MAX);   // 64 ln 2
-    const bool low = weigh.floor == -FLT_MAX;   // then minus infinity has to be told from the floor
     weigh.power = s.power;
-
-    // ---- top-k and top-p: the lowest key that is kept whole, and how many logits of the key in front of it ----
-    uint32_t keep = kLowestKey, tie_key = 0, ties = 0, tie_before = 0;   // (ties of the CTAs before this one)
-    int pass = 0;
-    // One pass: bins of the interval's logits, summed over the cluster; then the bin in which what lies above reaches the target.
-    // want_total: every weight is added up too, and the target worked out from that.
-    auto find = [&](const Interval& iv, uint64_t above_n, uint64_t above_w, bool by_weight, uint64_t& target, bool want_total) {
-        const int buf = pass & 1;
-        if (pass >= 2) {   // (its bins of two passes ago have been read: a barrier lies between)
-            if (tid < kSampleBins) s.count[buf][tid] = s.low[buf][tid] = s.high[buf][tid] = 0;
-            __syncthreads();
-        }
-        ++pass;
-        uint64_t total = 0;
+    const bool low = weigh.floor == -FLT_MAX;   // then minus infinity and NaN have to be told from the floor
+    const uint64_t least = min_p > 0.f ? (uint64_t)ceil((double)fminf(min_p, 1.f) * (double)weigh(m)) : 0;
+    auto block_sum = [&](uint64_t v) {   // (a barrier before the next one)
+        v = warp_sum_u64(v);
+        if (lane == 0) s.warp_sum[warp] = v;
+        __syncthreads();
+        return warp_sum_u64(lane < kSampleWarps ? s.warp_sum[lane] : 0);
+    };
+    // the units of the warp's run of logits, this lane's part
+    auto all_units = [&] {
+        uint64_t sum = 0;
+#pragma unroll 2
         for (int b = block0; b < block1; ++b) {
-            const float4 v4 = x4[b * 32 + lane];
-            const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+            float v[4];
+            quad_of(x + b * kBlock + lane * 4, v);
             uint64_t w[4];
-            if (want_total) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    w[i] = weigh(v[i]);
-                    if (low && v[i] == -INFINITY) w[i] = 0;
-                    total += w[i];
-                }
-            }
+            for (int i = 0; i < 4; ++i) w[i] = weigh.bits(v[i]);
+            if (low) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t key = key_of(v[i]);
-                if (key < iv.lo || key > iv.hi) continue;
-                const int at = iv.bin(v[i], key);
-                const uint64_t u = want_total ? w[i] : weigh(v[i]);
-                atomicAdd(&s.count[buf][at], 1u);
-                const uint32_t lo = (uint32_t)u, old = atomicAdd(&s.low[buf][at], lo), hi = (uint32_t)(u >> 32) + (old + lo < old);
-                if (hi) atomicAdd(&s.high[buf][at], hi);
+                for (int i = 0; i < 4; ++i) w[i] = v[i] > -INFINITY ? w[i] : Weigh::kZero;
             }
+            sum += (w[0] + w[1]) + (w[2] + w[3]);
         }
-        if (want_total) {
-            total = warp_sum_u64(total);
-            if (lane == 0) s.warp_sum[warp] = total;
+        return sum - (uint64_t)(4 * (block1 - block0)) * Weigh::kZero;
+    };
+    auto add_to_bin = [&](int buf, int at, uint64_t u) {
+        atomicAdd(&s.bins.count[buf][at], 1u);
+        const uint32_t lo = (uint32_t)u, old = atomicAdd(&s.bins.low[buf][at], lo), hi = (uint32_t)(u >> 32) + (old + lo < old);
+        if (hi) atomicAdd(&s.bins.high[buf][at], hi);
+    };
+    auto emit = [&](int token, uint64_t units, uint64_t total) {
+        p.tokens[row] = token;
+        if (p.log_probs) p.log_probs[row] = (float)log((double)units / (double)total);
+    };
+    // The draw from weights of `total` units: the token's sum exceeds it.
+    auto draw_of = [&](uint64_t total) {
+        const float u = fmaxf(uniform, 0.f);
+        return u < 1.f ? share_of(u, total, false) : total - 1;
+    };
+
+    uint32_t keep = kLowestKey, tie_key = 0, ties = 0, tie_before = 0;   // kept: keys from `keep` on, and the first `ties` logits of the key in front of it
+    uint64_t all = 0;
+    if (by_count || by_share) {
+        // ---- the logits above the cut, collected in one CTA ----
+        uint64_t total = by_share && !by_count ? all_units() : 0, above = 0;
+#pragma unroll 2
+        for (int b = block0; b < block1; ++b) {
+            float v[4];
+            quad_of(x + b * kBlock + lane * 4, v);
+            if (!(max4(v) >= cut)) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (v[i] >= cut && v[i] > -INFINITY) {
+                    const uint32_t at = atomicAdd(&s.num_mine, 1u);
+                    if (at < kListed) s.mine[at] = make_uint2(__float_as_uint(v[i]), (uint32_t)(first + b * kBlock + lane * 4 + i));
+                    if (by_share && !by_count) above += weigh(v[i]);
+                }
+        }
+        if (by_share && !by_count) {
+            total = block_sum(total);
             __syncthreads();
-            if (warp == 0) {
-                total = warp_sum_u64(lane < kSampleWarps ? s.warp_sum[lane] : 0);
-                if (lane < ranks) cluster.map_shared_rank(&s, lane)->rank_total[rank] = total;
-            }
+            above = block_sum(above);
+        } else {
+            __syncthreads();
+        }
+        const int collector = row % ranks;
+        const uint32_t listed = s.num_mine;
+        SampleShared* to = cluster.map_shared_rank(&s, collector);
+        if (tid < min(listed, (uint32_t)kListed)) to->listed[rank][tid] = s.mine[tid];
+        if (warp == 0 && lane < ranks) {
+            SampleShared* peer = cluster.map_shared_rank(&s, lane);
+            peer->rank_listed[rank] = listed;
+            peer->rank_total[rank] = total;
+            peer->rank_above[rank] = above;
         }
         all_here();
-        if (tid < kSampleBins) {
-            uint32_t n = 0, before = 0;
-            uint64_t w = 0;
-            for (int r = 0; r < ranks; ++r) {
-                const SampleShared* from = cluster.map_shared_rank(&s, r);
-                const uint32_t c = from->count[buf][tid];
-                n += c;
-                if (r < rank) before += c;
-                w += ((uint64_t)from->high[buf][tid] << 32) + from->low[buf][tid];
-            }
-            s.number[tid] = n;
-            s.before[tid] = before;
-            s.weight[tid] = w;
+        uint32_t n = 0, most = 0;
+        above = 0;
+        for (int r = 0; r < ranks; ++r) {
+            n += s.rank_listed[r];
+            most = max(most, s.rank_listed[r]);
+            all += s.rank_total[r];
+            above += s.rank_above[r];
         }
-        if (want_total) {
-            uint64_t all = 0;
-            for (int r = 0; r < ranks; ++r) all += s.rank_total[r];
-            target = max((uint64_t)1, share_of(fmaxf(top_p, 0.f), all, true));
-        }
-        __syncthreads();
-        if (warp == 0) {   // lane l has bins 255 - 8 l down to 248 - 8 l
-            uint64_t n = 0, w = 0;
+        uint64_t target = by_count ? (uint64_t)top_k : max((uint64_t)1, share_of(fmaxf(top_p, 0.f), all, true));
+        if (most <= kListed && (by_count ? n : above) >= target) {
+            if (rank != collector) return;
+            uint32_t key[kHeld], order[kHeld];   // order: falls with the index
+            uint64_t units[kHeld];
+            unsigned live = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                n += s.number[kSampleBins - 1 - lane * 8 - i];
-                w += s.weight[kSampleBins - 1 - lane * 8 - i];
-            }
-            const uint64_t n_to = above_n + warp_scan_u64(n, lane), w_to = above_w + warp_scan_u64(w, lane);
-            const unsigned reached = __ballot_sync(0xffffffffu, (by_weight ? w_to : n_to) >= target);
-            if (lane == (reached ? __ffs(reached) - 1 : 31)) {
-                n = n_to - n;
-                w = w_to - w;
-                int at = kSampleBins - 1 - lane * 8;
-                for (int i = 0; i < 8; ++i, --at) {
-                    const uint64_t n1 = n + s.number[at], w1 = w + s.weight[at];
-                    if ((by_weight ? w1 : n1) >= target) break;
-                    n = n1;
-                    w = w1;
-                }
-                if (!reached) at = -1;   // (n and w: everything)
-                s.found.bin = at;
-                s.found.above_n = (uint32_t)n;
-                s.found.above_w = w;
-                if (at >= 0) {
-                    s.found.n = s.number[at];
-                    s.found.w = s.weight[at];
-                    s.found.before = s.before[at];
+            for (int i = 0; i < kHeld; ++i) {
+                const int at = tid + i * kSampleThreads, r = at / kListed;
+                key[i] = order[i] = 0;
+                units[i] = 0;
+                if (r < ranks && at - r * kListed < (int)s.rank_listed[r]) {
+                    const uint2 e = s.listed[r][at - r * kListed];
+                    key[i] = key_of(__uint_as_float(e.x));
+                    order[i] = ~e.y;
+                    units[i] = weigh(__uint_as_float(e.x));
+                    live |= 1u << i;
                 }
             }
-        }
-        __syncthreads();
-        return s.found;
-    };
-    // Keeps the front part that reaches `target` logits, or units, of those from key `bottom` on.
-    // Returns the units of what lies above the ties, or is kept whole.
-    auto select = [&](Interval iv, uint32_t bottom, bool by_weight, uint64_t target, bool want_total) {
-        uint64_t above_n = 0, above_w = 0;
-        const uint32_t old_ties = ties;
-        for (;;) {
-            const auto f = find(iv, above_n, above_w, by_weight, target, want_total);
-            want_total = false;
-            above_n = f.above_n;
-            above_w = f.above_w;
-            if (f.bin < 0) {
-                if (iv.lo <= bottom) {   // everything from there on, and of what was kept of the key in front of it
-                    keep = bottom;
-                    if (by_weight && old_ties > 0) {
-                        const uint64_t w = max((uint64_t)1, weigh(value_of(tie_key)));
-                        ties = (uint32_t)min((uint64_t)old_ties, target <= above_w ? 0 : (target - above_w + w - 1) / w);
+            // Of the held logits in `of`, by falling `k`: leaves in `of` those in front of and in the bin where the target is reached, and in f what
+            // that bin is; it has one logit, or one k, or (by number) it is kept whole.
+            auto descend = [&](const uint32_t (&k)[kHeld], unsigned& of, uint32_t lo, uint32_t hi, bool by_weight, uint64_t target, uint32_t& bin_lo,
+                               uint32_t& bin_hi) {
+                uint64_t above_n = 0, above_w = 0;
+                for (;;) {
+                    const int shift = max(0, 24 - __clz(hi - lo));
+                    __syncthreads();
+                    s.bins.count[0][tid] = s.bins.low[0][tid] = s.bins.high[0][tid] = 0;
+                    __syncthreads();
+#pragma unroll
+                    for (int i = 0; i < kHeld; ++i)
+                        if (of >> i & 1 && k[i] >= lo && k[i] <= hi) add_to_bin(0, (int)((k[i] - lo) >> shift), units[i]);
+                    __syncthreads();
+                    if (warp == 0) {
+                        const auto f = pick_bin([&](int i) { return s.bins.count[0][i]; },
+                                                [&](int i) { return ((uint64_t)s.bins.high[0][i] << 32) + s.bins.low[0][i]; }, above_n, above_w, by_weight, target, lane);
+                        if (f.bin >= 0) s.found = f;
                     }
+                    __syncthreads();
+                    const auto f = s.found;
+                    above_n = f.above_n;
+                    above_w = f.above_w;
+                    const uint32_t bin_at = lo + ((uint32_t)f.bin << shift);
+                    hi = bin_at + min(hi - bin_at, (1u << shift) - 1);
+                    lo = bin_at;
+                    if (lo == hi || f.n == 1 || (!by_weight && above_n + f.n == target)) {
+#pragma unroll
+                        for (int i = 0; i < kHeld; ++i)
+                            if (k[i] < lo) of &= ~(1u << i);
+                        bin_lo = lo;
+                        bin_hi = hi;
+                        return f;
+                    }
+                }
+            };
+            // Keeps the front part of the live logits that reaches the target; of equal ones the first.
+            auto cut_to = [&](bool by_weight, uint64_t target) {
+                uint32_t lo, hi;
+                const auto f = descend(key, live, min(key_of(cut), m_key), m_key, by_weight, target, lo, hi);
+                const uint32_t n = by_weight ? (f.w == 0 ? f.n : (uint32_t)min((uint64_t)f.n, (target - f.above_w + f.w / f.n - 1) / (f.w / f.n)))
+                                             : (uint32_t)(target - f.above_n);
+                if (n == f.n) return;
+                unsigned equal = 0;   // (all of one key)
+#pragma unroll
+                for (int i = 0; i < kHeld; ++i)
+                    if (live >> i & 1 && key[i] == lo) equal |= 1u << i;
+                live &= ~equal;
+                descend(order, equal, ~(uint32_t)(p.vocab - 1), ~0u, false, n, lo, hi);
+                live |= equal;
+            };
+            auto live_units = [&] {
+                uint64_t sum = 0;
+#pragma unroll
+                for (int i = 0; i < kHeld; ++i)
+                    if (live >> i & 1) sum += units[i];
+                __syncthreads();
+                return block_sum(sum);
+            };
+            if (by_count) {
+                if (n > (uint32_t)top_k) cut_to(false, target);
+                if (by_share) target = max((uint64_t)1, share_of(fmaxf(top_p, 0.f), live_units(), true));
+            }
+            if (by_share) cut_to(true, target);
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if (units[i] < least) live &= ~(1u << i);
+            const uint64_t kept = live_units();
+            uint32_t lo, hi;
+            unsigned up_to = live;
+            descend(order, up_to, ~(uint32_t)(p.vocab - 1), ~0u, true, draw_of(kept) + 1, lo, hi);
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if (live >> i & 1 && order[i] >= lo && order[i] <= hi) emit((int)~order[i], units[i], kept);
+            return;
+        }
+
+        // ---- the threshold lies lower: the lowest key that is kept whole, and how many logits of the key in front of it, by all CTAs ----
+        for (int buf = 0; buf < 2; ++buf) s.bins.count[buf][tid] = s.bins.low[buf][tid] = s.bins.high[buf][tid] = 0;
+        __syncthreads();
+        int pass = 0;
+        // One pass: bins of the interval's logits, summed over the cluster; then the bin in which what lies above reaches the target.
+        auto find = [&](const Interval& iv, uint64_t above_n, uint64_t above_w, bool by_weight, uint64_t target) {
+            const int buf = pass & 1;
+            if (pass >= 2) {   // (its bins of two passes ago have been read: a barrier lies between)
+                s.bins.count[buf][tid] = s.bins.low[buf][tid] = s.bins.high[buf][tid] = 0;
+                __syncthreads();
+            }
+            ++pass;
+            const float from = value_of(iv.lo);
+            for (int b = block0; b < block1; ++b) {
+                float v[4];
+                quad_of(x + b * kBlock + lane * 4, v);
+                if (!(max4(v) >= from)) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t key = key_of(v[i]);
+                    if (v[i] >= from && key >= iv.lo && key <= iv.hi) add_to_bin(buf, iv.bin(v[i], key), weigh(v[i]));
+                }
+            }
+            all_here();
+            {
+                uint32_t n = 0;
+                uint64_t w = 0;
+                for (int r = 0; r < ranks; ++r) {
+                    const SampleShared* from = cluster.map_shared_rank(&s, r);
+                    n += from->bins.count[buf][tid];
+                    w += ((uint64_t)from->bins.high[buf][tid] << 32) + from->bins.low[buf][tid];
+                }
+                s.bins.number[tid] = n;
+                s.bins.weight[tid] = w;
+            }
+            __syncthreads();
+            if (warp == 0) {
+                const auto f = pick_bin([&](int i) { return s.bins.number[i]; }, [&](int i) { return s.bins.weight[i]; }, above_n, above_w, by_weight, target, lane);
+                const unsigned has = __ballot_sync(0xffffffffu, f.bin >= 0);
+                if (lane == (has ? __ffs(has) - 1 : 31)) s.found = f;
+            }
+            __syncthreads();
+            return s.found;
+        };
+        // Keeps the front part that reaches `target` logits, or units, of those from key `bottom` on.
+        // Returns the units of what lies above the ties, or is kept whole.
+        auto select = [&](Interval iv, uint32_t bottom, bool by_weight, uint64_t target) {
+            uint64_t above_n = 0, above_w = 0;
+            const uint32_t old_ties = ties;
+            for (;;) {
+                const auto f = find(iv, above_n, above_w, by_weight, target);
+                above_n = f.above_n;
+                above_w = f.above_w;
+                if (f.bin < 0) {
+                    if (iv.lo <= bottom) {   // everything from there on, and of what was kept of the key in front of it
+                        keep = bottom;
+                        if (by_weight && old_ties > 0) {
+                            const uint64_t w = max((uint64_t)1, weigh(value_of(tie_key)));
+                            ties = (uint32_t)min((uint64_t)old_ties, target <= above_w ? 0 : (target - above_w + w - 1) / w);
+                        }
+                        break;
+                    }
+                    iv.hi = iv.lo - 1;
+                    iv.lo = bottom;
+                    iv.linear = true;
+                    iv.x_lo = fmaxf(weigh.floor, value_of(bottom));
+                    iv.per = 256.f / fmaxf(value_of(iv.hi) - iv.x_lo, 1e-30f);
+                    continue;
+                }
+                if (!iv.linear && iv.shift == 0) {   // one key, of equal weights
+                    const uint32_t key = iv.lo + f.bin;
+                    const uint64_t w = max((uint64_t)1, f.w / f.n);
+                    const uint32_t n = (uint32_t)(by_weight ? min((uint64_t)f.n, f.w == 0 ? f.n : (target - above_w + w - 1) / w) : target - above_n);
+                    tie_key = key;
+                    ties = n == f.n ? 0 : n;
+                    tie_before = 0;
+                    for (int r = 0; r < rank; ++r) tie_before += cluster.map_shared_rank(&s, r)->bins.count[(pass - 1) & 1][f.bin];
+                    keep = n == f.n ? key : key + 1;
+                    above_w += n == f.n ? f.w : 0;
                     break;
                 }
-                iv.hi = iv.lo - 1;
-                iv.lo = bottom;
-                iv.linear = true;
-                iv.x_lo = fmaxf(weigh.floor, value_of(bottom));
-                iv.per = 256.f / fmaxf(value_of(iv.hi) - iv.x_lo, 1e-30f);
-                continue;
-            }
-            if (!iv.linear && iv.shift == 0) {   // one key, of equal weights
-                const uint32_t key = iv.lo + f.bin;
-                const uint64_t w = max((uint64_t)1, f.w / f.n);
-                const uint32_t n = (uint32_t)(by_weight ? min((uint64_t)f.n, f.w == 0 ? f.n : (target - above_w + w - 1) / w) : target - above_n);
-                tie_key = key;
-                ties = n == f.n ? 0 : n;
-                tie_before = f.before;
-                keep = n == f.n ? key : key + 1;
-                above_w += n == f.n ? f.w : 0;
-                break;
-            }
-            uint32_t lo = iv.lo + (iv.linear ? 0 : (uint32_t)f.bin << iv.shift), hi = lo + min(iv.hi - lo, (1u << iv.shift) - 1);
-            if (iv.linear) {
-                // the lowest keys of the bin and of the next one: the bin of a number never falls
-                if (tid < 2) {
-                    uint32_t a = iv.lo, b = iv.hi + 1;   // (b: past the last)
-                    while (a < b) {
-                        const uint32_t mid = a + (b - a) / 2;
-                        if (iv.bin(value_of(mid), mid) >= f.bin + tid) b = mid;
-                        else a = mid + 1;
+                uint32_t lo = iv.lo + (iv.linear ? 0 : (uint32_t)f.bin << iv.shift), hi = lo + min(iv.hi - lo, (1u << iv.shift) - 1);
+                if (iv.linear) {
+                    // the lowest keys of the bin and of the next one: the bin of a number never falls
+                    if (tid < 2) {
+                        uint32_t a = iv.lo, b = iv.hi + 1;   // (b: past the last)
+                        while (a < b) {
+                            const uint32_t mid = a + (b - a) / 2;
+                            if (iv.bin(value_of(mid), mid) >= f.bin + tid) b = mid;
+                            else a = mid + 1;
+                        }
+                        s.edge[tid] = a;
                     }
-                    s.edge[tid] = a;
+                    __syncthreads();
+                    lo = s.edge[0];
+                    hi = s.edge[1] - 1;
                 }
-                __syncthreads();
-                lo = s.edge[0];
-                hi = s.edge[1] - 1;
+                if (by_weight ? f.n == 1 : above_n + f.n == target) {
+                    keep = lo;
+                    ties = 0;
+                    above_w += f.w;
+                    break;
+                }
+                iv.by_key(lo, hi);
             }
-            if (by_weight ? f.n == 1 : above_n + f.n == target) {
-                keep = lo;
-                ties = 0;
-                above_w += f.w;
-                break;
-            }
-            iv.by_key(lo, hi);
-        }
-        return above_w;
-    };
-    uint64_t total_k = 0;
-    if (by_count) {
+            return above_w;
+        };
         Interval iv;
         iv.by_key(max(kLowestKey, key_of(cut)), m_key);
-        total_k = select(iv, kLowestKey, false, (uint64_t)top_k, false);
-        if (ties > 0) total_k += ties * weigh(value_of(tie_key));
-    }
-    if (by_share) {
-        const uint64_t target = max((uint64_t)1, share_of(fmaxf(top_p, 0.f), total_k, true));
-        Interval iv;
-        if (!by_count) {
-            iv.by_key(max(kLowestKey, key_of(cut)), m_key);
-            select(iv, kLowestKey, true, 0, true);
-        } else if (keep <= m_key) {
-            iv.by_key(keep, m_key);
-            select(iv, keep, true, target, false);
-        } else {   // all of what is left are equal
-            const uint64_t w = weigh(value_of(tie_key));
-            ties = (uint32_t)min((uint64_t)ties, (target + w - 1) / w);
+        uint64_t total_k = select(iv, kLowestKey, !by_count, target);
+        if (by_count && by_share) {
+            if (ties > 0) total_k += ties * weigh(value_of(tie_key));
+            target = max((uint64_t)1, share_of(fmaxf(top_p, 0.f), total_k, true));
+            if (keep <= m_key) {
+                iv.by_key(keep, m_key);
+                select(iv, keep, true, target);
+            } else {   // all of what is left are equal
+                const uint64_t w = weigh(value_of(tie_key));
+                ties = (uint32_t)min((uint64_t)ties, (target + w - 1) / w);
+            }
         }
     }
 
     // ---- the kept weights' sums ----
-    const uint64_t least = min_p > 0.f ? (uint64_t)ceil((double)fminf(min_p, 1.f) * (double)weigh(m)) : 0;
+    const float tie = value_of(tie_key);
     uint32_t tie_at = 0;   // ties in front of the warp's next block
     if (ties > 0) {
         uint32_t n = 0;
         for (int b = block0; b < block1; ++b) {
-            const float4 v = x4[b * 32 + lane];
-            n += (key_of(v.x) == tie_key) + (key_of(v.y) == tie_key) + (key_of(v.z) == tie_key) + (key_of(v.w) == tie_key);
+            float v[4];
+            quad_of(x + b * kBlock + lane * 4, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n += v[i] == tie;
         }
         n = __reduce_add_sync(0xffffffffu, n);
         if (lane == 0) s.warp_word[warp] = n;
@@ -495,18 +654,22 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sw_sample_kernel(const Samp
         tie_at = tie_before;
         for (int w = 0; w < warp; ++w) tie_at += s.warp_word[w];
     }
+    // No logit below this one is kept: of the threshold, or of min_p (less what the rounding of its place can be off).
+    float from = value_of(ties > 0 ? tie_key : keep);
+    if (least > 0) from = fmaxf(from, fmaxf(-FLT_MAX, m + t * logf(fminf(min_p, 1.f)) * 1.0001f - 1e-5f * (fabsf(m) + t)));
+    const bool everything = keep == kLowestKey && least == 0;
     // units of four neighbouring logits of block b, none where they are not kept; `at`: ties so far, moved on
     auto kept_units = [&](int b, uint32_t& at, uint64_t (&w)[4]) {
-        const float4 v4 = x4[b * 32 + lane];
-        const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+        float v[4];
+        quad_of(x + b * kBlock + lane * 4, v);
         bool in[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) in[i] = key_of(v[i]) >= keep;
+        for (int i = 0; i < 4; ++i) in[i] = v[i] >= from && key_of(v[i]) >= keep;
         if (ties > 0) {
             unsigned of[4], any = 0;
             const unsigned lower = (1u << lane) - 1;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) any |= of[i] = __ballot_sync(0xffffffffu, key_of(v[i]) == tie_key);
+            for (int i = 0; i < 4; ++i) any |= of[i] = __ballot_sync(0xffffffffu, v[i] == tie);
             if (any) {
                 uint32_t mine = at;
 #pragma unroll
@@ -530,20 +693,28 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sw_sample_kernel(const Samp
         }
     };
     uint64_t sum = 0;
-    {
+    if (everything) {
+        sum = all_units();
+    } else {
         uint32_t at = tie_at;
         for (int b = block0; b < block1; ++b) {
+            if (ties == 0) {
+                float v[4];
+                quad_of(x + b * kBlock + lane * 4, v);
+                if (!__any_sync(0xffffffffu, max4(v) >= from)) continue;
+            }
             uint64_t w[4];
             kept_units(b, at, w);
             sum += (w[0] + w[1]) + (w[2] + w[3]);
         }
     }
     sum = warp_sum_u64(sum);
+    __syncthreads();
     if (lane == 0) s.warp_sum[warp] = sum;
     __syncthreads();
     if (warp == 0) {
-        const uint64_t all = warp_sum_u64(lane < kSampleWarps ? s.warp_sum[lane] : 0);
-        if (lane < ranks) cluster.map_shared_rank(&s, lane)->rank_kept[rank] = all;
+        const uint64_t cta = warp_sum_u64(lane < kSampleWarps ? s.warp_sum[lane] : 0);
+        if (lane < ranks) cluster.map_shared_rank(&s, lane)->rank_kept[rank] = cta;
     }
     all_here();
 
@@ -554,8 +725,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sw_sample_kernel(const Samp
         if (r < rank) in_front += s.rank_kept[r];
     }
     for (int w = 0; w < warp; ++w) in_front += s.warp_sum[w];
-    const float u = fmaxf(p.uniform[row], 0.f);
-    const uint64_t drawn = u < 1.f ? share_of(u, total, false) : total - 1;   // the token's sum exceeds it
+    const uint64_t drawn = draw_of(total);
     if (drawn < in_front || drawn >= in_front + sum) return;
     for (int b = block0; b < block1; ++b) {
         uint64_t w[4];
@@ -570,9 +740,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sw_sample_kernel(const Samp
                     at += w[i];
                     if (at > drawn) break;
                 }
-                const uint64_t units = i == 0 ? w[0] : i == 1 ? w[1] : i == 2 ? w[2] : w[3];
-                p.tokens[row] = first + b * kBlock + lane * 4 + i;
-                if (p.log_probs) p.log_probs[row] = (float)log((double)units / (double)total);
+                emit(first + b * kBlock + lane * 4 + i, i == 0 ? w[0] : i == 1 ? w[1] : i == 2 ? w[2] : w[3], total);
             }
             return;
         }
@@ -582,6 +750,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sw_sample_kernel(const Samp
 
 constexpr int kMaxStretch = (227 * 1024 - (int)sizeof(SampleShared)) / 4 / kBlock * kBlock;
 static_assert((int64_t)kMaxStretch * kSampleRanks >= kMaxVocab + 8 + kSampleRanks * kBlock, "the largest vocabulary fits eight CTAs");
+static_assert(kSampleCtasPerSm * (sizeof(SampleShared) + 16128 * 4 + 1024) <= 228 * 1024, "three stretches of an eighth of 128256 logits fit an SM");
 
 template <class F>
 cudaError_t for_each_sample(F f) {
@@ -598,8 +767,9 @@ cudaError_t configure_sample_kernels() {
 
 cudaError_t launch_sample(const SampleParams& params, int dtype, int num_sms, cudaStream_t stream) {
     SampleParams p = params;
-    // CTAs of a row: as many as give each 16384 logits at most (64 KB: two CTAs an SM, one loads while the other works), and more where rows are few.
-    const int64_t positions = (int64_t)p.vocab + 16 / (dtype == SW_DTYPE_F32 ? 4 : 2) - 1;   // (a row may start anywhere behind a 16-byte boundary)
+    const int size = dtype == SW_DTYPE_F32 ? 4 : 2;
+    // CTAs of a row: as many as give each 16384 logits at most (64 KB: three CTAs an SM, one loads while the others work), and more where rows are few.
+    const int64_t positions = (int64_t)p.vocab + 16 / size - 1;   // (a row may start anywhere behind a 16-byte boundary)
     int ranks = 1;
     while (ranks < kSampleRanks && (positions > ranks * 16384 || (p.rows * ranks < num_sms && positions > ranks * 2048))) ranks *= 2;
     p.stretch = (int)((positions + ranks * kBlock - 1) / (ranks * kBlock) * kBlock);
@@ -612,7 +782,7 @@ cudaError_t launch_sample(const SampleParams& params, int dtype, int num_sms, cu
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(p.rows * ranks));
     cfg.blockDim = dim3(kSampleThreads);
-    cfg.dynamicSmemBytes = sizeof(SampleShared) + (size_t)p.stretch * 4;
+    cfg.dynamicSmemBytes = sizeof(SampleShared) + (size_t)p.stretch * size;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
