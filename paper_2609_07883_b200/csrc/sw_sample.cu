@@ -5,7 +5,7 @@
 // kept weights sum to more than u times their total.
 //
 // A border between tokens, or of top-p, is a sum over all logits: with 128256 about equal ones, sums in fp32 would put every tenth draw on the wrong side.
-// Weights are worked out in 64 bits (2^x from a table of 32 powers and a polynomial of degree four, 8e-14 off) and rounded to 2^-44 of the
+// Weights are worked out in 64 bits (2^x from a table of 16 powers and a polynomial of degree five, 1e-14 off) and rounded to 2^-44 of the
 // largest; their sums are integers, exact in any order, and equal logits have equal weights.
 //
 // A cluster of 1 to 8 CTAs has a row; each CTA copies an equal stretch to shared memory, so logits are read from memory once.  Then
@@ -28,13 +28,11 @@
 namespace sw {
 namespace cg = cooperative_groups;
 
-constexpr int kSampleThreads = 256, kSampleWarps = kSampleThreads / 32, kSampleBins = 256, kSampleRanks = 8;
-constexpr int kSampleCtasPerSm = 3;
+constexpr int kSampleBins = 256, kSampleRanks = 8, kMaxWarps = 32;
 constexpr int kBlock = 128;   // logits that a warp takes at once
-constexpr int kListed = 144, kHeld = (kListed * kSampleRanks + kSampleThreads - 1) / kSampleThreads;   // collected from a CTA; by a thread of the collecting one
+constexpr int kListed = 144;  // logits collected from a CTA
 constexpr uint32_t kLowestKey = 0x00800000u;   // key_of() of the lowest finite number
 constexpr int kUnitBits = 44;                  // the largest weight is 2^44 units: sums of up to 2^19 of them fit 63 bits
-static_assert(kSampleThreads == kSampleBins, "a thread per bin");
 
 struct SampleShared {
     union {
@@ -44,12 +42,13 @@ struct SampleShared {
             uint64_t weight[kSampleBins];                                                // summed over the cluster
             uint32_t number[kSampleBins];                                                // likewise
         } bins;
+        uint64_t block[kMaxWarps];   // units of the blocks that the warps look through
     };
     uint2 mine[kListed];
-    double power[32];   // 2^(44 + j / 32)
-    uint64_t rank_total[kSampleRanks], rank_above[kSampleRanks], rank_kept[kSampleRanks], warp_sum[kSampleWarps];
-    float rank_top[kSampleRanks], rank_cut[kSampleRanks], warp_top[kSampleWarps], warp_cut[kSampleWarps];
-    uint32_t rank_listed[kSampleRanks], warp_word[kSampleWarps];
+    double power[16];   // (see Weigh)
+    uint64_t rank_total[kSampleRanks], rank_above[kSampleRanks], rank_kept[kSampleRanks], warp_sum[kMaxWarps];
+    float rank_top[kSampleRanks], rank_cut[kSampleRanks], warp_top[kMaxWarps], warp_cut[kMaxWarps];
+    uint32_t rank_listed[kSampleRanks], warp_word[kMaxWarps];
     struct Found {
         uint64_t above_w, w;   // units of what lies above the bin, and in it
         uint32_t above_n, n;
@@ -66,20 +65,24 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
 
-// A logit's weight in units.
+// A logit's weight in units: 2^44 2^((x - max) c / 16) with x c to the nearest integer in the exponent and a table of 16 powers, the rest in a polynomial.
+// |x c| < 2^36: of large numbers, a temperature below that at which only the largest has a weight is not taken (below).
 struct Weigh {
-    double c, mc;        // 32 / ln 2 / temperature, and times the largest logit
-    float floor;         // weights below 2^-64 are none
-    const double* power;
-    static constexpr uint64_t kZero = 0x4330000000000000ull;   // bits of 2^52: a sum with it is rounded to an integer, which its low bits hold
+    double c;             // 16 / ln 2 / temperature
+    double shift;         // 1.5 2^52 less the largest logit's c, rounded: a sum with it is rounded to an integer, which its low word holds
+    float floor;          // weights below 2^-64 are none
+    const double* power;  // 2^(44 + (j - f) / 16), f what was rounded off the largest logit's c
+    static constexpr uint64_t kZero = 0x4330000000000000ull;   // bits of 2^52: a sum with it is rounded likewise
+    static __device__ __forceinline__ double power_of(double f) {   // 2^(f / 16), |f| <= 1/2, to 4.5e-15
+        return fma(fma(fma(fma(fma(1.2715658865126869e-09, f, 1.4676444610409443e-07), f, 1.3550807790817295e-05), f, 0.0009383847924862347), f,
+                       0.043321698784995775), f, 1.0000000000000044);
+    }
     __device__ __forceinline__ uint64_t bits(float x) const {  // kZero + units
-        const double magic = 6755399441055744.0;   // 1.5 2^52: likewise, of either sign
-        const double t = fma((double)fmaxf(x, floor), c, -mc), r = t + magic, f = t - (r - magic);   // (NaN: the floor)
+        const double d = (double)fmaxf(x, floor), r = fma(d, c, shift), f = fma(d, c, shift - r);   // (NaN: the floor)
         const int n = __double2loint(r);
-        const double q = fma(fma(fma(fma(9.172517872816247e-09, f, 1.6938633901956802e-06), f, 0.00023459619822185958), f, 0.021660849391722196), f,
-                             0.9999999999999993);   // 2^(f / 32), |f| <= 1/2
-        const double s = power[n & 31];
-        return (uint64_t)__double_as_longlong(fma(q, __hiloint2double(__double2hiint(s) + (n & ~31) * 0x8000, __double2loint(s)), 4503599627370496.0));
+        const double q = power_of(f);
+        const double s = power[n & 15];
+        return (uint64_t)__double_as_longlong(fma(q, __hiloint2double(__double2hiint(s) + (n & ~15) * 0x10000, __double2loint(s)), 4503599627370496.0));
     }
     __device__ __forceinline__ uint64_t operator()(float x) const { return bits(x) - kZero; }
 };
@@ -201,8 +204,11 @@ __device__ __forceinline__ SampleShared::Found pick_bin(N number, W weight, uint
     return f;   // (of lane `last`; the caller keeps that one's)
 }
 
-template <class T>
-__global__ void __launch_bounds__(kSampleThreads, kSampleCtasPerSm) sw_sample_kernel(const SampleParams p) {
+// Threads of a CTA, and CTAs an SM: small ones that work while others load, or large ones where no SM gets a second.
+constexpr int kManySampleThreads = 1024, kFewSampleThreads = 256;
+template <class T, int kSampleThreads>
+__global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleThreads ? 3 : 1) sw_sample_kernel(const SampleParams p) {
+    constexpr int kSampleWarps = kSampleThreads / 32, kHeld = (kListed * kSampleRanks + kSampleThreads - 1) / kSampleThreads;   // kHeld: of the collected logits
     extern __shared__ __align__(16) unsigned char sample_raw[];
     SampleShared& s = *reinterpret_cast<SampleShared*>(sample_raw);
     T* const x = reinterpret_cast<T*>(s.x);
@@ -234,11 +240,12 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleCtasPerSm) sw_sample_ke
         }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    if (tid < 32) s.power[tid] = exp2((double)kUnitBits + (double)tid / 32.);
+    if (tid < 16) s.power[tid] = exp2((double)kUnitBits + (double)tid / 16.);
     if (tid == 0) s.num_mine = 0;
     const float temperature = p.temperature ? p.temperature[row] : 1.f;
     const int top_k = p.top_k ? p.top_k[row] : 0;
     const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f, uniform = p.uniform[row];
+    const double usual_c = 16. * 1.4426950408889634 / (double)temperature;
     const bool greedy = !(temperature > 0.f), by_count = !greedy && top_k > 0 && top_k < p.vocab, by_share = !greedy && top_p < 1.f;
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
@@ -269,12 +276,13 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleCtasPerSm) sw_sample_ke
     } else {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (lane == 0) s.warp_top[warp] = s.warp_cut[warp] = top;
+        if (lane == 0) s.warp_top[warp] = top;
     }
     __syncthreads();
     if (warp == 0) {
         float t = lane < kSampleWarps ? s.warp_top[lane] : -INFINITY;
-        const float cut = lanes_rank(lane < kSampleWarps ? s.warp_cut[lane] : -INFINITY, kSampleWarps, min(kSampleWarps, blocks) / 2, lane);
+        float cut = 0.f;
+        if (by_count || by_share) cut = lanes_rank(lane < kSampleWarps ? s.warp_cut[lane] : -INFINITY, kSampleWarps, min(kSampleWarps, blocks) / 2, lane);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
         if (lane < ranks) {
@@ -318,21 +326,26 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleCtasPerSm) sw_sample_ke
         }
         return;
     }
-    float cut = lanes_rank(lane < ranks ? s.rank_cut[lane] : -INFINITY, ranks, ranks / 2, lane);
+    float cut = 0.f;
+    if (by_count || by_share) cut = lanes_rank(lane < ranks ? s.rank_cut[lane] : -INFINITY, ranks, ranks / 2, lane);
     if (m == INFINITY) {   // the infinite ones share the draw
         for (int i = tid; i < p.stretch; i += kSampleThreads) store_logit(&x[i], load_logit(&x[i]) == INFINITY ? 0.f : -INFINITY);
         m = cut = 0.f;
         __syncthreads();
     }
 
-    // Temperatures at which no number but the largest logit has a weight are all alike.
+    // Temperatures at which no number but the largest logit has a weight are all alike: the next one lies 2^-24 of it below at least, and here 128 times the
+    // temperature.
     const uint32_t m_key = key_of(m);
-    const float below = fmaxf(value_of(m_key - 1), -FLT_MAX), t = fmaxf(temperature, (m - below) * (1.f / 256.f));
+    const float below = fmaxf(value_of(m_key - 1), -FLT_MAX), t = fmaxf(temperature, fabsf(m) * 0x1p-31f);
     Weigh weigh;
-    weigh.c = 32. * 1.4426950408889634 / (double)t;
-    weigh.mc = (double)m * weigh.c;
+    weigh.c = t == temperature ? usual_c : 16. * 1.4426950408889634 / (double)t;
+    const double top_c = rint((double)m * weigh.c);
+    weigh.shift = 6755399441055744.0 - top_c;
+    if (tid < 16) s.power[tid] *= Weigh::power_of(top_c - (double)m * weigh.c);
     weigh.floor = fmaxf(fminf(below, m - 44.3614f * t), -FLT_MAX);   // 64 ln 2
     weigh.power = s.power;
+    __syncthreads();
     const bool low = weigh.floor == -FLT_MAX;   // then minus infinity and NaN have to be told from the floor
     const uint64_t least = min_p > 0.f ? (uint64_t)ceil((double)fminf(min_p, 1.f) * (double)weigh(m)) : 0;
     auto block_sum = [&](uint64_t v) {   // (a barrier before the next one)
@@ -445,7 +458,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleCtasPerSm) sw_sample_ke
                 for (;;) {
                     const int shift = max(0, 24 - __clz(hi - lo));
                     __syncthreads();
-                    s.bins.count[0][tid] = s.bins.low[0][tid] = s.bins.high[0][tid] = 0;
+                    if (tid < kSampleBins) s.bins.count[0][tid] = s.bins.low[0][tid] = s.bins.high[0][tid] = 0;
                     __syncthreads();
 #pragma unroll
                     for (int i = 0; i < kHeld; ++i)
@@ -515,14 +528,14 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleCtasPerSm) sw_sample_ke
         }
 
         // ---- the threshold lies lower: the lowest key that is kept whole, and how many logits of the key in front of it, by all CTAs ----
-        for (int buf = 0; buf < 2; ++buf) s.bins.count[buf][tid] = s.bins.low[buf][tid] = s.bins.high[buf][tid] = 0;
+        for (int i = tid; i < 2 * kSampleBins; i += kSampleThreads) (&s.bins.count[0][0])[i] = (&s.bins.low[0][0])[i] = (&s.bins.high[0][0])[i] = 0;
         __syncthreads();
         int pass = 0;
         // One pass: bins of the interval's logits, summed over the cluster; then the bin in which what lies above reaches the target.
         auto find = [&](const Interval& iv, uint64_t above_n, uint64_t above_w, bool by_weight, uint64_t target) {
             const int buf = pass & 1;
             if (pass >= 2) {   // (its bins of two passes ago have been read: a barrier lies between)
-                s.bins.count[buf][tid] = s.bins.low[buf][tid] = s.bins.high[buf][tid] = 0;
+                if (tid < kSampleBins) s.bins.count[buf][tid] = s.bins.low[buf][tid] = s.bins.high[buf][tid] = 0;
                 __syncthreads();
             }
             ++pass;
@@ -538,7 +551,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleCtasPerSm) sw_sample_ke
                 }
             }
             all_here();
-            {
+            if (tid < kSampleBins) {
                 uint32_t n = 0;
                 uint64_t w = 0;
                 for (int r = 0; r < ranks; ++r) {
@@ -724,40 +737,63 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleCtasPerSm) sw_sample_ke
         total += s.rank_kept[r];
         if (r < rank) in_front += s.rank_kept[r];
     }
-    for (int w = 0; w < warp; ++w) in_front += s.warp_sum[w];
     const uint64_t drawn = draw_of(total);
-    if (drawn < in_front || drawn >= in_front + sum) return;
-    for (int b = block0; b < block1; ++b) {
-        uint64_t w[4];
-        kept_units(b, tie_at, w);
-        const uint64_t here = (w[0] + w[1]) + (w[2] + w[3]), to = in_front + warp_scan_u64(here, lane);
-        const unsigned past = __ballot_sync(0xffffffffu, to > drawn);
-        if (past) {
-            if (lane == __ffs(past) - 1) {
-                uint64_t at = to - here;
-                int i = 0;
-                for (; i < 3; ++i) {
-                    at += w[i];
-                    if (at > drawn) break;
+    if (drawn < in_front || drawn >= in_front + s.rank_kept[rank]) return;
+    // The warps look through the run of the one that it falls into, a block each.
+    int of = 0;
+    for (uint64_t w = s.warp_sum[0]; in_front + w <= drawn; w = s.warp_sum[of]) {
+        in_front += w;
+        ++of;
+    }
+    const int run0 = blocks * of / kSampleWarps, run1 = blocks * (of + 1) / kSampleWarps;
+    for (int round = run0; round < run1; round += kSampleWarps) {
+        const int b = round + warp;
+        uint64_t w[4] = {0, 0, 0, 0};
+        if (b < run1) {
+            uint32_t at = tie_before;
+            if (ties > 0) {   // those in front of the block
+                uint32_t n = 0;
+                for (int c = run0; c < b; ++c) {
+                    float v[4];
+                    quad_of(x + c * kBlock + lane * 4, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) n += v[i] == tie;
                 }
-                emit(first + b * kBlock + lane * 4 + i, i == 0 ? w[0] : i == 1 ? w[1] : i == 2 ? w[2] : w[3], total);
+                at += __reduce_add_sync(0xffffffffu, n);
+                for (int c = 0; c < of; ++c) at += s.warp_word[c];
             }
-            return;
+            kept_units(b, at, w);
         }
-        in_front = __shfl_sync(0xffffffffu, to, 31);
+        const uint64_t here = (w[0] + w[1]) + (w[2] + w[3]), up_to = warp_scan_u64(here, lane);
+        if (round > run0) __syncthreads();
+        if (lane == 31) s.block[warp] = up_to;
+        __syncthreads();
+        uint64_t before = in_front;
+        for (int c = 0; c < warp; ++c) before += s.block[c];
+        const uint64_t to = before + up_to;
+        if (drawn >= to - here && drawn < to) {   // one lane of one warp
+            uint64_t at = to - here;
+            int i = 0;
+            for (; i < 3; ++i) {
+                at += w[i];
+                if (at > drawn) break;
+            }
+            emit(first + b * kBlock + lane * 4 + i, i == 0 ? w[0] : i == 1 ? w[1] : i == 2 ? w[2] : w[3], total);
+        }
+        for (int c = 0; c < kSampleWarps; ++c) in_front += s.block[c];
     }
 }
 
 constexpr int kMaxStretch = (227 * 1024 - (int)sizeof(SampleShared)) / 4 / kBlock * kBlock;
 static_assert((int64_t)kMaxStretch * kSampleRanks >= kMaxVocab + 8 + kSampleRanks * kBlock, "the largest vocabulary fits eight CTAs");
-static_assert(kSampleCtasPerSm * (sizeof(SampleShared) + 16128 * 4 + 1024) <= 228 * 1024, "three stretches of an eighth of 128256 logits fit an SM");
+static_assert(3 * (sizeof(SampleShared) + 16128 * 4 + 1024) <= 228 * 1024, "three stretches of an eighth of 128256 logits fit an SM");
 
 template <class F>
 cudaError_t for_each_sample(F f) {
-    cudaError_t e = f(sw_sample_kernel<float>);
-    if (e == cudaSuccess) e = f(sw_sample_kernel<__nv_bfloat16>);
-    if (e == cudaSuccess) e = f(sw_sample_kernel<__half>);
-    return e;
+    for (auto* kernel : {sw_sample_kernel<float, kFewSampleThreads>, sw_sample_kernel<float, kManySampleThreads>, sw_sample_kernel<__nv_bfloat16, kFewSampleThreads>,
+                         sw_sample_kernel<__nv_bfloat16, kManySampleThreads>, sw_sample_kernel<__half, kFewSampleThreads>, sw_sample_kernel<__half, kManySampleThreads>})
+        if (const cudaError_t e = f(kernel)) return e;
+    return cudaSuccess;
 }
 cudaError_t configure_sample_kernels() {
     return for_each_sample([](auto* kernel) {
@@ -773,6 +809,7 @@ cudaError_t launch_sample(const SampleParams& params, int dtype, int num_sms, cu
     int ranks = 1;
     while (ranks < kSampleRanks && (positions > ranks * 16384 || (p.rows * ranks < num_sms && positions > ranks * 2048))) ranks *= 2;
     p.stretch = (int)((positions + ranks * kBlock - 1) / (ranks * kBlock) * kBlock);
+    const bool many = p.rows * ranks <= num_sms && p.stretch >= 4 * kManySampleThreads;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -781,14 +818,15 @@ cudaError_t launch_sample(const SampleParams& params, int dtype, int num_sms, cu
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(p.rows * ranks));
-    cfg.blockDim = dim3(kSampleThreads);
+    cfg.blockDim = dim3(many ? kManySampleThreads : kFewSampleThreads);
     cfg.dynamicSmemBytes = sizeof(SampleShared) + (size_t)p.stretch * size;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return dtype == SW_DTYPE_F32    ? cudaLaunchKernelEx(&cfg, sw_sample_kernel<float>, p)
-           : dtype == SW_DTYPE_BF16 ? cudaLaunchKernelEx(&cfg, sw_sample_kernel<__nv_bfloat16>, p)
-                                    : cudaLaunchKernelEx(&cfg, sw_sample_kernel<__half>, p);
+    auto launch = [&](auto* few_kernel, auto* many_kernel) { return cudaLaunchKernelEx(&cfg, many ? many_kernel : few_kernel, p); };
+    if (dtype == SW_DTYPE_F32) return launch(sw_sample_kernel<float, kFewSampleThreads>, sw_sample_kernel<float, kManySampleThreads>);
+    if (dtype == SW_DTYPE_BF16) return launch(sw_sample_kernel<__nv_bfloat16, kFewSampleThreads>, sw_sample_kernel<__nv_bfloat16, kManySampleThreads>);
+    return launch(sw_sample_kernel<__half, kFewSampleThreads>, sw_sample_kernel<__half, kManySampleThreads>);
 }
 
 }  // namespace sw
