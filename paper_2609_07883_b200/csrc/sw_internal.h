@@ -128,7 +128,7 @@ struct RopeParams {
 struct SampleParams {
     const void* logits;   // [rows], row_stride elements apart
     int rows, vocab;
-    int stretch;          // logits of a CTA: the launcher's
+    int stretch, held;    // logits of a CTA, and 128s of them that each of its warps keeps in shared memory: the launcher's
     int64_t row_stride;
     const float *temperature, *top_p, *min_p, *uniform;
     const int32_t* top_k;

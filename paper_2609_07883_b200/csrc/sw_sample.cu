@@ -8,17 +8,19 @@
 // Weights are worked out in 64 bits (2^x from a table of 16 powers and a polynomial of degree five, 1e-14 off) and rounded to 2^-44 of the
 // largest; their sums are integers, exact in any order, and equal logits have equal weights.
 //
-// A cluster of 1 to 8 CTAs has a row; each CTA copies an equal stretch to shared memory, so logits are read from memory once.  Then
+// A cluster of 1 to 8 CTAs has a row, each CTA an equal stretch of it and each warp a run of that.  As much of the runs as there is room for is copied to shared
+// memory; the rest is read again where it is needed, from L2.  Then
 //   - the row's largest logit, and a cut above which some hundreds of logits lie: a quantile of the threads' largest ones (its median over warps and
 //     CTAs).  It only has to be about right;
-//   - without top-k and top-p, the sums of the weights of every warp's run of logits; the warp that the draw falls into looks for the token;
+//   - without top-k and top-p, the sums of the weights of every run; the CTA that the draw falls into looks for the token in one of its runs;
 //   - with them, the logits above the cut are collected in one CTA (another one for the next row; top-p: and all weights summed).  If the threshold lies among
 //     them, that CTA has the rest to itself: it keeps them in registers, finds the threshold by radix, 256 bins a pass with their number of logits and
 //     weight, and the token likewise, by index.  The others end;
-//   - if it does not (a large k, or weights spread over thousands of tokens), all CTAs search their stretches, and read one another's bins: first those
-//     above the cut, then 256 bins of equal width over the rest, then the bin that the threshold lies in.
-// Bound by the logits' bytes, by the instructions of a weight where all are needed (19 a logit, nine of them in 64 bits), and for a few rows by the
-// chain of two cluster barriers and the passes.
+//   - if it does not, and there is no top-k (weights spread over thousands of tokens): an eighth of the logits tell about where the threshold lies, the weights
+//     above three places around it where it lies to some hundreds of logits, and these are collected, and the threshold found among them, as before;
+//   - otherwise (a large k, logits of very unlike runs) all CTAs search their stretches by bins, and read one another's.
+// Bound by the logits' bytes, by the instructions of a weight where all are needed (some 20 a logit, nine of them in 64 bits, and a conversion), and for a
+// few rows by the chain of two cluster barriers and the passes.
 #include <cfloat>
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
@@ -29,32 +31,30 @@ namespace sw {
 namespace cg = cooperative_groups;
 
 constexpr int kSampleBins = 256, kSampleRanks = 8, kMaxWarps = 32;
-constexpr int kBlock = 128;   // logits that a warp takes at once
-constexpr int kListed = 144;  // logits collected from a CTA
+constexpr int kBlock = 128, kFar = 4;   // logits that a warp takes at once; such blocks outside shared memory that it loads at once
+constexpr int kListed = 128;  // logits collected from a CTA
 constexpr uint32_t kLowestKey = 0x00800000u;   // key_of() of the lowest finite number
 constexpr int kUnitBits = 44;                  // the largest weight is 2^44 units: sums of up to 2^19 of them fit 63 bits
 
 struct SampleShared {
     union {
         uint2 listed[kSampleRanks][kListed];   // the collecting CTA: logits above the cut, as bits, and their indices
-        struct {
-            uint32_t count[2][kSampleBins], low[2][kSampleBins], high[2][kSampleBins];   // by the parity of the pass: logits, and units in two halves
-            uint64_t weight[kSampleBins];                                                // summed over the cluster
-            uint32_t number[kSampleBins];                                                // likewise
-        } bins;
+        uint32_t bins[2][4][kSampleBins];   // by the parity of the pass: logits, and units in three parts of 15 bits
         uint64_t block[kMaxWarps];   // units of the blocks that the warps look through
     };
     uint2 mine[kListed];
     double power[16];   // (see Weigh)
-    uint64_t rank_total[kSampleRanks], rank_above[kSampleRanks], rank_kept[kSampleRanks], warp_sum[kMaxWarps];
+    uint64_t rank_total[kSampleRanks], rank_above[kSampleRanks], rank_kept[kSampleRanks], warp_sum[kMaxWarps], pick_w[8];
     float rank_top[kSampleRanks], rank_cut[kSampleRanks], warp_top[kMaxWarps], warp_cut[kMaxWarps];
-    uint32_t rank_listed[kSampleRanks], warp_word[kMaxWarps];
+    uint32_t rank_listed[kSampleRanks], warp_word[kMaxWarps], pick_n[8];
     struct Found {
         uint64_t above_w, w;   // units of what lies above the bin, and in it
         uint32_t above_n, n;
         int bin;               // -1: the target is not reached
     } found;
     uint32_t edge[2], num_mine;
+    uint32_t front[4];       // from the collecting CTA: keep, and the key in front of it with the last index that is kept of it
+    uint64_t rank_places[kSampleRanks][3];
     alignas(16) unsigned char x[];
 };
 
@@ -67,24 +67,31 @@ __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float
 
 // A logit's weight in units: 2^44 2^((x - max) c / 16) with x c to the nearest integer in the exponent and a table of 16 powers, the rest in a polynomial.
 // |x c| < 2^36: of large numbers, a temperature below that at which only the largest has a weight is not taken (below).
+// A sum with 2^52, and with such sums up to 2^53, is rounded to an integer: so the weight is added as it is rounded.
 struct Weigh {
     double c;             // 16 / ln 2 / temperature
     double shift;         // 1.5 2^52 less the largest logit's c, rounded: a sum with it is rounded to an integer, which its low word holds
     float floor;          // weights below 2^-64 are none
-    const double* power;  // 2^(44 + (j - f) / 16), f what was rounded off the largest logit's c
-    static constexpr uint64_t kZero = 0x4330000000000000ull;   // bits of 2^52: a sum with it is rounded likewise
+    const double* power;  // 2^(44 + (j - f) / 16), f what was rounded off the largest logit's c; j 2^48 less, as integers
+    static constexpr double kZero = 4503599627370496.0;   // 2^52
     static __device__ __forceinline__ double power_of(double f) {   // 2^(f / 16), |f| <= 1/2, to 4.5e-15
         return fma(fma(fma(fma(fma(1.2715658865126869e-09, f, 1.4676444610409443e-07), f, 1.3550807790817295e-05), f, 0.0009383847924862347), f,
                        0.043321698784995775), f, 1.0000000000000044);
     }
-    __device__ __forceinline__ uint64_t bits(float x) const {  // kZero + units
+    __device__ __forceinline__ void factors(float x, double& a, double& b) const {
         const double d = (double)fmaxf(x, floor), r = fma(d, c, shift), f = fma(d, c, shift - r);   // (NaN: the floor)
         const int n = __double2loint(r);
-        const double q = power_of(f);
         const double s = power[n & 15];
-        return (uint64_t)__double_as_longlong(fma(q, __hiloint2double(__double2hiint(s) + (n & ~15) * 0x10000, __double2loint(s)), 4503599627370496.0));
+        a = power_of(f);
+        b = __hiloint2double(__double2hiint(s) + n * 0x10000, __double2loint(s));
     }
-    __device__ __forceinline__ uint64_t operator()(float x) const { return bits(x) - kZero; }
+    __device__ __forceinline__ double add(float x, double sum) const {   // sum: kZero and units
+        double a, b;
+        factors(x, a, b);
+        return fma(a, b, sum);
+    }
+    static __device__ __forceinline__ uint64_t units(double sum) { return (uint64_t)(__double_as_longlong(sum) - __double_as_longlong(kZero)); }
+    __device__ __forceinline__ uint64_t operator()(float x) const { return units(add(x, kZero)); }
 };
 
 // share * total, rounded down or up from the exact product (a share of 24 bits times 63); share in [0, 1).
@@ -154,9 +161,9 @@ __device__ __forceinline__ float load_logit(const __half* x) { return __half2flo
 // Logits whose keys lie in [lo, hi], in 256 bins: of 2^shift keys each, or (linear) of equal width from x_lo on.
 struct Interval {
     uint32_t lo, hi;
-    int shift;
+    int shift = 0;
     bool linear;
-    float x_lo, per;
+    float x_lo = 0.f, per = 0.f;
     __device__ __forceinline__ int bin(float x, uint32_t key) const {
         return linear ? min(kSampleBins - 1, max(0, (int)((x - x_lo) * per))) : (int)((key - lo) >> shift);
     }
@@ -164,47 +171,51 @@ struct Interval {
         lo = l, hi = h, linear = false;
         shift = max(0, 24 - __clz(h - l));   // (256 << shift > h - l)
     }
+    __device__ __forceinline__ void over(uint32_t l, uint32_t h, float floor) {   // what lies below `floor` is in the first bin
+        lo = l, hi = h, linear = true;
+        x_lo = fmaxf(floor, value_of(l));
+        per = (float)kSampleBins / fmaxf(value_of(h) - x_lo, 1e-30f);
+    }
 };
 
-// The bin in which what lies above it, from above_n logits and above_w units on, reaches the target.  One warp; number(i) and weight(i) of bin i.
-template <class N, class W>
-__device__ __forceinline__ SampleShared::Found pick_bin(N number, W weight, uint64_t above_n, uint64_t above_w, bool by_weight, uint64_t target, int lane) {
-    // lane l has bins 255 - 8 l down to 248 - 8 l
-    uint64_t n = 0, w = 0;
+// What runs once or twice a row is not inlined: the kernel's code is fetched line by line where it runs for the first time, and with all of this in it
+// several times over a row took 3 to 6 us longer.
+__device__ __noinline__ uint64_t units_once(double c, double shift, float floor, const double* power, float x) { return Weigh{c, shift, floor, power}(x); }
+
+// The bin, from the highest on, in which what lies above, above_n logits and above_w units included, reaches the target.  Thread i < 256 brings the
+// n logits and w units of bin 255 - i.
+__device__ __noinline__ void pick(SampleShared& s, uint32_t n, uint64_t w, uint32_t above_n, uint64_t above_w, bool by_weight, uint64_t target) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint32_t n_to = n;
+    uint64_t w_to = w;
+    if (warp < 8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        n += number(kSampleBins - 1 - lane * 8 - i);
-        w += weight(kSampleBins - 1 - lane * 8 - i);
-    }
-    const uint64_t n_to = above_n + warp_scan_u64(n, lane), w_to = above_w + warp_scan_u64(w, lane);
-    const unsigned reached = __ballot_sync(0xffffffffu, (by_weight ? w_to : n_to) >= target);
-    n = n_to - n;
-    w = w_to - w;
-    SampleShared::Found f;
-    f.bin = -1;
-    f.n = 0;
-    f.w = 0;
-    const int last = reached ? __ffs(reached) - 1 : 31;
-    if (lane == last) {
-        for (int i = 0; i < 8 && f.bin < 0; ++i) {
-            const int at = kSampleBins - 1 - lane * 8 - i;
-            const uint64_t n1 = number(at), w1 = weight(at);
-            if (reached && (by_weight ? w + w1 : n + n1) >= target) {
-                f.bin = at;
-                f.n = (uint32_t)n1;
-                f.w = w1;
-            } else {
-                n += n1;
-                w += w1;
-            }
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t a = __shfl_up_sync(0xffffffffu, n_to, o);
+            const uint64_t b = __shfl_up_sync(0xffffffffu, w_to, o);
+            if (lane >= o) n_to += a, w_to += b;
         }
-        f.above_n = (uint32_t)n;
-        f.above_w = w;
+        if (lane == 31) s.pick_n[warp] = n_to, s.pick_w[warp] = w_to;
     }
-    return f;   // (of lane `last`; the caller keeps that one's)
+    __syncthreads();
+    if (warp < 8) {
+        n_to += above_n;
+        w_to += above_w;
+        for (int i = 0; i < warp; ++i) n_to += s.pick_n[i], w_to += s.pick_w[i];
+        const uint64_t to = by_weight ? w_to : n_to, before = by_weight ? w_to - w : n_to - n;
+        if (before < target && (to >= target || tid == kSampleBins - 1)) {
+            const bool here = to >= target;
+            s.found.bin = here ? kSampleBins - 1 - tid : -1;
+            s.found.n = here ? n : 0;
+            s.found.w = here ? w : 0;
+            s.found.above_n = here ? n_to - n : n_to;
+            s.found.above_w = here ? w_to - w : w_to;
+        }
+    }
+    __syncthreads();
 }
 
-// Threads of a CTA, and CTAs an SM: small ones that work while others load, or large ones where no SM gets a second.
+// Threads of a CTA: few, three CTAs an SM, that work while others load, or many where no SM gets a second CTA.
 constexpr int kManySampleThreads = 1024, kFewSampleThreads = 256;
 template <class T, int kSampleThreads>
 __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleThreads ? 3 : 1) sw_sample_kernel(const SampleParams p) {
@@ -224,18 +235,25 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
 
     // ---- the row's logits to shared memory, and its settings ----
     // Position i of the stretch is logit first + i; the row's first logit lies `-first` past a 16-byte boundary in CTA 0.
-    constexpr int kN = 16 / sizeof(T);
-    const T* logits = static_cast<const T*>(p.logits) + row * p.row_stride;
+    const T* const logits = static_cast<const T*>(p.logits) + row * p.row_stride;
     const int first = rank * p.stretch - (int)((reinterpret_cast<uintptr_t>(logits) & 15) / sizeof(T));
-    for (int v = tid; v < p.stretch / kN; v += kSampleThreads) {
-        const int e = first + v * kN;
-        if (e >= 0 && e + kN <= p.vocab) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(x + v * kN)), "l"(logits + e) : "memory");
+    // A warp's run: blocks [block0, block0 + run) of the stretch, the first `held` of them in shared memory.
+    const int blocks = p.stretch / kBlock, block0 = blocks * warp / kSampleWarps, run = blocks * (warp + 1) / kSampleWarps - block0;
+    const int held = p.held;
+    const int from_e = first + block0 * kBlock + lane * 4;   // this lane's first logit
+    T* const x_lane = x + warp * held * kBlock + lane * 4;
+    // whether all of block j of the run are logits of the row
+    auto inside = [&](int e0) { return e0 >= 0 && e0 + kBlock <= p.vocab; };
+    for (int j = 0; j < min(held, run); ++j) {
+        const int e = from_e + j * kBlock;
+        if (inside(first + (block0 + j) * kBlock)) {
+            if constexpr (sizeof(T) == 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(x_lane + j * kBlock)), "l"(logits + e) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(x_lane + j * kBlock)), "l"(logits + e) : "memory");
         } else {
 #pragma unroll
-            for (int i = 0; i < kN; ++i) {
-                if (e + i >= 0 && e + i < p.vocab) x[v * kN + i] = logits[e + i];
-                else store_logit(&x[v * kN + i], -INFINITY);
+            for (int i = 0; i < 4; ++i) {
+                if (e + i >= 0 && e + i < p.vocab) x_lane[j * kBlock + i] = logits[e + i];
+                else store_logit(&x_lane[j * kBlock + i], -INFINITY);
             }
         }
     }
@@ -247,31 +265,84 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
     const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f, uniform = p.uniform[row];
     const double usual_c = 16. * 1.4426950408889634 / (double)temperature;
     const bool greedy = !(temperature > 0.f), by_count = !greedy && top_k > 0 && top_k < p.vocab, by_share = !greedy && top_p < 1.f;
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    __syncthreads();
-    const int blocks = p.stretch / kBlock, block0 = blocks * warp / kSampleWarps, block1 = blocks * (warp + 1) / kSampleWarps;   // of this warp
+    bool infinite = false;
+    // this lane's four logits of block j of warp w's run
+    auto quad_at = [&](int w, int j, float (&v)[4]) {
+        const int b = blocks * w / kSampleWarps + j, e0 = first + b * kBlock, e = e0 + lane * 4;
+        if (j < held || inside(e0)) {
+            quad_of(j < held ? x + (w * held + j) * kBlock + lane * 4 : logits + e, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = e + i >= 0 && e + i < p.vocab ? load_logit(logits + e + i) : -INFINITY;
+        }
+        if (infinite && j >= held) {   // the infinite ones share the draw
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = v[i] == INFINITY ? 0.f : -INFINITY;
+        }
+    };
+    auto far_quad = [&](int j, float (&v)[4]) {
+        const int e0 = first + (block0 + j) * kBlock, e = from_e + j * kBlock;
+        if (inside(e0)) {
+            quad_of(logits + e, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = e + i >= 0 && e + i < p.vocab ? load_logit(logits + e + i) : -INFINITY;
+        }
+        if (infinite) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = v[i] == INFINITY ? 0.f : -INFINITY;
+        }
+    };
+    // f(j, v) for every block of the warp's run; those in shared memory first, and without looking where they lie (which doubles what a weight costs)
+    const int near = min(held, run);
+    auto for_blocks = [&](auto f) {
+#pragma unroll 2
+        for (int j = 0; j < near; ++j) {
+            float v[4];
+            quad_of(x_lane + j * kBlock, v);
+            f(j, v);
+        }
+#pragma unroll 1
+        for (int j = near; j < run; j += kFar) {   // (the loads of a few blocks at once)
+            float v[kFar][4];
+#pragma unroll
+            for (int i = 0; i < kFar; ++i)
+                if (j + i < run) far_quad(j + i, v[i]);
+#pragma unroll
+            for (int i = 0; i < kFar; ++i)
+                if (j + i < run) f(j + i, v[i]);
+        }
+    };
 
     // ---- the largest logit, and the cut ----
     float top = -INFINITY;
 #pragma unroll 4
-    for (int b = block0; b < block1; ++b) {
+    for (int j = near; j < run; ++j) {
         float v[4];
-        quad_of(x + b * kBlock + lane * 4, v);
+        far_quad(j, v);
         top = max3(max3(top, v[0], v[1]), v[2], v[3]);
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncwarp();   // (a warp copies its own run)
+#pragma unroll 4
+    for (int j = 0; j < near; ++j) {
+        float v[4];
+        quad_of(x_lane + j * kBlock, v);
+        top = max3(max3(top, v[0], v[1]), v[2], v[3]);
+    }
+    top = fmaxf(top, -INFINITY);   // (NaN where all are)
     if (by_count || by_share) {
-        // the warp's 32 tops in falling order
-#pragma unroll
-        for (int k = 2; k <= 32; k <<= 1)
-#pragma unroll
-            for (int j = k >> 1; j > 0; j >>= 1) {
-                const float o = __shfl_xor_sync(0xffffffffu, top, j);
-                top = ((lane & j) == 0) == ((lane & k) == 0) ? fmaxf(top, o) : fminf(top, o);
-            }
-        // With `want` logits above the cut, a share of 1 - exp(-want / threads) of the threads' tops is.
-        const float want = by_count ? fmaxf(256.f, 1.5f * (float)top_k + 64.f) : 512.f;
+        // With `want` logits above the cut, a share of 1 - exp(-want / threads) of the threads' tops is: the warp's q-th largest one of 32, from 0 on.
+        const float want = by_count ? fmaxf(192.f, 1.5f * (float)top_k + 64.f) : 512.f;
         const int q = min(31, (int)(32.f * (1.f - __expf(-want / (float)(ranks * kSampleThreads)))));
-        const float cut = __shfl_sync(0xffffffffu, top, q);
+        uint32_t key = key_of(top), most = __reduce_max_sync(0xffffffffu, key);
+        top = value_of(most);
+#pragma unroll 1
+        for (int i = 0; i < q; ++i) {
+            if (lane == __ffs(__ballot_sync(0xffffffffu, key == most)) - 1) key = 0;
+            most = __reduce_max_sync(0xffffffffu, key);
+        }
+        const float cut = value_of(max(most, key_of(-INFINITY)));
         if (lane == 0) s.warp_top[warp] = top, s.warp_cut[warp] = cut;
     } else {
 #pragma unroll
@@ -280,8 +351,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
     }
     __syncthreads();
     if (warp == 0) {
-        float t = lane < kSampleWarps ? s.warp_top[lane] : -INFINITY;
-        float cut = 0.f;
+        float t = lane < kSampleWarps ? s.warp_top[lane] : -INFINITY, cut = 0.f;
         if (by_count || by_share) cut = lanes_rank(lane < kSampleWarps ? s.warp_cut[lane] : -INFINITY, kSampleWarps, min(kSampleWarps, blocks) / 2, lane);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
@@ -307,12 +377,13 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
     if (greedy) {   // the first CTA with that logit has the token
         if (__ffs(__ballot_sync(0xffffffffu, rank_top == m)) - 1 != rank) return;
         uint32_t at = 0xffffffffu;
-        for (int b = block0; b < block1; ++b) {
+#pragma unroll 1
+        for (int j = 0; j < run; ++j) {
             float v[4];
-            quad_of(x + b * kBlock + lane * 4, v);
+            quad_at(warp, j, v);
 #pragma unroll
             for (int i = 3; i >= 0; --i)
-                if (v[i] == m) at = min(at, (uint32_t)(first + b * kBlock + lane * 4 + i));
+                if (v[i] == m) at = min(at, (uint32_t)(from_e + j * kBlock + i));
         }
         at = __reduce_min_sync(0xffffffffu, at);
         if (lane == 0) s.warp_word[warp] = at;
@@ -328,10 +399,12 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
     }
     float cut = 0.f;
     if (by_count || by_share) cut = lanes_rank(lane < ranks ? s.rank_cut[lane] : -INFINITY, ranks, ranks / 2, lane);
-    if (m == INFINITY) {   // the infinite ones share the draw
-        for (int i = tid; i < p.stretch; i += kSampleThreads) store_logit(&x[i], load_logit(&x[i]) == INFINITY ? 0.f : -INFINITY);
+    if (m == INFINITY) {
+        infinite = true;
         m = cut = 0.f;
-        __syncthreads();
+        for (int j = 0; j < near; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) store_logit(&x_lane[j * kBlock + i], load_logit(&x_lane[j * kBlock + i]) == INFINITY ? 0.f : -INFINITY);
     }
 
     // Temperatures at which no number but the largest logit has a weight are all alike: the next one lies 2^-24 of it below at least, and here 128 times the
@@ -342,41 +415,43 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
     weigh.c = t == temperature ? usual_c : 16. * 1.4426950408889634 / (double)t;
     const double top_c = rint((double)m * weigh.c);
     weigh.shift = 6755399441055744.0 - top_c;
-    if (tid < 16) s.power[tid] *= Weigh::power_of(top_c - (double)m * weigh.c);
+    if (tid < 16) {
+        const double power = s.power[tid] * Weigh::power_of(top_c - (double)m * weigh.c);
+        s.power[tid] = __hiloint2double(__double2hiint(power) - tid * 0x10000, __double2loint(power));
+    }
     weigh.floor = fmaxf(fminf(below, m - 44.3614f * t), -FLT_MAX);   // 64 ln 2
     weigh.power = s.power;
-    __syncthreads();
     const bool low = weigh.floor == -FLT_MAX;   // then minus infinity and NaN have to be told from the floor
-    const uint64_t least = min_p > 0.f ? (uint64_t)ceil((double)fminf(min_p, 1.f) * (double)weigh(m)) : 0;
+    __syncthreads();
+    const uint64_t least = min_p > 0.f ? (uint64_t)ceil((double)fminf(min_p, 1.f) * (double)units_once(weigh.c, weigh.shift, weigh.floor, weigh.power, m)) : 0;
     auto block_sum = [&](uint64_t v) {   // (a barrier before the next one)
         v = warp_sum_u64(v);
         if (lane == 0) s.warp_sum[warp] = v;
         __syncthreads();
         return warp_sum_u64(lane < kSampleWarps ? s.warp_sum[lane] : 0);
     };
-    // the units of the warp's run of logits, this lane's part
-    auto all_units = [&] {
-        uint64_t sum = 0;
-#pragma unroll 2
-        for (int b = block0; b < block1; ++b) {
-            float v[4];
-            quad_of(x + b * kBlock + lane * 4, v);
-            uint64_t w[4];
+    // Adds four logits' units to four sums (of a run of 2^8 blocks at most, less than 2^52 units each).
+    auto add_units = [&](const float (&v)[4], double (&sum)[4]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = weigh.bits(v[i]);
-            if (low) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = v[i] > -INFINITY ? w[i] : Weigh::kZero;
-            }
-            sum += (w[0] + w[1]) + (w[2] + w[3]);
+        for (int i = 0; i < 4; ++i) {
+            const double to = weigh.add(v[i], sum[i]);
+            sum[i] = !low || v[i] > -INFINITY ? to : sum[i];
         }
-        return sum - (uint64_t)(4 * (block1 - block0)) * Weigh::kZero;
     };
+    auto units_of = [&](const double (&sum)[4]) { return (Weigh::units(sum[0]) + Weigh::units(sum[1])) + (Weigh::units(sum[2]) + Weigh::units(sum[3])); };
+    // (Parts whose sums over a stretch fit 32 bits: a sum in two halves needs what was there before for its carry, and waits for it.)
     auto add_to_bin = [&](int buf, int at, uint64_t u) {
-        atomicAdd(&s.bins.count[buf][at], 1u);
-        const uint32_t lo = (uint32_t)u, old = atomicAdd(&s.bins.low[buf][at], lo), hi = (uint32_t)(u >> 32) + (old + lo < old);
-        if (hi) atomicAdd(&s.bins.high[buf][at], hi);
+        atomicAdd(&s.bins[buf][0][at], 1u);
+        atomicAdd(&s.bins[buf][1][at], (uint32_t)u & 0x7fffu);
+        atomicAdd(&s.bins[buf][2][at], (uint32_t)(u >> 15) & 0x7fffu);
+        if (u >> 30) atomicAdd(&s.bins[buf][3][at], (uint32_t)(u >> 30));
     };
+    auto clear_bins = [&](int buf) {
+        if (tid < kSampleBins)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s.bins[buf][i][tid] = 0;
+    };
+    auto units_at = [&](float v) { return units_once(weigh.c, weigh.shift, weigh.floor, weigh.power, v); };
     auto emit = [&](int token, uint64_t units, uint64_t total) {
         p.tokens[row] = token;
         if (p.log_probs) p.log_probs[row] = (float)log((double)units / (double)total);
@@ -388,34 +463,39 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
     };
 
     uint32_t keep = kLowestKey, tie_key = 0, ties = 0, tie_before = 0;   // kept: keys from `keep` on, and the first `ties` logits of the key in front of it
-    uint64_t all = 0;
+    int tie_to = -1;   // or those up to this index, whatever their number
     if (by_count || by_share) {
         // ---- the logits above the cut, collected in one CTA ----
-        uint64_t total = by_share && !by_count ? all_units() : 0, above = 0;
-#pragma unroll 2
-        for (int b = block0; b < block1; ++b) {
-            float v[4];
-            quad_of(x + b * kBlock + lane * 4, v);
-            if (!(max4(v) >= cut)) continue;
+        uint64_t total = 0, above = 0;
+        auto list = [&](const float (&v)[4], int j) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (v[i] >= cut && v[i] > -INFINITY) {
                     const uint32_t at = atomicAdd(&s.num_mine, 1u);
-                    if (at < kListed) s.mine[at] = make_uint2(__float_as_uint(v[i]), (uint32_t)(first + b * kBlock + lane * 4 + i));
-                    if (by_share && !by_count) above += weigh(v[i]);
+                    if (at < kListed) s.mine[at] = make_uint2(__float_as_uint(v[i]), (uint32_t)(from_e + j * kBlock + i));
                 }
-        }
+        };
         if (by_share && !by_count) {
-            total = block_sum(total);
-            __syncthreads();
-            above = block_sum(above);
+            double sums[4] = {Weigh::kZero, Weigh::kZero, Weigh::kZero, Weigh::kZero};
+            for_blocks([&](int j, const float (&v)[4]) {
+                add_units(v, sums);
+                if (max4(v) >= cut) list(v, j);
+            });
+            total = block_sum(units_of(sums));
         } else {
-            __syncthreads();
+            for_blocks([&](int j, const float (&v)[4]) {
+                if (max4(v) >= cut) list(v, j);
+            });
         }
+        __syncthreads();
         const int collector = row % ranks;
         const uint32_t listed = s.num_mine;
-        SampleShared* to = cluster.map_shared_rank(&s, collector);
-        if (tid < min(listed, (uint32_t)kListed)) to->listed[rank][tid] = s.mine[tid];
+        if (tid < min(listed, (uint32_t)kListed)) {
+            const uint2 e = s.mine[tid];
+            cluster.map_shared_rank(&s, collector)->listed[rank][tid] = e;
+            if (!by_count) above = units_at(__uint_as_float(e.x));
+        }
+        if (!by_count) above = block_sum(above);   // (of those that are listed)
         if (warp == 0 && lane < ranks) {
             SampleShared* peer = cluster.map_shared_rank(&s, lane);
             peer->rank_listed[rank] = listed;
@@ -423,17 +503,143 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
             peer->rank_above[rank] = above;
         }
         all_here();
-        uint32_t n = 0, most = 0;
-        above = 0;
-        for (int r = 0; r < ranks; ++r) {
-            n += s.rank_listed[r];
-            most = max(most, s.rank_listed[r]);
-            all += s.rank_total[r];
-            above += s.rank_above[r];
+        uint32_t n = lane < ranks ? s.rank_listed[lane] : 0;
+        const bool fits = __all_sync(0xffffffffu, n <= kListed);
+        n = __reduce_add_sync(0xffffffffu, n);
+        uint64_t all = 0, target = top_k;
+        if (!by_count) {
+            all = warp_sum_u64(lane < ranks ? s.rank_total[lane] : 0);
+            above = warp_sum_u64(lane < ranks ? s.rank_above[lane] : 0);
+            target = max((uint64_t)1, share_of(fmaxf(top_p, 0.f), all, true));
         }
-        uint64_t target = by_count ? (uint64_t)top_k : max((uint64_t)1, share_of(fmaxf(top_p, 0.f), all, true));
-        if (most <= kListed && (by_count ? n : above) >= target) {
-            if (rank != collector) return;
+        const bool direct = fits && (by_count ? n : above) >= target;
+        bool listed_window = false;
+        uint32_t low_key = min(key_of(cut), m_key);   // of what is collected
+        if (direct && rank != collector) return;
+        if (!direct && fits && !by_count && cut > -FLT_MAX) {
+            // -- about where the threshold lies: an eighth of the blocks below the cut, in 256 bins of equal width
+            Interval iv;
+            iv.over(kLowestKey, max(key_of(cut), kLowestKey + 1) - 1, weigh.floor);
+            __syncthreads();
+            clear_bins(0);
+            __syncthreads();
+            const int step = min(8, max(2, run));
+            const float first_v = value_of(iv.lo);
+#pragma unroll 1
+            for (int j = step / 2; j < run; j += step) {
+                float v[4];
+                quad_at(warp, j, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (v[i] >= first_v && v[i] < cut) atomicAdd(&s.bins[0][0][iv.bin(v[i], 0)], (uint32_t)(units_at(v[i]) >> 24));
+            }
+            all_here();
+            uint64_t w = 0;
+            if (tid < kSampleBins) {
+                uint32_t part[kSampleRanks];
+#pragma unroll
+                for (int r = 0; r < kSampleRanks; ++r) part[r] = cluster.map_shared_rank(&s, min(r, ranks - 1))->bins[0][0][kSampleBins - 1 - tid];
+#pragma unroll
+                for (int r = 0; r < kSampleRanks; ++r) w += r < ranks ? part[r] : 0;
+            }
+            pick(s, 0, w, 0, 0, true, ~0ull);   // (everything)
+            const double sampled = (double)s.found.above_w, rest = (double)(all - above);
+            pick(s, 0, w, 0, 0, true, (uint64_t)fmax(1., fmin(sampled, ceil(sampled * ((double)(target - above) / rest)))));
+            const auto f = s.found;
+            listed_window = sampled > 0. && f.bin >= 0 && f.w > 0;
+            if (listed_window) {   // (the same in all CTAs)
+                const double in_bin = (sampled * ((double)(target - above) / rest) - (double)f.above_w) / (double)f.w;
+                const double density = (double)f.w / sampled * rest * (double)iv.per;   // units per unit of x
+                // -- the units above three places, a fiftieth of the rest apart
+                const float apart = (float)(0.02 * rest / density), mid = iv.x_lo + ((float)(f.bin + 1) - (float)in_bin) / iv.per;
+                const float place[3] = {fminf(mid + apart, cut), mid, fmaxf(mid - apart, -FLT_MAX)};
+                double sums[3][2];
+#pragma unroll
+                for (int i = 0; i < 3; ++i) sums[i][0] = sums[i][1] = Weigh::kZero;
+#pragma unroll 1
+                for (int j = 0; j < run; ++j) {
+                    float v[4];
+                    if (j < held) quad_of(x_lane + j * kBlock, v);
+                    else quad_at(warp, j, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        double a, b;
+                        weigh.factors(v[i], a, b);
+#pragma unroll
+                        for (int c = 0; c < 3; ++c) {
+                            const double to = fma(a, b, sums[c][i & 1]);
+                            sums[c][i & 1] = v[i] >= place[c] ? to : sums[c][i & 1];
+                        }
+                    }
+                }
+                uint64_t sum[3];
+#pragma unroll
+                for (int c = 0; c < 3; ++c) {
+                    __syncthreads();
+                    sum[c] = block_sum(Weigh::units(sums[c][0]) + Weigh::units(sums[c][1]));
+                }
+                if (warp == 0 && lane < ranks) {
+                    SampleShared* peer = cluster.map_shared_rank(&s, lane);
+#pragma unroll
+                    for (int c = 0; c < 3; ++c) peer->rank_places[rank][c] = sum[c];
+                }
+                if (tid == 0) s.num_mine = 0;
+                all_here();
+                double miss[3];   // units by which the target lies further
+#pragma unroll
+                for (int c = 0; c < 3; ++c) miss[c] = (double)(int64_t)(target - warp_sum_u64(lane < ranks ? s.rank_places[lane][c] : 0));
+                // the place where nothing is missed, by the parabola through the three; within their width either way
+                const double d01 = (place[1] - place[0]) / (miss[1] - miss[0]), d12 = (place[2] - place[1]) / (miss[2] - miss[1]);
+                const double d012 = (d12 - d01) / (miss[2] - miss[0]);
+                double at = place[0] - miss[0] * d01 + miss[0] * miss[1] * d012;
+                if (!(at > place[2] - apart)) at = place[2] - apart;
+                if (!(at < place[0] + apart)) at = place[0] + apart;
+                // -- some hundreds of logits around it, and the units above them
+                const double each = (double)units_at((float)at) + 1., wide = 320. * each / fmax(density, 1.);
+                const float hi_v = (float)(at + wide), lo_v = fminf((float)(at - wide), hi_v);
+                sums[0][0] = sums[0][1] = Weigh::kZero;
+#pragma unroll 1
+                for (int j = 0; j < run; ++j) {
+                    float v[4];
+                    if (j < held) quad_of(x_lane + j * kBlock, v);
+                    else quad_at(warp, j, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const double to = weigh.add(v[i], sums[0][i & 1]);
+                        sums[0][i & 1] = v[i] > hi_v ? to : sums[0][i & 1];
+                        if (v[i] >= lo_v && v[i] <= hi_v && v[i] > -INFINITY) {
+                            const uint32_t to_at = atomicAdd(&s.num_mine, 1u);
+                            if (to_at < kListed) s.mine[to_at] = make_uint2(__float_as_uint(v[i]), (uint32_t)(from_e + j * kBlock + i));
+                        }
+                    }
+                }
+                sum[0] = block_sum(Weigh::units(sums[0][0]) + Weigh::units(sums[0][1]));
+                const uint32_t mine = s.num_mine;
+                uint64_t mine_w = 0;
+                if (tid < min(mine, (uint32_t)kListed)) {
+                    const uint2 e = s.mine[tid];
+                    cluster.map_shared_rank(&s, collector)->listed[rank][tid] = e;
+                    mine_w = units_at(__uint_as_float(e.x));
+                }
+                __syncthreads();
+                mine_w = block_sum(mine_w);
+                if (warp == 0 && lane < ranks) {
+                    SampleShared* peer = cluster.map_shared_rank(&s, lane);
+                    peer->rank_listed[rank] = mine;
+                    peer->rank_total[rank] = sum[0];
+                    peer->rank_above[rank] = mine_w;
+                }
+                all_here();
+                const uint64_t over = warp_sum_u64(lane < ranks ? s.rank_total[lane] : 0), among = warp_sum_u64(lane < ranks ? s.rank_above[lane] : 0);
+                const bool all_listed = __all_sync(0xffffffffu, lane >= ranks || s.rank_listed[lane] <= kListed);
+                listed_window = all_listed && over < target && over + among >= target;
+                if (listed_window) {
+                    target -= over;
+                    low_key = key_of(lo_v);
+                }
+            }
+        }
+        if ((direct || listed_window) && rank == collector) {
             uint32_t key[kHeld], order[kHeld];   // order: falls with the index
             uint64_t units[kHeld];
             unsigned live = 0;
@@ -446,181 +652,222 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
                     const uint2 e = s.listed[r][at - r * kListed];
                     key[i] = key_of(__uint_as_float(e.x));
                     order[i] = ~e.y;
-                    units[i] = weigh(__uint_as_float(e.x));
+                    units[i] = units_at(__uint_as_float(e.x));
                     live |= 1u << i;
                 }
             }
-            // Of the held logits in `of`, by falling `k`: leaves in `of` those in front of and in the bin where the target is reached, and in f what
-            // that bin is; it has one logit, or one k, or (by number) it is kept whole.
-            auto descend = [&](const uint32_t (&k)[kHeld], unsigned& of, uint32_t lo, uint32_t hi, bool by_weight, uint64_t target, uint32_t& bin_lo,
-                               uint32_t& bin_hi) {
-                uint64_t above_n = 0, above_w = 0;
-                for (;;) {
-                    const int shift = max(0, 24 - __clz(hi - lo));
-                    __syncthreads();
-                    if (tid < kSampleBins) s.bins.count[0][tid] = s.bins.low[0][tid] = s.bins.high[0][tid] = 0;
-                    __syncthreads();
+            __syncthreads();
+            clear_bins(0);
+            auto live_units = [&](unsigned of) {
+                uint64_t sum = 0;
 #pragma unroll
-                    for (int i = 0; i < kHeld; ++i)
-                        if (of >> i & 1 && k[i] >= lo && k[i] <= hi) add_to_bin(0, (int)((k[i] - lo) >> shift), units[i]);
-                    __syncthreads();
-                    if (warp == 0) {
-                        const auto f = pick_bin([&](int i) { return s.bins.count[0][i]; },
-                                                [&](int i) { return ((uint64_t)s.bins.high[0][i] << 32) + s.bins.low[0][i]; }, above_n, above_w, by_weight, target, lane);
-                        if (f.bin >= 0) s.found = f;
-                    }
-                    __syncthreads();
-                    const auto f = s.found;
-                    above_n = f.above_n;
-                    above_w = f.above_w;
-                    const uint32_t bin_at = lo + ((uint32_t)f.bin << shift);
-                    hi = bin_at + min(hi - bin_at, (1u << shift) - 1);
-                    lo = bin_at;
-                    if (lo == hi || f.n == 1 || (!by_weight && above_n + f.n == target)) {
+                for (int i = 0; i < kHeld; ++i)
+                    if (of >> i & 1) sum += units[i];
+                __syncthreads();
+                return block_sum(sum);
+            };
+            // Five steps of one kind: of some logits, in falling order of their key or of `order`, those are left that reach a target of number or weight.
+            // 0: top-k; 1: of equal ones at its threshold the first; 2, 3: top-p likewise; 4: the token, the last of those that the draw takes to reach.
+            uint64_t kept = 0;   // units of what is left (0: not known)
+            unsigned equal = 0;
+#pragma unroll 1
+            for (int step = by_count ? 0 : 2; step < (direct ? 5 : 4); ++step) {
+                if (step == 0 && n <= (uint32_t)top_k) step = 2;
+                if (step == 2) {
+                    if (by_count && by_share) target = max((uint64_t)1, share_of(fmaxf(top_p, 0.f), kept ? kept : live_units(live), true));
+                    if (!by_share) step = 4;
+                }
+                if (step == 4) {
+                    if (least > 0) {
+                        kept = 0;
 #pragma unroll
                         for (int i = 0; i < kHeld; ++i)
-                            if (k[i] < lo) of &= ~(1u << i);
-                        bin_lo = lo;
-                        bin_hi = hi;
-                        return f;
+                            if (units[i] < least) live &= ~(1u << i);
                     }
+                    if (kept == 0) kept = live_units(live);
+                    target = draw_of(kept) + 1;
                 }
-            };
-            // Keeps the front part of the live logits that reaches the target; of equal ones the first.
-            auto cut_to = [&](bool by_weight, uint64_t target) {
-                uint32_t lo, hi;
-                const auto f = descend(key, live, min(key_of(cut), m_key), m_key, by_weight, target, lo, hi);
-                const uint32_t n = by_weight ? (f.w == 0 ? f.n : (uint32_t)min((uint64_t)f.n, (target - f.above_w + f.w / f.n - 1) / (f.w / f.n)))
-                                             : (uint32_t)(target - f.above_n);
-                if (n == f.n) return;
-                unsigned equal = 0;   // (all of one key)
+                const bool by_index = step == 1 || step >= 3, by_weight = step == 2 || step == 4;
+                uint32_t lo = by_index ? ~(uint32_t)(p.vocab - 1) : low_key, hi = by_index ? ~0u : m_key, above_n = 0;
+                uint64_t above_w = 0;
+                unsigned of = step == 1 || step == 3 ? equal : live;
+                SampleShared::Found f;
+#pragma unroll 1
+                for (;;) {   // 256 bins a pass, until the one where the target is reached has one logit, or one key, or (by number) is kept whole
+                    const int shift = max(0, 24 - __clz(hi - lo));
+                    __syncthreads();
+#pragma unroll
+                    for (int i = 0; i < kHeld; ++i) {
+                        const uint32_t k = by_index ? order[i] : key[i];
+                        if (of >> i & 1 && k >= lo && k <= hi) add_to_bin(0, (int)((k - lo) >> shift), units[i]);
+                    }
+                    __syncthreads();
+                    uint32_t bin_n = 0;
+                    uint64_t bin_w = 0;
+                    if (tid < kSampleBins) {   // (and the bin is ready for the next pass)
+                        const int at = kSampleBins - 1 - tid;
+                        bin_n = s.bins[0][0][at];
+                        bin_w = ((uint64_t)s.bins[0][3][at] << 30) + ((uint64_t)s.bins[0][2][at] << 15) + s.bins[0][1][at];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s.bins[0][i][at] = 0;
+                    }
+                    pick(s, bin_n, bin_w, above_n, above_w, by_weight, target);
+                    f = s.found;
+                    above_n = f.above_n;
+                    above_w = f.above_w;
+                    lo += (uint32_t)f.bin << shift;
+                    hi = lo + min(hi - lo, (1u << shift) - 1);
+                    if (lo == hi || f.n == 1 || (!by_weight && (direct || !by_index) && above_n + f.n == target)) break;
+                }
+                if (step == 4) {
+#pragma unroll
+                    for (int i = 0; i < kHeld; ++i)
+                        if (live >> i & 1 && order[i] >= lo && order[i] <= hi) emit((int)~order[i], units[i], kept);
+                    break;
+                }
+#pragma unroll
+                for (int i = 0; i < kHeld; ++i)
+                    if ((by_index ? order[i] : key[i]) < lo) of &= ~(1u << i);
+                if (by_index) {
+                    live |= of;
+                    if (!direct && tid < ranks) cluster.map_shared_rank(&s, tid)->front[2] = ~lo;   // (the last of them: the search ends at a single one)
+                    continue;
+                }
+                live = of;
+                uint32_t take = f.n;
+                const uint64_t each = f.n > 1 ? f.w / f.n : f.w;
+                if (!by_weight) take = (uint32_t)(target - above_n);
+                else if (f.n > 1 && each > 0) take = (uint32_t)min((uint64_t)f.n, (target - above_w + each - 1) / each);
+                kept = above_w + (take == f.n ? f.w : take * each);
+                if (!direct && tid < ranks) {
+                    SampleShared* peer = cluster.map_shared_rank(&s, tid);
+                    peer->front[0] = take == f.n ? lo : lo + 1;
+                    peer->front[1] = take == f.n ? 0 : lo;
+                }
+                if (take == f.n) {
+                    ++step;   // (none of equal ones are left out)
+                    continue;
+                }
+                equal = 0;
 #pragma unroll
                 for (int i = 0; i < kHeld; ++i)
                     if (live >> i & 1 && key[i] == lo) equal |= 1u << i;
                 live &= ~equal;
-                descend(order, equal, ~(uint32_t)(p.vocab - 1), ~0u, false, n, lo, hi);
-                live |= equal;
-            };
-            auto live_units = [&] {
-                uint64_t sum = 0;
-#pragma unroll
-                for (int i = 0; i < kHeld; ++i)
-                    if (live >> i & 1) sum += units[i];
-                __syncthreads();
-                return block_sum(sum);
-            };
-            if (by_count) {
-                if (n > (uint32_t)top_k) cut_to(false, target);
-                if (by_share) target = max((uint64_t)1, share_of(fmaxf(top_p, 0.f), live_units(), true));
+                target = take;
             }
-            if (by_share) cut_to(true, target);
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i)
-                if (units[i] < least) live &= ~(1u << i);
-            const uint64_t kept = live_units();
-            uint32_t lo, hi;
-            unsigned up_to = live;
-            descend(order, up_to, ~(uint32_t)(p.vocab - 1), ~0u, true, draw_of(kept) + 1, lo, hi);
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i)
-                if (live >> i & 1 && order[i] >= lo && order[i] <= hi) emit((int)~order[i], units[i], kept);
-            return;
+            if (direct) return;
         }
+        if (listed_window) {
+            all_here();
+            keep = s.front[0];
+            if (s.front[1] != 0) {
+                tie_key = s.front[1];
+                tie_to = (int)s.front[2];
+            }
+        } else {
 
         // ---- the threshold lies lower: the lowest key that is kept whole, and how many logits of the key in front of it, by all CTAs ----
-        for (int i = tid; i < 2 * kSampleBins; i += kSampleThreads) (&s.bins.count[0][0])[i] = (&s.bins.low[0][0])[i] = (&s.bins.high[0][0])[i] = 0;
+        clear_bins(0);
+        clear_bins(1);
         __syncthreads();
-        int pass = 0;
-        // One pass: bins of the interval's logits, summed over the cluster; then the bin in which what lies above reaches the target.
-        auto find = [&](const Interval& iv, uint64_t above_n, uint64_t above_w, bool by_weight, uint64_t target) {
+        // the lowest key of the linear interval's bin `bin` (one past the last where there is none): the bin of a number never falls
+        auto edge_of = [&](const Interval& iv, int bin) {
+            uint32_t a = iv.lo, b = iv.hi + 1;
+#pragma unroll 1
+            while (a < b) {
+                const uint32_t mid = a + (b - a) / 2;
+                if (iv.bin(value_of(mid), mid) >= bin) b = mid;
+                else a = mid + 1;
+            }
+            return a;
+        };
+        auto edges = [&](const Interval& iv, int bin_lo, int bin_hi) {   // to s.edge: the lowest keys of a bin and of another one
+            if (lane == 0 && warp < 2) s.edge[warp] = edge_of(iv, warp ? bin_hi : bin_lo);
+            __syncthreads();
+        };
+        // The search: of the logits from key `bottom` on the front part is kept that reaches `target` logits, or units; above_n and above_w lie above the interval.
+        bool by_weight = !by_count;
+        const uint32_t cut_key = max(kLowestKey, key_of(cut));
+        uint32_t bottom = kLowestKey, above_n = 0;
+        uint64_t above_w = 0;
+        if (!by_count) target = max((uint64_t)1, share_of(fmaxf(top_p, 0.f), all, true));
+        Interval iv;
+        iv.by_key(cut_key, m_key);
+#pragma unroll 1
+        for (int pass = 0;; ++pass) {
+            // bins of the interval's logits, summed over the cluster
             const int buf = pass & 1;
             if (pass >= 2) {   // (its bins of two passes ago have been read: a barrier lies between)
-                if (tid < kSampleBins) s.bins.count[buf][tid] = s.bins.low[buf][tid] = s.bins.high[buf][tid] = 0;
+                clear_bins(buf);
                 __syncthreads();
             }
-            ++pass;
-            const float from = value_of(iv.lo);
-            for (int b = block0; b < block1; ++b) {
-                float v[4];
-                quad_of(x + b * kBlock + lane * 4, v);
-                if (!(max4(v) >= from)) continue;
+            uint32_t bin_n = 0;
+            uint64_t bin_w = 0;
+            {
+                const float from = value_of(iv.lo), to = value_of(iv.hi);
+#pragma unroll 1
+                for (int j = 0; j < run; ++j) {
+                    float v[4];
+                    quad_at(warp, j, v);
+                    bool any = false;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t key = key_of(v[i]);
-                    if (v[i] >= from && key >= iv.lo && key <= iv.hi) add_to_bin(buf, iv.bin(v[i], key), weigh(v[i]));
-                }
-            }
-            all_here();
-            if (tid < kSampleBins) {
-                uint32_t n = 0;
-                uint64_t w = 0;
-                for (int r = 0; r < ranks; ++r) {
-                    const SampleShared* from = cluster.map_shared_rank(&s, r);
-                    n += from->bins.count[buf][tid];
-                    w += ((uint64_t)from->bins.high[buf][tid] << 32) + from->bins.low[buf][tid];
-                }
-                s.bins.number[tid] = n;
-                s.bins.weight[tid] = w;
-            }
-            __syncthreads();
-            if (warp == 0) {
-                const auto f = pick_bin([&](int i) { return s.bins.number[i]; }, [&](int i) { return s.bins.weight[i]; }, above_n, above_w, by_weight, target, lane);
-                const unsigned has = __ballot_sync(0xffffffffu, f.bin >= 0);
-                if (lane == (has ? __ffs(has) - 1 : 31)) s.found = f;
-            }
-            __syncthreads();
-            return s.found;
-        };
-        // Keeps the front part that reaches `target` logits, or units, of those from key `bottom` on.
-        // Returns the units of what lies above the ties, or is kept whole.
-        auto select = [&](Interval iv, uint32_t bottom, bool by_weight, uint64_t target) {
-            uint64_t above_n = 0, above_w = 0;
-            const uint32_t old_ties = ties;
-            for (;;) {
-                const auto f = find(iv, above_n, above_w, by_weight, target);
-                above_n = f.above_n;
-                above_w = f.above_w;
-                if (f.bin < 0) {
-                    if (iv.lo <= bottom) {   // everything from there on, and of what was kept of the key in front of it
-                        keep = bottom;
-                        if (by_weight && old_ties > 0) {
-                            const uint64_t w = max((uint64_t)1, weigh(value_of(tie_key)));
-                            ties = (uint32_t)min((uint64_t)old_ties, target <= above_w ? 0 : (target - above_w + w - 1) / w);
-                        }
-                        break;
+                    for (int i = 0; i < 4; ++i) any |= v[i] >= from && v[i] <= to;
+                    if (!any) continue;
+                    uint64_t u[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) u[i] = weigh(v[i]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t key = key_of(v[i]);
+                        if (v[i] >= from && key >= iv.lo && key <= iv.hi) add_to_bin(buf, iv.bin(v[i], key), u[i]);
                     }
-                    iv.hi = iv.lo - 1;
-                    iv.lo = bottom;
-                    iv.linear = true;
-                    iv.x_lo = fmaxf(weigh.floor, value_of(bottom));
-                    iv.per = 256.f / fmaxf(value_of(iv.hi) - iv.x_lo, 1e-30f);
-                    continue;
                 }
-                if (!iv.linear && iv.shift == 0) {   // one key, of equal weights
-                    const uint32_t key = iv.lo + f.bin;
-                    const uint64_t w = max((uint64_t)1, f.w / f.n);
-                    const uint32_t n = (uint32_t)(by_weight ? min((uint64_t)f.n, f.w == 0 ? f.n : (target - above_w + w - 1) / w) : target - above_n);
-                    tie_key = key;
-                    ties = n == f.n ? 0 : n;
-                    tie_before = 0;
-                    for (int r = 0; r < rank; ++r) tie_before += cluster.map_shared_rank(&s, r)->bins.count[(pass - 1) & 1][f.bin];
-                    keep = n == f.n ? key : key + 1;
-                    above_w += n == f.n ? f.w : 0;
-                    break;
+                all_here();
+                if (tid < kSampleBins) {
+                    const int at = kSampleBins - 1 - tid;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t part[kSampleRanks];
+#pragma unroll
+                        for (int r = 0; r < kSampleRanks; ++r) part[r] = cluster.map_shared_rank(&s, min(r, ranks - 1))->bins[buf][i][at];   // (all on their way at once)
+                        uint64_t sum = 0;
+#pragma unroll
+                        for (int r = 0; r < kSampleRanks; ++r) sum += r < ranks ? part[r] : 0;
+                        if (i == 0) bin_n = (uint32_t)sum;
+                        else bin_w += sum << 15 * (i - 1);
+                    }
                 }
+            }
+            pick(s, bin_n, bin_w, above_n, above_w, by_weight, target);
+            const auto f = s.found;
+            above_n = f.above_n;
+            above_w = f.above_w;
+            bool done = true;
+            if (f.bin < 0) {
+                if (iv.lo > bottom) {
+                    iv.over(bottom, iv.lo - 1, weigh.floor);
+                    done = false;
+                } else {   // everything from there on, and of what was kept of the key in front of it
+                    keep = bottom;
+                    if (ties > 0) {
+                        const uint64_t w = max((uint64_t)1, units_at(value_of(tie_key)));
+                        ties = (uint32_t)min((uint64_t)ties, target <= above_w ? 0 : (target - above_w + w - 1) / w);
+                    }
+                }
+            } else if (!iv.linear && iv.shift == 0) {   // one key, of equal weights
+                const uint32_t key = iv.lo + f.bin;
+                const uint64_t w = max((uint64_t)1, f.w / f.n);
+                const uint32_t take = (uint32_t)(by_weight ? min((uint64_t)f.n, f.w == 0 ? f.n : (target - above_w + w - 1) / w) : target - above_n);
+                tie_key = key;
+                ties = take == f.n ? 0 : take;
+                tie_before = 0;
+                for (int r = 0; r < rank; ++r) tie_before += cluster.map_shared_rank(&s, r)->bins[buf][0][f.bin];
+                keep = take == f.n ? key : key + 1;
+                above_w += take == f.n ? f.w : take * w;
+            } else {
                 uint32_t lo = iv.lo + (iv.linear ? 0 : (uint32_t)f.bin << iv.shift), hi = lo + min(iv.hi - lo, (1u << iv.shift) - 1);
                 if (iv.linear) {
-                    // the lowest keys of the bin and of the next one: the bin of a number never falls
-                    if (tid < 2) {
-                        uint32_t a = iv.lo, b = iv.hi + 1;   // (b: past the last)
-                        while (a < b) {
-                            const uint32_t mid = a + (b - a) / 2;
-                            if (iv.bin(value_of(mid), mid) >= f.bin + tid) b = mid;
-                            else a = mid + 1;
-                        }
-                        s.edge[tid] = a;
-                    }
-                    __syncthreads();
+                    edges(iv, f.bin, f.bin + 1);
                     lo = s.edge[0];
                     hi = s.edge[1] - 1;
                 }
@@ -628,25 +875,26 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
                     keep = lo;
                     ties = 0;
                     above_w += f.w;
-                    break;
+                } else {
+                    iv.by_key(lo, hi);
+                    done = false;
                 }
-                iv.by_key(lo, hi);
             }
-            return above_w;
-        };
-        Interval iv;
-        iv.by_key(max(kLowestKey, key_of(cut)), m_key);
-        uint64_t total_k = select(iv, kLowestKey, !by_count, target);
-        if (by_count && by_share) {
-            if (ties > 0) total_k += ties * weigh(value_of(tie_key));
-            target = max((uint64_t)1, share_of(fmaxf(top_p, 0.f), total_k, true));
-            if (keep <= m_key) {
-                iv.by_key(keep, m_key);
-                select(iv, keep, true, target);
-            } else {   // all of what is left are equal
-                const uint64_t w = weigh(value_of(tie_key));
+            if (!done) continue;
+            if (by_weight || !by_share) break;
+            // top-p of what top-k has left (above_w units)
+            by_weight = true;
+            target = max((uint64_t)1, share_of(fmaxf(top_p, 0.f), above_w, true));
+            if (keep > m_key) {   // all of it are equal
+                const uint64_t w = units_at(value_of(tie_key));
                 ties = (uint32_t)min((uint64_t)ties, (target + w - 1) / w);
+                break;
             }
+            bottom = keep;
+            above_n = 0;
+            above_w = 0;
+            iv.by_key(keep, m_key);
+        }
         }
     }
 
@@ -655,29 +903,28 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
     uint32_t tie_at = 0;   // ties in front of the warp's next block
     if (ties > 0) {
         uint32_t n = 0;
-        for (int b = block0; b < block1; ++b) {
+#pragma unroll 1
+        for (int j = 0; j < run; ++j) {
             float v[4];
-            quad_of(x + b * kBlock + lane * 4, v);
+            quad_at(warp, j, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i) n += v[i] == tie;
         }
         n = __reduce_add_sync(0xffffffffu, n);
+        __syncthreads();
         if (lane == 0) s.warp_word[warp] = n;
         __syncthreads();
         tie_at = tie_before;
         for (int w = 0; w < warp; ++w) tie_at += s.warp_word[w];
     }
     // No logit below this one is kept: of the threshold, or of min_p (less what the rounding of its place can be off).
-    float from = value_of(ties > 0 ? tie_key : keep);
+    float from = value_of(ties > 0 || tie_to >= 0 ? tie_key : keep);
     if (least > 0) from = fmaxf(from, fmaxf(-FLT_MAX, m + t * logf(fminf(min_p, 1.f)) * 1.0001f - 1e-5f * (fabsf(m) + t)));
-    const bool everything = keep == kLowestKey && least == 0;
-    // units of four neighbouring logits of block b, none where they are not kept; `at`: ties so far, moved on
-    auto kept_units = [&](int b, uint32_t& at, uint64_t (&w)[4]) {
-        float v[4];
-        quad_of(x + b * kBlock + lane * 4, v);
+    // units of four neighbouring logits from index e on, none where they are not kept; `at`: ties so far, moved on
+    auto kept_units = [&](const float (&v)[4], int e, uint32_t& at, uint64_t (&w)[4]) {
         bool in[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) in[i] = v[i] >= from && key_of(v[i]) >= keep;
+        for (int i = 0; i < 4; ++i) in[i] = v[i] >= from && (key_of(v[i]) >= keep || (v[i] == tie && e + i <= tie_to));
         if (ties > 0) {
             unsigned of[4], any = 0;
             const unsigned lower = (1u << lane) - 1;
@@ -706,18 +953,25 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
         }
     };
     uint64_t sum = 0;
-    if (everything) {
-        sum = all_units();
+    if (ties == 0 && tie_to < 0 && least == 0) {
+        double sums[4] = {Weigh::kZero, Weigh::kZero, Weigh::kZero, Weigh::kZero};
+        for_blocks([&](int, const float (&v)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const double to = weigh.add(v[i], sums[i]);
+                sums[i] = v[i] >= from ? to : sums[i];
+            }
+        });
+        sum = units_of(sums);
     } else {
         uint32_t at = tie_at;
-        for (int b = block0; b < block1; ++b) {
-            if (ties == 0) {
-                float v[4];
-                quad_of(x + b * kBlock + lane * 4, v);
-                if (!__any_sync(0xffffffffu, max4(v) >= from)) continue;
-            }
+#pragma unroll 1
+        for (int j = 0; j < run; ++j) {
+            float v[4];
             uint64_t w[4];
-            kept_units(b, at, w);
+            quad_at(warp, j, v);
+            if (ties == 0 && !__any_sync(0xffffffffu, max4(v) >= from)) continue;
+            kept_units(v, from_e + j * kBlock, at, w);
             sum += (w[0] + w[1]) + (w[2] + w[3]);
         }
     }
@@ -732,11 +986,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
     all_here();
 
     // ---- the draw ----
-    uint64_t total = 0, in_front = 0;
-    for (int r = 0; r < ranks; ++r) {
-        total += s.rank_kept[r];
-        if (r < rank) in_front += s.rank_kept[r];
-    }
+    const uint64_t rank_sum = lane < ranks ? s.rank_kept[lane] : 0, total = warp_sum_u64(rank_sum);
+    uint64_t in_front = warp_sum_u64(lane < rank ? rank_sum : 0);
     const uint64_t drawn = draw_of(total);
     if (drawn < in_front || drawn >= in_front + s.rank_kept[rank]) return;
     // The warps look through the run of the one that it falls into, a block each.
@@ -745,27 +996,28 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
         in_front += w;
         ++of;
     }
-    const int run0 = blocks * of / kSampleWarps, run1 = blocks * (of + 1) / kSampleWarps;
-    for (int round = run0; round < run1; round += kSampleWarps) {
-        const int b = round + warp;
+    const int of_block0 = blocks * of / kSampleWarps, of_run = blocks * (of + 1) / kSampleWarps - of_block0;
+    for (int round = 0; round < of_run; round += kSampleWarps) {
+        const int j = round + warp;
         uint64_t w[4] = {0, 0, 0, 0};
-        if (b < run1) {
+        if (j < of_run) {
+            float v[4];
             uint32_t at = tie_before;
             if (ties > 0) {   // those in front of the block
                 uint32_t n = 0;
-                for (int c = run0; c < b; ++c) {
-                    float v[4];
-                    quad_of(x + c * kBlock + lane * 4, v);
+                for (int c = 0; c < j; ++c) {
+                    quad_at(of, c, v);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) n += v[i] == tie;
                 }
                 at += __reduce_add_sync(0xffffffffu, n);
                 for (int c = 0; c < of; ++c) at += s.warp_word[c];
             }
-            kept_units(b, at, w);
+            quad_at(of, j, v);
+            kept_units(v, first + (of_block0 + j) * kBlock + lane * 4, at, w);
         }
         const uint64_t here = (w[0] + w[1]) + (w[2] + w[3]), up_to = warp_scan_u64(here, lane);
-        if (round > run0) __syncthreads();
+        if (round > 0) __syncthreads();
         if (lane == 31) s.block[warp] = up_to;
         __syncthreads();
         uint64_t before = in_front;
@@ -778,15 +1030,15 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
                 at += w[i];
                 if (at > drawn) break;
             }
-            emit(first + b * kBlock + lane * 4 + i, i == 0 ? w[0] : i == 1 ? w[1] : i == 2 ? w[2] : w[3], total);
+            emit(first + (of_block0 + j) * kBlock + lane * 4 + i, i == 0 ? w[0] : i == 1 ? w[1] : i == 2 ? w[2] : w[3], total);
         }
         for (int c = 0; c < kSampleWarps; ++c) in_front += s.block[c];
     }
 }
 
-constexpr int kMaxStretch = (227 * 1024 - (int)sizeof(SampleShared)) / 4 / kBlock * kBlock;
-static_assert((int64_t)kMaxStretch * kSampleRanks >= kMaxVocab + 8 + kSampleRanks * kBlock, "the largest vocabulary fits eight CTAs");
-static_assert(3 * (sizeof(SampleShared) + 16128 * 4 + 1024) <= 228 * 1024, "three stretches of an eighth of 128256 logits fit an SM");
+static_assert((kMaxVocab + 8 + kSampleRanks * kBlock) / kSampleRanks < 1 << 16, "parts of a bin's sum fit 32 bits");
+constexpr int kSampleSmem = 227 * 1024, kSmallSmem = 228 * 1024 / 3 - 1024;   // of a CTA alone on its SM, and of one of three
+static_assert(kSmallSmem - sizeof(SampleShared) >= 64 * 1024, "what is left of a third of an SM's shared memory is 16384 logits of 32 bits");
 
 template <class F>
 cudaError_t for_each_sample(F f) {
@@ -797,19 +1049,21 @@ cudaError_t for_each_sample(F f) {
 }
 cudaError_t configure_sample_kernels() {
     return for_each_sample([](auto* kernel) {
-        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SampleShared) + kMaxStretch * 4);
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSampleSmem);
     });
 }
 
 cudaError_t launch_sample(const SampleParams& params, int dtype, int num_sms, cudaStream_t stream) {
     SampleParams p = params;
     const int size = dtype == SW_DTYPE_F32 ? 4 : 2;
-    // CTAs of a row: as many as give each 16384 logits at most (64 KB: three CTAs an SM, one loads while the others work), and more where rows are few.
     const int64_t positions = (int64_t)p.vocab + 16 / size - 1;   // (a row may start anywhere behind a 16-byte boundary)
     int ranks = 1;
     while (ranks < kSampleRanks && (positions > ranks * 16384 || (p.rows * ranks < num_sms && positions > ranks * 2048))) ranks *= 2;
     p.stretch = (int)((positions + ranks * kBlock - 1) / (ranks * kBlock) * kBlock);
     const bool many = p.rows * ranks <= num_sms && p.stretch >= 4 * kManySampleThreads;
+    const int warps = (many ? kManySampleThreads : kFewSampleThreads) / 32, run = (p.stretch / kBlock + warps - 1) / warps;   // blocks of the longest run
+    const int room = ((many ? kSampleSmem : kSmallSmem) - (int)sizeof(SampleShared)) / (warps * kBlock * size);
+    p.held = room < run ? room : run;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -819,7 +1073,7 @@ cudaError_t launch_sample(const SampleParams& params, int dtype, int num_sms, cu
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(p.rows * ranks));
     cfg.blockDim = dim3(many ? kManySampleThreads : kFewSampleThreads);
-    cfg.dynamicSmemBytes = sizeof(SampleShared) + (size_t)p.stretch * size;
+    cfg.dynamicSmemBytes = sizeof(SampleShared) + (size_t)p.held * warps * kBlock * size;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
