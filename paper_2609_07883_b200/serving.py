@@ -56,9 +56,15 @@ class Request:
         self.done_at = None
 
 
-def gpu_executor(ctx, pools, shape: W.AttnShape, c_max: int, max_decode: int, seed: int = W.SEED_BASE + 44):
+def gpu_executor(ctx, pools, shape: W.AttnShape, c_max: int, max_decode: int, seed: int = W.SEED_BASE + 44, rope=None, vocab: int = 0,
+                 temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0):
     """Returns execute(batch) -> measured device nanoseconds of one iteration over the layer stack: per layer one
-    launch that appends the new K/V rows and runs the mixed attention, timed with CUDA events on the current stream."""
+    launch that appends the new K/V rows and runs the mixed attention, timed with CUDA events on the current stream.
+
+    With ``rope`` (a ``binding.Rope``) a layer's queries and new keys are rotated as they are appended, one launch, and the attention is the other.
+    With ``vocab`` the iteration ends with the draw of a token for every decode and for the last row of every chunk, from random logits of that many
+    entries; ``execute.tokens`` holds them (decodes first).  ``execute.extra_ns`` is what these two cost at the largest batch, measured here: a cost
+    table of attention iterations does not hold it, so it belongs into the controller's margin."""
     import torch
 
     from . import binding as B
@@ -71,18 +77,52 @@ def gpu_executor(ctx, pools, shape: W.AttnShape, c_max: int, max_decode: int, se
     k_new = torch.randn(rows_max, shape.num_kv_heads, shape.head_dim, device=dev, generator=gen).to(torch.bfloat16)
     v_new = torch.randn(rows_max, shape.num_kv_heads, shape.head_dim, device=dev, generator=gen).to(torch.bfloat16)
     out = torch.empty_like(q)
+    turned = torch.empty_like(q) if rope is not None else None
+    draws_max = max_decode + B.SW_MAX_CHUNKS
+    if vocab:
+        logits = (2 * torch.randn(draws_max, vocab, device=dev, generator=gen)).to(torch.bfloat16)
+        tokens, log_probs = torch.zeros(draws_max, dtype=torch.int32, device=dev), torch.zeros(draws_max, device=dev)
+        setting = lambda v, dtype=torch.float32: torch.full((draws_max,), v, dtype=dtype, device=dev)  # noqa: E731
+        settings = (setting(temperature), setting(top_k, torch.int32), setting(top_p), setting(min_p))
     ev0, ev1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+
+    def draw(count: int) -> None:
+        u = torch.rand(count, device=dev, generator=gen)
+        B.sw_sample_run(ctx, logits[:count], u, tokens, log_probs, *settings)
+        execute.tokens = tokens[:count]
 
     def execute(batch: W.MixedBatch) -> int:
         db = B.DeviceBatch(batch, dev)
         rows = batch.num_rows
         ev0.record()
         for pool_t in pools:
-            B.sw_mixed_iteration_run(ctx, pool_t, db, k_new[:rows], v_new[:rows], q[:rows], out[:rows])
+            if rope is None:
+                B.sw_mixed_iteration_run(ctx, pool_t, db, k_new[:rows], v_new[:rows], q[:rows], out[:rows])
+            else:
+                B.sw_rope_append(ctx, pool_t, db, rope, q[:rows], k_new[:rows], v_new[:rows], turned[:rows])
+                B.sw_mixed_attn_run(ctx, pool_t, db, turned[:rows], out[:rows])
+        if vocab:
+            draw(batch.num_decode + len(batch.chunks()))
         ev1.record()
         ev1.synchronize()
         return int(ev0.elapsed_time(ev1) * 1e6)
 
+    execute.tokens, execute.extra_ns = None, 0
+    if rope is not None or vocab:
+        keys = torch.empty_like(k_new) if rope is not None else None
+        db = B.DeviceBatch(W.make_batch(shape, ctx.layout.num_pages, [1] * max_decode, 0, c_max, np.random.default_rng(seed)), dev)
+        times = []
+        for _ in range(5):
+            ev0.record()
+            if rope is not None:
+                for _ in pools:
+                    B.sw_rope_run(ctx, db, rope, q, k_new, turned, keys)
+            if vocab:
+                draw(draws_max)
+            ev1.record()
+            ev1.synchronize()
+            times.append(int(ev0.elapsed_time(ev1) * 1e6))
+        execute.extra_ns, execute.tokens = max(times[1:]), None          # (the first one warms up)
     return execute
 
 
@@ -370,6 +410,13 @@ def main(argv=None):
                     help="also count the requests that meet both SLOs and the goodput (Sec. 4.3)")
     ap.add_argument("--telemetry", action="store_true",
                     help="residual feedback (Sec. 3.3): add the P99 residual of the (n, L) bin to the controller's margin")
+    ap.add_argument("--rope", choices=["plain", "linear", "base", "bands", "ramp"], default=None,
+                    help="rotary positions in every layer, with this way to stretch them (factor 8 over 8192 positions)")
+    ap.add_argument("--vocab", type=int, default=0, help="draw the next tokens from logits of this many entries at the end of every iteration")
+    ap.add_argument("--temperature", type=float, default=1.0)
+    ap.add_argument("--top-k", type=int, default=0)
+    ap.add_argument("--top-p", type=float, default=1.0)
+    ap.add_argument("--min-p", type=float, default=0.0)
     ap.add_argument("--out", default="bursty_results.json")
     args = ap.parse_args(argv)
 
@@ -403,7 +450,12 @@ def main(argv=None):
     stats = profiler.monotone_report(tab, table)
     log("cost table: " + json.dumps(stats))
     trace = W.bursty_trace(num_requests=args.requests)
-    execute = gpu_executor(ctx, pools, shape, args.c_max, max_decode)
+    rope = None
+    if args.rope:
+        turns, magnitude = B.sw_rope_frequencies(shape.head_dim, 500000.0, args.rope, 8.0, 8192, 1.0, 4.0 if args.rope == "bands" else 32.0)
+        rope = B.Rope(turns, False, magnitude, device=dev)
+    execute = gpu_executor(ctx, pools, shape, args.c_max, max_decode, rope=rope, vocab=args.vocab, temperature=args.temperature, top_k=args.top_k,
+                           top_p=args.top_p, min_p=args.min_p)
     results = {"layers": args.layers, "pages_per_layer": args.pages, "table_points": int(np.prod(np.shape(tab["p99_ns"]))),
                "table_stats": stats, "runs": []}
     for scale in args.rate_scale:
@@ -413,7 +465,7 @@ def main(argv=None):
                 log(f"run: rate x{scale} tpot={tpot} ms policy={policy}")
                 tele = B.Telemetry([1, 4, 16, 48, 128, 256], [0, 64, 256, 1024, 2048, 4096]) if args.telemetry else None
                 res = run_trace(scaled, tpot, table, execute, shape, args.pages, policy=policy, c_max=args.c_max,
-                                margin_ppm=args.margin_ppm, max_decode=max_decode, ctx_cap=tab["ctx_grid"][-1], log=log,
+                                margin_ppm=args.margin_ppm, margin_abs_ns=execute.extra_ns, max_decode=max_decode, ctx_cap=tab["ctx_grid"][-1], log=log,
                                 max_prefills=args.max_prefills if policy == "sloweave" else 1, prefix_cap=tab["prefix_grid"][-1],
                                 telemetry=tele, ttft_slo_ms=args.ttft_slo_ms)
                 B.sw_check_status(ctx)
