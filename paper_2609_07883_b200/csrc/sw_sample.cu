@@ -30,19 +30,18 @@
 namespace sw {
 namespace cg = cooperative_groups;
 
-constexpr int kSampleBins = 256, kSampleRanks = 8, kMaxWarps = 32;
+constexpr int kSampleBins = 256, kSampleRanks = 8, kMaxWarps = 16;
 constexpr int kBlock = 128, kFar = 4;   // logits that a warp takes at once; such blocks outside shared memory that it loads at once
-constexpr int kListed = 128;  // logits collected from a CTA
+constexpr int kListed = 1024;  // logits that can be collected: an equal part from each CTA
 constexpr uint32_t kLowestKey = 0x00800000u;   // key_of() of the lowest finite number
 constexpr int kUnitBits = 44;                  // the largest weight is 2^44 units: sums of up to 2^19 of them fit 63 bits
 
 struct SampleShared {
     union {
-        uint2 listed[kSampleRanks][kListed];   // the collecting CTA: logits above the cut, as bits, and their indices
+        uint2 listed[kListed];   // logits above the cut, as bits, and their indices: a part for each CTA, in its own place here and in the collecting CTA
         uint32_t bins[2][4][kSampleBins];   // by the parity of the pass: logits, and units in three parts of 15 bits
         uint64_t block[kMaxWarps];   // units of the blocks that the warps look through
     };
-    uint2 mine[kListed];
     double power[16];   // (see Weigh)
     uint64_t rank_total[kSampleRanks], rank_above[kSampleRanks], rank_kept[kSampleRanks], warp_sum[kMaxWarps], pick_w[8];
     float rank_top[kSampleRanks], rank_cut[kSampleRanks], warp_top[kMaxWarps], warp_cut[kMaxWarps];
@@ -215,11 +214,15 @@ __device__ __noinline__ void pick(SampleShared& s, uint32_t n, uint64_t w, uint3
     __syncthreads();
 }
 
-// Threads of a CTA: few, three CTAs an SM, that work while others load, or many where no SM gets a second CTA.
-constexpr int kManySampleThreads = 1024, kFewSampleThreads = 256;
-template <class T, int kSampleThreads>
-__global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleThreads ? 3 : 1) sw_sample_kernel(const SampleParams p) {
-    constexpr int kSampleWarps = kSampleThreads / 32, kHeld = (kListed * kSampleRanks + kSampleThreads - 1) / kSampleThreads;   // kHeld: of the collected logits
+// kCtas: CTAs an SM, of 256 threads, so that some work while others load, or of 512 where no SM gets a second one.  (Three of 384, or two of 512, which have
+// fewer registers a thread or a barrier for more warps: 256 rows of 128256 without limits 82 and 88 us instead of 70; where two an SM are all there are, 80
+// registers a thread instead of 128 make 128 rows of 32003 18.1 us instead of 14.1; 1024 threads one row of 128256 10.5 instead of 8.4.)
+template <int kCtas>
+constexpr int kThreadsFor = kCtas == 1 ? 512 : 256;
+template <class T, int kCtas>
+__global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(const SampleParams p) {
+    constexpr int kSampleThreads = kThreadsFor<kCtas>;
+    constexpr int kSampleWarps = kSampleThreads / 32, kHeld = kListed / kSampleThreads;   // kHeld: of the collected logits
     extern __shared__ __align__(16) unsigned char sample_raw[];
     SampleShared& s = *reinterpret_cast<SampleShared*>(sample_raw);
     T* const x = reinterpret_cast<T*>(s.x);
@@ -467,13 +470,26 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
     if (by_count || by_share) {
         // ---- the logits above the cut, collected in one CTA ----
         uint64_t total = 0, above = 0;
+        const int most = kListed / ranks;   // of a CTA (ranks: a power of two)
+        uint2* const mine = s.listed + rank * most;
         auto list = [&](const float (&v)[4], int j) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (v[i] >= cut && v[i] > -INFINITY) {
                     const uint32_t at = atomicAdd(&s.num_mine, 1u);
-                    if (at < kListed) s.mine[at] = make_uint2(__float_as_uint(v[i]), (uint32_t)(from_e + j * kBlock + i));
+                    if (at < most) mine[at] = make_uint2(__float_as_uint(v[i]), (uint32_t)(from_e + j * kBlock + i));
                 }
+        };
+        const int collector = row % ranks;
+        // The CTA's part to the collecting CTA; returns the units of what this thread had of it where they are asked for.
+        auto hand_over = [&](bool weighed) {
+            uint64_t w = 0;
+            for (int i = tid; i < (int)min(s.num_mine, (uint32_t)most); i += kSampleThreads) {
+                const uint2 e = mine[i];
+                if (rank != collector) cluster.map_shared_rank(&s, collector)->listed[rank * most + i] = e;
+                if (weighed) w += units_at(__uint_as_float(e.x));
+            }
+            return w;
         };
         if (by_share && !by_count) {
             double sums[4] = {Weigh::kZero, Weigh::kZero, Weigh::kZero, Weigh::kZero};
@@ -488,13 +504,8 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
             });
         }
         __syncthreads();
-        const int collector = row % ranks;
         const uint32_t listed = s.num_mine;
-        if (tid < min(listed, (uint32_t)kListed)) {
-            const uint2 e = s.mine[tid];
-            cluster.map_shared_rank(&s, collector)->listed[rank][tid] = e;
-            if (!by_count) above = units_at(__uint_as_float(e.x));
-        }
+        above = hand_over(!by_count);
         if (!by_count) above = block_sum(above);   // (of those that are listed)
         if (warp == 0 && lane < ranks) {
             SampleShared* peer = cluster.map_shared_rank(&s, lane);
@@ -504,7 +515,7 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
         }
         all_here();
         uint32_t n = lane < ranks ? s.rank_listed[lane] : 0;
-        const bool fits = __all_sync(0xffffffffu, n <= kListed);
+        const bool fits = __all_sync(0xffffffffu, n <= most);
         n = __reduce_add_sync(0xffffffffu, n);
         uint64_t all = 0, target = top_k;
         if (!by_count) {
@@ -609,29 +620,24 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
                         sums[0][i & 1] = v[i] > hi_v ? to : sums[0][i & 1];
                         if (v[i] >= lo_v && v[i] <= hi_v && v[i] > -INFINITY) {
                             const uint32_t to_at = atomicAdd(&s.num_mine, 1u);
-                            if (to_at < kListed) s.mine[to_at] = make_uint2(__float_as_uint(v[i]), (uint32_t)(from_e + j * kBlock + i));
+                            if (to_at < most) mine[to_at] = make_uint2(__float_as_uint(v[i]), (uint32_t)(from_e + j * kBlock + i));
                         }
                     }
                 }
                 sum[0] = block_sum(Weigh::units(sums[0][0]) + Weigh::units(sums[0][1]));
-                const uint32_t mine = s.num_mine;
-                uint64_t mine_w = 0;
-                if (tid < min(mine, (uint32_t)kListed)) {
-                    const uint2 e = s.mine[tid];
-                    cluster.map_shared_rank(&s, collector)->listed[rank][tid] = e;
-                    mine_w = units_at(__uint_as_float(e.x));
-                }
+                const uint32_t found = s.num_mine;
+                uint64_t found_w = hand_over(true);
                 __syncthreads();
-                mine_w = block_sum(mine_w);
+                found_w = block_sum(found_w);
                 if (warp == 0 && lane < ranks) {
                     SampleShared* peer = cluster.map_shared_rank(&s, lane);
-                    peer->rank_listed[rank] = mine;
+                    peer->rank_listed[rank] = found;
                     peer->rank_total[rank] = sum[0];
-                    peer->rank_above[rank] = mine_w;
+                    peer->rank_above[rank] = found_w;
                 }
                 all_here();
                 const uint64_t over = warp_sum_u64(lane < ranks ? s.rank_total[lane] : 0), among = warp_sum_u64(lane < ranks ? s.rank_above[lane] : 0);
-                const bool all_listed = __all_sync(0xffffffffu, lane >= ranks || s.rank_listed[lane] <= kListed);
+                const bool all_listed = __all_sync(0xffffffffu, lane >= ranks || s.rank_listed[lane] <= most);
                 listed_window = all_listed && over < target && over + among >= target;
                 if (listed_window) {
                     target -= over;
@@ -645,11 +651,11 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
             unsigned live = 0;
 #pragma unroll
             for (int i = 0; i < kHeld; ++i) {
-                const int at = tid + i * kSampleThreads, r = at / kListed;
+                const int at = tid + i * kSampleThreads, r = at / most;
                 key[i] = order[i] = 0;
                 units[i] = 0;
-                if (r < ranks && at - r * kListed < (int)s.rank_listed[r]) {
-                    const uint2 e = s.listed[r][at - r * kListed];
+                if (at - r * most < (int)s.rank_listed[r]) {
+                    const uint2 e = s.listed[at];
                     key[i] = key_of(__uint_as_float(e.x));
                     order[i] = ~e.y;
                     units[i] = units_at(__uint_as_float(e.x));
@@ -1037,32 +1043,34 @@ __global__ void __launch_bounds__(kSampleThreads, kSampleThreads == kFewSampleTh
 }
 
 static_assert((kMaxVocab + 8 + kSampleRanks * kBlock) / kSampleRanks < 1 << 16, "parts of a bin's sum fit 32 bits");
-constexpr int kSampleSmem = 227 * 1024, kSmallSmem = 228 * 1024 / 3 - 1024;   // of a CTA alone on its SM, and of one of three
-static_assert(kSmallSmem - sizeof(SampleShared) >= 64 * 1024, "what is left of a third of an SM's shared memory is 16384 logits of 32 bits");
+constexpr int sample_smem(int ctas) { return ctas == 1 ? 227 * 1024 : 228 * 1024 / ctas - 1024; }   // of a CTA
+static_assert(sample_smem(3) - sizeof(SampleShared) >= 64 * 1024, "what is left of a third of an SM's shared memory is 16384 logits of 32 bits");
 
-template <class F>
-cudaError_t for_each_sample(F f) {
-    for (auto* kernel : {sw_sample_kernel<float, kFewSampleThreads>, sw_sample_kernel<float, kManySampleThreads>, sw_sample_kernel<__nv_bfloat16, kFewSampleThreads>,
-                         sw_sample_kernel<__nv_bfloat16, kManySampleThreads>, sw_sample_kernel<__half, kFewSampleThreads>, sw_sample_kernel<__half, kManySampleThreads>})
-        if (const cudaError_t e = f(kernel)) return e;
-    return cudaSuccess;
+template <class T>
+cudaError_t configure_sample() {
+    cudaError_t e = cudaFuncSetAttribute(sw_sample_kernel<T, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, sample_smem(1));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(sw_sample_kernel<T, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, sample_smem(2));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(sw_sample_kernel<T, 3>, cudaFuncAttributeMaxDynamicSharedMemorySize, sample_smem(3));
+    return e;
 }
 cudaError_t configure_sample_kernels() {
-    return for_each_sample([](auto* kernel) {
-        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSampleSmem);
-    });
+    cudaError_t e = configure_sample<float>();
+    if (e == cudaSuccess) e = configure_sample<__nv_bfloat16>();
+    if (e == cudaSuccess) e = configure_sample<__half>();
+    return e;
 }
 
 cudaError_t launch_sample(const SampleParams& params, int dtype, int num_sms, cudaStream_t stream) {
     SampleParams p = params;
     const int size = dtype == SW_DTYPE_F32 ? 4 : 2;
+    // CTAs of a row: as many as give each 16384 logits at most (64 KB: three CTAs an SM), and more where rows are few.
     const int64_t positions = (int64_t)p.vocab + 16 / size - 1;   // (a row may start anywhere behind a 16-byte boundary)
     int ranks = 1;
     while (ranks < kSampleRanks && (positions > ranks * 16384 || (p.rows * ranks < num_sms && positions > ranks * 2048))) ranks *= 2;
     p.stretch = (int)((positions + ranks * kBlock - 1) / (ranks * kBlock) * kBlock);
-    const bool many = p.rows * ranks <= num_sms && p.stretch >= 4 * kManySampleThreads;
-    const int warps = (many ? kManySampleThreads : kFewSampleThreads) / 32, run = (p.stretch / kBlock + warps - 1) / warps;   // blocks of the longest run
-    const int room = ((many ? kSampleSmem : kSmallSmem) - (int)sizeof(SampleShared)) / (warps * kBlock * size);
+    const int ctas = p.rows * ranks > 2 * num_sms ? 3 : p.rows * ranks > num_sms || p.stretch < 4096 ? 2 : 1, warps = (ctas == 1 ? kThreadsFor<1> : kThreadsFor<2>) / 32;
+    const int run = (p.stretch / kBlock + warps - 1) / warps;   // blocks of the longest run
+    const int room = (sample_smem(ctas) - (int)sizeof(SampleShared)) / (warps * kBlock * size);
     p.held = room < run ? room : run;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1072,15 +1080,15 @@ cudaError_t launch_sample(const SampleParams& params, int dtype, int num_sms, cu
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(p.rows * ranks));
-    cfg.blockDim = dim3(many ? kManySampleThreads : kFewSampleThreads);
+    cfg.blockDim = dim3(warps * 32);
     cfg.dynamicSmemBytes = sizeof(SampleShared) + (size_t)p.held * warps * kBlock * size;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    auto launch = [&](auto* few_kernel, auto* many_kernel) { return cudaLaunchKernelEx(&cfg, many ? many_kernel : few_kernel, p); };
-    if (dtype == SW_DTYPE_F32) return launch(sw_sample_kernel<float, kFewSampleThreads>, sw_sample_kernel<float, kManySampleThreads>);
-    if (dtype == SW_DTYPE_BF16) return launch(sw_sample_kernel<__nv_bfloat16, kFewSampleThreads>, sw_sample_kernel<__nv_bfloat16, kManySampleThreads>);
-    return launch(sw_sample_kernel<__half, kFewSampleThreads>, sw_sample_kernel<__half, kManySampleThreads>);
+    auto launch = [&](auto* one, auto* two, auto* three) { return cudaLaunchKernelEx(&cfg, ctas == 1 ? one : ctas == 2 ? two : three, p); };
+    if (dtype == SW_DTYPE_F32) return launch(sw_sample_kernel<float, 1>, sw_sample_kernel<float, 2>, sw_sample_kernel<float, 3>);
+    if (dtype == SW_DTYPE_BF16) return launch(sw_sample_kernel<__nv_bfloat16, 1>, sw_sample_kernel<__nv_bfloat16, 2>, sw_sample_kernel<__nv_bfloat16, 3>);
+    return launch(sw_sample_kernel<__half, 1>, sw_sample_kernel<__half, 2>, sw_sample_kernel<__half, 3>);
 }
 
 }  // namespace sw

@@ -159,6 +159,22 @@ def test_infinite_and_extreme_logits(ctx):
         check(ctx, x, uniforms(9, 4), **settings)
 
 
+@pytest.mark.parametrize("vocab", [700, 5000, 33000, 128256])
+def test_many_at_the_threshold(ctx, vocab):
+    """More logits at, or just above, a threshold than one CTA can collect; infinite ones among them; spread evenly or all in one place."""
+    x = logits(6, vocab, 21, kind="flat").clamp(max=3.0)
+    x[1, : vocab // 2] = INF
+    x[2, ::7] = INF
+    x[3] = torch.round(x[3])
+    x[4] = torch.where(torch.arange(vocab, device="cuda") % 50 == 0, 3.0, x[4])
+    x[5, -vocab // 3:] = 3.0
+    u = torch.tensor([0.02, 0.3, 0.5, 0.7, 0.9, 0.999], device="cuda")
+    for dtype in (torch.float32, torch.bfloat16):
+        for settings in (dict(top_p=0.2), dict(top_p=0.6), dict(top_p=0.97), dict(top_k=vocab // 9 + 1), dict(top_k=vocab // 3, top_p=0.7, min_p=0.5),
+                         dict(top_p=0.95, temperature=3.0), dict(top_p=0.9, temperature=0.05)):
+            check(ctx, x.to(dtype), u, **settings)
+
+
 def test_extreme_settings(ctx):
     x = logits(10, 3001, 8)
     for t in (0.0, -1.0, NAN, 1e-45, 1e-30, 1e-8, 1e-4, 1e4, 1e30, 3e38, INF):
