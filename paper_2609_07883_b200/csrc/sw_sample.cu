@@ -18,7 +18,7 @@
 //     weight, and the token likewise, by index.  The others end;
 //   - if it does not, and there is no top-k (weights spread over thousands of tokens): an eighth of the logits tell about where the threshold lies, the weights
 //     above three places around it where it lies to some hundreds of logits, and these are collected, and the threshold found among them, as before;
-//   - otherwise (a large k, logits of very unlike runs) all CTAs search their stretches by bins, and read one another's.
+//   - otherwise (a large k, more than hundreds of equal logits at the threshold) all CTAs search their stretches by bins, and read one another's.
 // Bound by the logits' bytes, by the instructions of a weight where all are needed (some 20 a logit, nine of them in 64 bits, and a conversion), and for a
 // few rows by the chain of two cluster barriers and the passes.
 #include <cfloat>
@@ -135,6 +135,21 @@ __device__ __forceinline__ float lanes_rank(float v, int n, int rank, int lane) 
     return __shfl_sync(0xffffffffu, v, __ffs(at) - 1);
 }
 
+// Bits at the end of a key in which the logits of one sign do not differ: so many neighbouring keys hold one logit at most.
+template <class T>
+constexpr int kGrain = 0;
+template <>
+constexpr int kGrain<__nv_bfloat16> = 16;
+template <>
+constexpr int kGrain<__half> = 13;
+template <class T>
+__device__ __forceinline__ uint32_t only_key(uint32_t lo) {   // the one of keys [lo, lo + 2^kGrain)
+    constexpr uint32_t kLow = (1u << kGrain<T>) - 1;
+    if (kLow == 0) return lo;
+    if (lo < 0x80000000u && (lo | kLow) != 0x7fffffffu) return lo | kLow;   // (keys of negative numbers end in ones; there is no -0)
+    return (max(lo, 0x80000000u) + kLow) & ~kLow;
+}
+
 // Four neighbouring logits in shared memory as fp32.
 __device__ __forceinline__ void quad_of(const float* x, float (&v)[4]) {
     const float4 q = *reinterpret_cast<const float4*>(x);
@@ -166,9 +181,9 @@ struct Interval {
     __device__ __forceinline__ int bin(float x, uint32_t key) const {
         return linear ? min(kSampleBins - 1, max(0, (int)((x - x_lo) * per))) : (int)((key - lo) >> shift);
     }
-    __device__ __forceinline__ void by_key(uint32_t l, uint32_t h) {
+    __device__ __forceinline__ void by_key(uint32_t l, uint32_t h, int grain) {
         lo = l, hi = h, linear = false;
-        shift = max(0, 24 - __clz(h - l));   // (256 << shift > h - l)
+        shift = max(grain, 24 - __clz(h - l));   // (256 << shift > h - l)
     }
     __device__ __forceinline__ void over(uint32_t l, uint32_t h, float floor) {   // what lies below `floor` is in the first bin
         lo = l, hi = h, linear = true;
@@ -177,8 +192,7 @@ struct Interval {
     }
 };
 
-// What runs once or twice a row is not inlined: the kernel's code is fetched line by line where it runs for the first time, and with all of this in it
-// several times over a row took 3 to 6 us longer.
+// (What runs once or twice a row is not inlined: the kernels stay small, and no slower.)
 __device__ __noinline__ uint64_t units_once(double c, double shift, float floor, const double* power, float x) { return Weigh{c, shift, floor, power}(x); }
 
 // The bin, from the highest on, in which what lies above, above_n logits and above_w units included, reaches the target.  Thread i < 256 brings the
@@ -296,7 +310,7 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
             for (int i = 0; i < 4; ++i) v[i] = v[i] == INFINITY ? 0.f : -INFINITY;
         }
     };
-    // f(j, v) for every block of the warp's run; those in shared memory first, and without looking where they lie (which doubles what a weight costs)
+    // f(j, v) for every block of the warp's run; those in shared memory first, and without looking where they lie
     const int near = min(held, run);
     auto for_blocks = [&](auto f) {
 #pragma unroll 2
@@ -335,7 +349,8 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
     }
     top = fmaxf(top, -INFINITY);   // (NaN where all are)
     if (by_count || by_share) {
-        // With `want` logits above the cut, a share of 1 - exp(-want / threads) of the threads' tops is: the warp's q-th largest one of 32, from 0 on.
+        // About `want` logits: enough that a cut somewhat too high still leaves k, or most rows' top-p, and few beside the room for kListed.
+        // With so many above the cut, a share of 1 - exp(-want / threads) of the threads' tops is: the warp's q-th largest one of 32, from 0 on.
         const float want = by_count ? fmaxf(192.f, 1.5f * (float)top_k + 64.f) : 512.f;
         const int q = min(31, (int)(32.f * (1.f - __expf(-want / (float)(ranks * kSampleThreads)))));
         uint32_t key = key_of(top), most = __reduce_max_sync(0xffffffffu, key);
@@ -525,6 +540,8 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
         }
         const bool direct = fits && (by_count ? n : above) >= target;
         bool listed_window = false;
+        uint32_t window_lo = 0, window_hi = 0;   // keys among which the threshold may lie, where they were too many for a list
+        uint64_t window_above = 0;
         uint32_t low_key = min(key_of(cut), m_key);   // of what is collected
         if (direct && rank != collector) return;
         if (!direct && fits && !by_count && cut > -FLT_MAX) {
@@ -536,13 +553,14 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
             __syncthreads();
             const int step = min(8, max(2, run));
             const float first_v = value_of(iv.lo);
+            const int drop = max(0, 64 - __clzll((long long)units_at(cut)) - 19);   // 19 bits of a weight: sums of 8192 of them fit 32
 #pragma unroll 1
             for (int j = step / 2; j < run; j += step) {
                 float v[4];
                 quad_at(warp, j, v);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (v[i] >= first_v && v[i] < cut) atomicAdd(&s.bins[0][0][iv.bin(v[i], 0)], (uint32_t)(units_at(v[i]) >> 24));
+                    if (v[i] >= first_v && v[i] < cut) atomicAdd(&s.bins[0][0][iv.bin(v[i], 0)], (uint32_t)(units_at(v[i]) >> drop));
             }
             all_here();
             uint64_t w = 0;
@@ -642,6 +660,10 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
                 if (listed_window) {
                     target -= over;
                     low_key = key_of(lo_v);
+                } else if (over < target && lo_v <= hi_v) {
+                    window_lo = max(key_of(lo_v), kLowestKey);
+                    window_hi = min(key_of(hi_v), m_key);
+                    window_above = over;
                 }
             }
         }
@@ -700,7 +722,7 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
                 SampleShared::Found f;
 #pragma unroll 1
                 for (;;) {   // 256 bins a pass, until the one where the target is reached has one logit, or one key, or (by number) is kept whole
-                    const int shift = max(0, 24 - __clz(hi - lo));
+                    const int shift = max(by_index ? 0 : kGrain<T>, 24 - __clz(hi - lo));
                     __syncthreads();
 #pragma unroll
                     for (int i = 0; i < kHeld; ++i) {
@@ -723,6 +745,7 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
                     above_w = f.above_w;
                     lo += (uint32_t)f.bin << shift;
                     hi = lo + min(hi - lo, (1u << shift) - 1);
+                    if (!by_index && shift == kGrain<T>) lo = hi = only_key<T>(lo);
                     if (lo == hi || f.n == 1 || (!by_weight && (direct || !by_index) && above_n + f.n == target)) break;
                 }
                 if (step == 4) {
@@ -763,8 +786,8 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
             }
             if (direct) return;
         }
+        all_here();   // (with the front part, or all have read the bins that told nothing)
         if (listed_window) {
-            all_here();
             keep = s.front[0];
             if (s.front[1] != 0) {
                 tie_key = s.front[1];
@@ -798,7 +821,12 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
         uint64_t above_w = 0;
         if (!by_count) target = max((uint64_t)1, share_of(fmaxf(top_p, 0.f), all, true));
         Interval iv;
-        iv.by_key(cut_key, m_key);
+        if (window_lo != 0 && window_lo <= window_hi) {
+            iv.by_key(window_lo, window_hi, kGrain<T>);
+            above_w = window_above;
+        } else {
+            iv.by_key(cut_key, m_key, kGrain<T>);
+        }
 #pragma unroll 1
         for (int pass = 0;; ++pass) {
             // bins of the interval's logits, summed over the cluster
@@ -860,8 +888,8 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
                         ties = (uint32_t)min((uint64_t)ties, target <= above_w ? 0 : (target - above_w + w - 1) / w);
                     }
                 }
-            } else if (!iv.linear && iv.shift == 0) {   // one key, of equal weights
-                const uint32_t key = iv.lo + f.bin;
+            } else if (!iv.linear && iv.shift == kGrain<T>) {   // one key, of equal weights
+                const uint32_t key = only_key<T>(iv.lo + ((uint32_t)f.bin << iv.shift));
                 const uint64_t w = max((uint64_t)1, f.w / f.n);
                 const uint32_t take = (uint32_t)(by_weight ? min((uint64_t)f.n, f.w == 0 ? f.n : (target - above_w + w - 1) / w) : target - above_n);
                 tie_key = key;
@@ -882,7 +910,7 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
                     ties = 0;
                     above_w += f.w;
                 } else {
-                    iv.by_key(lo, hi);
+                    iv.by_key(lo, hi, kGrain<T>);
                     done = false;
                 }
             }
@@ -899,7 +927,7 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
             bottom = keep;
             above_n = 0;
             above_w = 0;
-            iv.by_key(keep, m_key);
+            iv.by_key(keep, m_key, kGrain<T>);
         }
         }
     }

@@ -175,6 +175,25 @@ def test_many_at_the_threshold(ctx, vocab):
             check(ctx, x.to(dtype), u, **settings)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("vocab", [5000, 50257, 128256, 300000])
+def test_a_tail_of_small_weights(ctx, vocab, dtype):
+    """A threshold far down among logits that are each nothing beside the largest; or just behind a step, where nothing follows for long; and wide spreads."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(vocab)
+    x = torch.randn(8, vocab, device="cuda", generator=g) * 0.05 - torch.tensor([14.0, 16.5, 20.0, 28.0, 9.0, 3.0, 0.0, 0.0], device="cuda")[:, None]
+    x[:6, vocab // 3] = 0.0
+    x[4, 5:505] = 0.0
+    x[5, ::2] -= 12.0
+    x[6] *= 60.0
+    x[7] *= 400.0
+    u = torch.tensor([0.9999999, 0.99, 0.5, 0.999, 0.9, 0.97, 0.6, 0.8], device="cuda")
+    x = x.to(dtype)
+    for settings in (dict(top_p=0.9), dict(top_p=0.99), dict(top_p=0.9995), dict(top_p=0.9999999), dict(top_p=0.95, temperature=1.5),
+                     dict(top_p=0.99, temperature=20.0), dict(top_k=vocab // 2, top_p=0.95, temperature=1.2)):
+        check(ctx, x, u, **settings)
+
+
 def test_extreme_settings(ctx):
     x = logits(10, 3001, 8)
     for t in (0.0, -1.0, NAN, 1e-45, 1e-30, 1e-8, 1e-4, 1e4, 1e30, 3e38, INF):
