@@ -359,7 +359,8 @@ def sw_rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "
 
 
 class Rope:
-    """Frequencies on the device, how the pairs of a head lie, and (optional) the rows' positions (int32, one per row of the batch)."""
+    """Frequencies on the device, how the pairs of a head lie, and (optional) the rows' positions (int32, one per row of the batch).  What a call reads of
+    it is set once, here; the positions' values may change."""
 
     def __init__(self, turns, interleaved: bool = False, magnitude: float = 1.0, positions=None, device=None):
         import torch
@@ -369,18 +370,23 @@ class Rope:
             raise ValueError("turns must be float64, one per pair")
         if positions is not None and (positions.dtype != torch.int32 or positions.dim() != 1 or not positions.is_contiguous()):
             raise ValueError("positions must be a contiguous int32 tensor")
-        self.turns = turns.to("cuda" if device is None else device).contiguous()
-        self.interleaved, self.magnitude, self.positions = bool(interleaved), float(magnitude), positions
-        self.num_positions = None if positions is None else positions.numel()
+        self._turns = turns.to("cuda" if device is None else device).contiguous()
+        self._interleaved, self._magnitude, self._positions = bool(interleaved), float(magnitude), positions
+        self._num_positions = None if positions is None else positions.numel()
         self._structs = {}
 
+    turns = property(lambda self: self._turns)
+    interleaved = property(lambda self: self._interleaved)
+    magnitude = property(lambda self: self._magnitude)
+    positions = property(lambda self: self._positions)
+
     def struct(self, rows: int, strides) -> sw_rope:
-        if self.num_positions is not None and self.num_positions < rows:
-            raise ValueError(f"positions names {self.num_positions} rows, the batch has {rows}")
+        if self._num_positions is not None and self._num_positions < rows:
+            raise ValueError(f"positions names {self._num_positions} rows, the batch has {rows}")
         s = self._structs.get(strides)
         if s is None:
-            s = self._structs[strides] = sw_rope(self.turns.data_ptr(), 2 * self.turns.numel(), int(self.interleaved), self.magnitude,
-                                                 _ptr(self.positions), *strides)
+            s = self._structs[strides] = sw_rope(self._turns.data_ptr(), 2 * self._turns.numel(), int(self._interleaved), self._magnitude,
+                                                 _ptr(self._positions), *strides)
         return s
 
 
@@ -392,6 +398,8 @@ def _row_stride(name: str, t, rows: int, heads: int, head_dim: int, bf16, dense:
     width = heads * head_dim
     if stride[2] != 1 or (stride[1] != head_dim and heads > 1) or (dense and stride[0] != width and rows > 1):
         raise ValueError(f"{name}: {'rows' if dense else 'heads of a row'} must lie side by side")
+    if rows > 1 and stride[0] < width:   # (0, of an expanded tensor, would be taken for dense)
+        raise ValueError(f"{name}: rows overlap")
     return stride[0] if rows > 1 else width
 
 

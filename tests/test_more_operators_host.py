@@ -1,11 +1,14 @@
 """What rotary positions, cross attention and sampling refuse, and the frequencies of the rotation, without a GPU."""
 import ctypes as C
 import math
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2609_07883_b200 import binding as B
+from paper_2609_07883_b200 import workloads as W
 
 # seven roundings of fp64 (power, quotient, blend), and a power whose exponent's rounding counts ln(base^(2i/d)) times: 2^-53 (7 + 14)
 REL = 2.0 ** -48
@@ -85,3 +88,25 @@ def test_frequencies_null_and_unknown():
 def test_null_context(call):
     assert call() == B.SW_ERR_INVALID_ARG
     assert "null context" in B.sw_last_error()
+
+
+def test_rows_of_an_expanded_tensor_are_refused():
+    """One row expanded to many has a stride of 0, which the C interface takes for dense rows: it would read behind the row."""
+    shape = W.AttnShape(8, 2, 64)
+    ctx, batch = SimpleNamespace(shape=shape, handle=None), SimpleNamespace(rows=5, struct=None)
+    turns, magnitude = B.sw_rope_frequencies(64)
+    rope = B.Rope(torch.from_numpy(turns), magnitude=magnitude, device="cpu")
+    q, k = torch.zeros(5, 8, 64, dtype=torch.bfloat16), torch.zeros(5, 2, 64, dtype=torch.bfloat16)
+    for bad_q, bad_k in ((q[:1].expand(5, 8, 64), k), (q, k[:1].expand(5, 2, 64)), (q.as_strided((5, 8, 64), (256, 64, 1)), k)):
+        with pytest.raises(ValueError, match="rows overlap"):
+            B.sw_rope_run(ctx, batch, rope, bad_q, bad_k, torch.empty_like(q), torch.empty_like(k), stream=0)
+        with pytest.raises(ValueError, match="rows overlap"):
+            B.sw_rope_append(ctx, None, batch, rope, bad_q, bad_k, k, torch.empty_like(q), stream=0)
+
+
+def test_a_rope_is_set_once():
+    """Its calls read a structure made once: an attribute that is exchanged later would not be seen."""
+    rope = B.Rope(torch.zeros(32, dtype=torch.float64), device="cpu", positions=torch.zeros(3, dtype=torch.int32))
+    for name in ("turns", "interleaved", "magnitude", "positions"):
+        with pytest.raises(AttributeError):
+            setattr(rope, name, getattr(rope, name))
