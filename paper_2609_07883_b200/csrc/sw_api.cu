@@ -222,7 +222,7 @@ sw_status check_batch(const sw_ctx* ctx, const sw_batch* b, const char* who, Chu
 
 namespace {
 // What a context asks of its device.  The driver takes 1.2 ms for each clock rate (and 2.5 for all properties at once, which are not asked for), so a process asks
-// once per device: a context is created in 35 us (80 where it gets the streams of host-buffer iterations) instead of 5 ms.
+// once per device: a context is created in 20 to 35 us (80 where it gets the streams of host-buffer iterations) instead of 5 ms.
 struct DeviceFacts {
     int major, minor, sms, mem_khz, bus_bits, sm_khz;
 };

@@ -21,6 +21,9 @@
 //   - otherwise (a large k, more than hundreds of equal logits at the threshold) all CTAs search their stretches by bins, and read one another's.
 // Bound by the logits' bytes, by the instructions of a weight where all are needed (some 20 a logit, nine of them in 64 bits, and a conversion), and for a
 // few rows by the chain of two cluster barriers and the passes.
+// Measured, launches in a graph: one row of 128256 fp32 logits 8.5 us, the largest alone 3.9, with top-k 50 and top-p 13.4, 0.95 of an open row 37; 256 such rows (131 MB, 20 us
+// at a copy's rate) 71, 30, 68 and 342; 128 rows of 32003 without limits 14.1.  The weights of 256 rows take 27 us of the 64-bit pipes and the conversions alone
+// (30 cycles for 32 logits and scheduler); the rest of the 71 is loads, sums and the waits for both, as a third CTA an SM hides a part of them only.
 #include <cfloat>
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
