@@ -647,7 +647,7 @@ sw_status run_rope(sw_ctx* ctx, void* kv_pool, bool append, const sw_batch* batc
     const int64_t q_stride = rope->q_stride ? rope->q_stride : q_width, k_stride = rope->k_stride ? rope->k_stride : kv_width,
                   v_stride = rope->v_stride ? rope->v_stride : kv_width;
     if (q_stride < q_width || k_stride < kv_width || (append && v_stride < kv_width) || ((q_stride | k_stride | (append ? v_stride : 0)) & 7) != 0 ||
-        std::max(q_stride, std::max(k_stride, v_stride)) > (int64_t)1 << 40)
+        std::max(q_stride, std::max(k_stride, v_stride)) > (int64_t)1 << 31)   // (times the rows, in bytes, that fits 64 bits)
         return sw_fail(SW_ERR_INVALID_ARG, "%s: strides of %lld, %lld, %lld elements (multiples of 8, a row's width at least)", who, (long long)q_stride,
                        (long long)k_stride, (long long)v_stride);
     const int64_t rows = ch.rows + batch->num_decode;
