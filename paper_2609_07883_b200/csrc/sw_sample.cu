@@ -246,6 +246,7 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int row = (int)blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (ranks > 1) cluster_arrive();   // (waited for in front of the first store to another CTA, behind the loads)
     grid_launch_dependents();
     grid_dependency_wait();
     auto all_here = [&] {
@@ -371,6 +372,7 @@ __global__ void __launch_bounds__(kThreadsFor<kCtas>, kCtas) sw_sample_kernel(co
         if (lane == 0) s.warp_top[warp] = top;
     }
     __syncthreads();
+    if (ranks > 1) cluster_wait();   // all CTAs of the row have started: their shared memory may be written
     if (warp == 0) {
         float t = lane < kSampleWarps ? s.warp_top[lane] : -INFINITY, cut = 0.f;
         if (by_count || by_share) cut = lanes_rank(lane < kSampleWarps ? s.warp_cut[lane] : -INFINITY, kSampleWarps, min(kSampleWarps, blocks) / 2, lane);
