@@ -7,6 +7,7 @@ the library's kernels.  Loading fails loudly if ``libsloweave.so`` has not been 
 from __future__ import annotations
 
 import ctypes as C
+import math
 from pathlib import Path
 
 import numpy as np
@@ -429,8 +430,21 @@ def sw_rope_run(ctx: Context, batch: DeviceBatch, rope: Rope, q, k, q_out, k_out
            "sw_rope_run")
 
 
+def _check_dense(name: str, t, dtype, *sizes: int) -> None:
+    # (None is the library's to refuse)
+    if t is not None and (t.dtype is not dtype or not t.is_contiguous() or t.numel() < math.prod(sizes)):
+        raise ValueError(f"{name} must be contiguous, {str(dtype)[6:]} " + "".join(f"[{n}]" for n in sizes))
+
+
 def sw_cross_attn_run(ctx: Context, kv_pool, batch: DeviceBatch, q, out, lse=None, stream=None) -> None:
-    """As ``sw_mixed_attn_run``, but the rows of a chunk attend the ``prefix_len`` keys of its page list, all of them; no keys: zeros."""
+    """As ``sw_mixed_attn_run``, but the rows of a chunk attend the ``prefix_len`` keys of its page list, all of them; no keys: zeros.  ``q``, ``out``
+    (bf16) and ``lse`` (fp32) are dense, a row for each of the batch's at least."""
+    import torch
+
+    sh, rows = ctx.shape, batch.rows
+    _check_dense("q", q, torch.bfloat16, rows, sh.num_q_heads, sh.head_dim)
+    _check_dense("out", out, torch.bfloat16, rows, sh.num_q_heads, sh.head_dim)
+    _check_dense("lse", lse, torch.float32, rows, sh.num_q_heads)
     _check(_lib.sw_cross_attn_run(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), _ptr(q), _ptr(out), _ptr(lse), _stream_handle(stream)),
            "sw_cross_attn_run")
 
