@@ -372,6 +372,8 @@ class Rope:
         if positions is not None and (positions.dtype != torch.int32 or positions.dim() != 1 or not positions.is_contiguous()):
             raise ValueError("positions must be a contiguous int32 tensor")
         self._turns = turns.to("cuda" if device is None else device).contiguous()
+        if positions is not None and positions.device != self._turns.device:
+            raise ValueError(f"positions must be on {self._turns.device}, not {positions.device}")
         self._interleaved, self._magnitude, self._positions = bool(interleaved), float(magnitude), positions
         self._num_positions = None if positions is None else positions.numel()
         self._structs = {}
@@ -389,6 +391,13 @@ class Rope:
             s = self._structs[strides] = sw_rope(self._turns.data_ptr(), 2 * self._turns.numel(), int(self._interleaved), self._magnitude,
                                                  _ptr(self._positions), *strides)
         return s
+
+
+def _check_devices(ctx: Context, **tensors) -> None:
+    # addresses of the host or of another device would go to the kernel
+    for name, t in tensors.items():
+        if t is not None and t.device != ctx.device:
+            raise ValueError(f"{name} must be on {ctx.device}, not {t.device}")
 
 
 def _row_stride(name: str, t, rows: int, heads: int, head_dim: int, bf16, dense: bool = False) -> int:
@@ -413,12 +422,14 @@ def _rope_rows(ctx: Context, batch: DeviceBatch, rope: Rope, q, k, v, q_out, k_o
     _row_stride("q_out", q_out, rows, hq, d, bf16, True)
     if k_out is not None:
         _row_stride("k_out", k_out, rows, hkv, d, bf16, True)
+    _check_devices(ctx, batch=batch.decode_kv_len, rope=rope.turns, q=q, k=k, v=v, q_out=q_out, k_out=k_out)
     return rope.struct(rows, strides)
 
 
 def sw_rope_append(ctx: Context, kv_pool, batch: DeviceBatch, rope: Rope, q, k_new, v_new, q_out, stream=None) -> None:
     """Rotated queries to ``q_out``, rotated keys and the values to their pages.  ``q``, ``k_new``, ``v_new`` may be slices of one projection's rows."""
     s = _rope_rows(ctx, batch, rope, q, k_new, v_new, q_out, None)
+    _check_devices(ctx, kv_pool=kv_pool)
     _check(_lib.sw_rope_append(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), C.byref(s), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(q_out),
                                _stream_handle(stream)), "sw_rope_append")
 
@@ -445,6 +456,7 @@ def sw_cross_attn_run(ctx: Context, kv_pool, batch: DeviceBatch, q, out, lse=Non
     _check_dense("q", q, torch.bfloat16, rows, sh.num_q_heads, sh.head_dim)
     _check_dense("out", out, torch.bfloat16, rows, sh.num_q_heads, sh.head_dim)
     _check_dense("lse", lse, torch.float32, rows, sh.num_q_heads)
+    _check_devices(ctx, kv_pool=kv_pool, batch=batch.decode_kv_len, q=q, out=out, lse=lse)
     _check(_lib.sw_cross_attn_run(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), _ptr(q), _ptr(out), _ptr(lse), _stream_handle(stream)),
            "sw_cross_attn_run")
 
@@ -461,6 +473,7 @@ def sw_sample_run(ctx: Context, logits, uniform, tokens, log_probs=None, tempera
     for t, kind in ((uniform, f32), (tokens, i32), (log_probs, f32), (temperature, f32), (top_k, i32), (top_p, f32), (min_p, f32)):
         if t is not None and (t.dtype is not kind or t.numel() < rows or not t.is_contiguous()):
             raise ValueError("uniform, log_probs, temperature, top_p, min_p (fp32), tokens and top_k (int32) must be contiguous, one value per row")
+    _check_devices(ctx, logits=logits, uniform=uniform, tokens=tokens, log_probs=log_probs, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
     s = sw_sampling(logits.data_ptr(), dtype, rows, vocab, logits.stride(0) if rows > 1 else vocab, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
                     _ptr(uniform))
     _check(_lib.sw_sample_run(ctx.handle, C.byref(s), _ptr(tokens), _ptr(log_probs), _stream_handle(stream)), "sw_sample_run")
