@@ -645,8 +645,8 @@ sw_status run_rope(sw_ctx* ctx, void* kv_pool, bool append, const sw_batch* batc
         return sw_fail(SW_ERR_UNSUPPORTED, "%s: rotary_dim %d (multiples of 16 up to the head size, %d)", who, rope->rotary_dim, l.head_dim);
     const int64_t q_width = (int64_t)l.num_q_heads * l.head_dim, kv_width = (int64_t)l.num_kv_heads * l.head_dim;
     const int64_t q_stride = rope->q_stride ? rope->q_stride : q_width, k_stride = rope->k_stride ? rope->k_stride : kv_width,
-                  v_stride = rope->v_stride ? rope->v_stride : kv_width;
-    if (q_stride < q_width || k_stride < kv_width || (append && v_stride < kv_width) || ((q_stride | k_stride | (append ? v_stride : 0)) & 7) != 0 ||
+                  v_stride = append && rope->v_stride ? rope->v_stride : kv_width;   // (ignored where there are no values)
+    if (q_stride < q_width || k_stride < kv_width || v_stride < kv_width || ((q_stride | k_stride | v_stride) & 7) != 0 ||
         std::max(q_stride, std::max(k_stride, v_stride)) > (int64_t)1 << 31)   // (times the rows, in bytes, that fits 64 bits)
         return sw_fail(SW_ERR_INVALID_ARG, "%s: strides of %lld, %lld, %lld elements (multiples of 8, a row's width at least)", who, (long long)q_stride,
                        (long long)k_stride, (long long)v_stride);
