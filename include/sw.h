@@ -255,7 +255,7 @@ sw_status sw_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, 
 
 /* sw_kv_append of keys that are rotated on the way, with the queries: q [C+n][num_q_heads][head_dim] goes to q_out, k_new rotated and v_new as it is to
  * their places in the pool.  Places and problems as sw_kv_append's (of a row that has no place the queries are rotated all the same).  Followed by
- * sw_mixed_attn_run or one of its kind on q_out.  q_out may be q where q is dense; it overlaps no other input. */
+ * sw_mixed_attn_run or one of its kind on q_out.  q_out may be q where q is dense; it overlaps no other input, nor the pool. */
 sw_status sw_rope_append(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const sw_rope* rope, const void* q, const void* k_new, const void* v_new,
                          void* q_out, void* stream);
 

@@ -662,6 +662,8 @@ sw_status run_rope(sw_ctx* ctx, void* kv_pool, bool append, const sw_batch* batc
         for (int i = 0; i < (append ? 3 : 2); ++i)
             if (rows_overlap(out[o], in[i], rows) && !(o == i && out[o].at == in[i].at && out[o].stride == in[i].stride))
                 return sw_fail(SW_ERR_INVALID_ARG, "%s: %s overlaps %s", who, out[o].name, in[i].name);
+    const int64_t pool_elements = l.num_pages * 2 * l.num_kv_heads * sw::kPageSize * l.head_dim;
+    if (append && rows_overlap(out[0], Rows{kv_pool, 0, pool_elements, "the pool"}, rows)) return sw_fail(SW_ERR_INVALID_ARG, "%s: q_out overlaps the pool", who);
     if (!append && rows_overlap(out[0], out[1], rows)) return sw_fail(SW_ERR_INVALID_ARG, "%s: q_out overlaps k_out", who);
     st = check_current_device(ctx, who);
     if (st != SW_OK) return st;

@@ -41,3 +41,24 @@ def test_append_takes_the_stride_of_values():
         tensors = [x.data_ptr() for x in (c.q, c.k_new, c.v_new, c.out)]
         assert B._lib.sw_rope_append(c.ctx.handle, c.pool.data_ptr(), C.byref(c.db.struct), C.byref(s), *tensors, stream()) == B.SW_ERR_INVALID_ARG
     c.ok()
+
+
+def test_append_refuses_queries_over_the_pool():
+    """Other rows' keys go there in the same launch."""
+    c, rope = setup_case()
+    n, size = c.out.numel(), c.pool.numel()
+    one = torch.zeros(n + size + n, dtype=torch.bfloat16, device=c.dev)
+    pool = one[n:n + size].view(c.pool.shape)
+    pool.copy_(c.pool)
+    at = lambda first: one[first:first + n].view(c.out.shape)  # noqa: E731
+    for first in (n, n + 64, 8, n + size // 2 // 8 * 8, size, n + size - 8):
+        with pytest.raises(B.SwError, match="overlaps the pool") as e:
+            B.sw_rope_append(c.ctx, pool, c.db, rope, c.q, c.k_new, c.v_new, at(first))
+        assert e.value.status == B.SW_ERR_INVALID_ARG
+    torch.cuda.synchronize()
+    assert torch.equal(pool.nan_to_num(), c.pool.nan_to_num())
+    B.sw_rope_append(c.ctx, c.pool, c.db, rope, c.q, c.k_new, c.v_new, c.out)
+    for first in (0, n + size):                       # its neighbours on both sides
+        B.sw_rope_append(c.ctx, pool, c.db, rope, c.q, c.k_new, c.v_new, at(first))
+        c.ok()
+        assert torch.equal(at(first), c.out) and torch.equal(pool.nan_to_num(), c.pool.nan_to_num())
