@@ -63,8 +63,10 @@ def gpu_executor(ctx, pools, shape: W.AttnShape, c_max: int, max_decode: int, se
 
     With ``rope`` (a ``binding.Rope``) a layer's queries and new keys are rotated as they are appended, one launch, and the attention is the other.
     With ``vocab`` the iteration ends with the draw of a token for every decode and for the last row of every chunk, from random logits of that many
-    entries; ``execute.tokens`` holds them (decodes first).  ``execute.extra_ns`` is what these two cost at the largest batch, measured here: a cost
-    table of attention iterations does not hold it, so it belongs into the controller's margin."""
+    entries; ``execute.tokens`` holds them (decodes first).  ``execute.extra_ns`` is what these two cost, measured here: a cost table of iterations whose append
+    and attention are one launch does not hold it, so it belongs into the controller's margin.  It is the most that the layers' two launches took, less the median of
+    the one launch (at the largest batch or with one request, where a call's set-up counts: the larger), and the most that the draw of the largest batch took.
+    Measuring the layers writes new rows to pages of the pools, as the iterations do."""
     import torch
 
     from . import binding as B
@@ -91,38 +93,44 @@ def gpu_executor(ctx, pools, shape: W.AttnShape, c_max: int, max_decode: int, se
         B.sw_sample_run(ctx, logits[:count], u, tokens, log_probs, *settings)
         execute.tokens = tokens[:count]
 
-    def execute(batch: W.MixedBatch) -> int:
-        db = B.DeviceBatch(batch, dev)
-        rows = batch.num_rows
-        ev0.record()
+    def layers(db, turn: bool) -> None:
+        rows = db.rows
         for pool_t in pools:
-            if rope is None:
-                B.sw_mixed_iteration_run(ctx, pool_t, db, k_new[:rows], v_new[:rows], q[:rows], out[:rows])
-            else:
+            if turn:
                 B.sw_rope_append(ctx, pool_t, db, rope, q[:rows], k_new[:rows], v_new[:rows], turned[:rows])
                 B.sw_mixed_attn_run(ctx, pool_t, db, turned[:rows], out[:rows])
-        if vocab:
-            draw(batch.num_decode + len(batch.chunks()))
+            else:
+                B.sw_mixed_iteration_run(ctx, pool_t, db, k_new[:rows], v_new[:rows], q[:rows], out[:rows])
+
+    def timed(step) -> int:
+        ev0.record()
+        step()
         ev1.record()
         ev1.synchronize()
         return int(ev0.elapsed_time(ev1) * 1e6)
 
-    execute.tokens, execute.extra_ns = None, 0
-    if rope is not None or vocab:
-        keys = torch.empty_like(k_new) if rope is not None else None
-        db = B.DeviceBatch(W.make_batch(shape, ctx.layout.num_pages, [1] * max_decode, 0, c_max, np.random.default_rng(seed)), dev)
-        times = []
-        for _ in range(5):
-            ev0.record()
-            if rope is not None:
-                for _ in pools:
-                    B.sw_rope_run(ctx, db, rope, q, k_new, turned, keys)
+    def execute(batch: W.MixedBatch) -> int:
+        db = B.DeviceBatch(batch, dev)
+
+        def step():
+            layers(db, rope is not None)
             if vocab:
-                draw(draws_max)
-            ev1.record()
-            ev1.synchronize()
-            times.append(int(ev0.elapsed_time(ev1) * 1e6))
-        execute.extra_ns, execute.tokens = max(times[1:]), None          # (the first one warms up)
+                draw(batch.num_decode + len(batch.chunks()))
+        return timed(step)
+
+    execute.tokens, execute.extra_ns = None, 0
+    times = lambda step: sorted([timed(step) for _ in range(31)][1:])  # noqa: E731 (the first one warms up)
+    if rope is not None:
+        num_pages = ctx.layout.num_pages
+        requests = min(max_decode, num_pages)
+        chunk = min(c_max, (num_pages - requests) * shape.page_size)
+        for lens, tokens_new in (([1] * requests, chunk), ([1], 0) if requests else ([], min(chunk, 1))):
+            db = B.DeviceBatch(W.make_batch(shape, num_pages, lens, 0, tokens_new, np.random.default_rng(seed)), dev)
+            one, two = times(lambda: layers(db, False)), times(lambda: layers(db, True))
+            execute.extra_ns = max(execute.extra_ns, two[-1] - one[len(one) // 2])
+    if vocab:
+        execute.extra_ns += times(lambda: draw(draws_max))[-1]
+        execute.tokens = None
     return execute
 
 
