@@ -29,4 +29,4 @@ def test_many_launches_in_a_row(dtype, vocab, rows, settings):
     torch.cuda.synchronize()
     assert bool((tokens == tokens[0]).all()) and bool((log_probs == log_probs[0]).all())
     for r in {0, rows // 2, rows - 1}:
-        assert int(tokens[0, r]) == M.draw(x[r].double().cpu().numpy(), float(u[r]), **settings)[0]
+        assert int(tokens[0, r]) == M.draw(x[r].double().cpu().numpy(), float(u[r]), **{k: c[0].item() for k, c in columns.items()})[0]
