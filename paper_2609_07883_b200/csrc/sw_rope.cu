@@ -1,8 +1,9 @@
 // Rotary positions: the iteration's queries and new keys turned by their positions, the keys written to their pages with their values (or to a tensor).
 //
 // Pair (a, b) of a head becomes (a cos - b sin, b cos + a sin) of its angle, position times the pair's frequency.  Far positions times fp32
-// frequencies are off by whole turns' parts (131072 positions: 0.008 radians), so the frequencies are turns per position in 64 bits: their product
-// with the position less its nearest integer is exact to 2^-37 of a turn, and only that goes to 32 bits, with the sine and cosine of it.
+// frequencies are off by whole turns' parts (131072 positions: 0.008 radians), so the frequencies are turns per position in 64 bits.  Their product
+// with the position is off by 2^-53 of itself for its rounding and as much for the frequency's (the nearest integer is taken off without any): less than 2^-37 of a turn
+// up to position 2^17, 2^-23 at 2^31 - 1.  Only what is left of a turn goes to 32 bits, with the sine and cosine of it.
 //
 // A lane holds 16 elements of a head, both elements of its eight pairs: two 16-byte pieces `rotary / 16` pieces apart, in either layout.  Lanes
 // past the rotated part hold the rest.  4 (head size 128) or 8 heads lie side by side in a warp, so a lane's angles are the same for all heads of a row
