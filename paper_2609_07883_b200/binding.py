@@ -224,6 +224,7 @@ class DeviceBatch:
         self.decode_kv_len = to(batch.decode_kv_len)
         self.decode_page_indptr = to(batch.decode_page_indptr)
         self.decode_pages = to(batch.decode_pages)
+        self.device = self.decode_kv_len.device
         nch, cp, cl, ci, self._chunk_keep = _chunk_fields(batch)
         self.struct = sw_batch(batch.prefix_len, batch.chunk_len, self.prefill_pages.data_ptr(),
                                int(self.prefill_pages.numel()), batch.num_decode, self.decode_kv_len.data_ptr(),
@@ -375,6 +376,7 @@ class Rope:
         if positions is not None and positions.device != self._turns.device:
             raise ValueError(f"positions must be on {self._turns.device}, not {positions.device}")
         self._interleaved, self._magnitude, self._positions = bool(interleaved), float(magnitude), positions
+        self._device = self._turns.device
         self._num_positions = None if positions is None else positions.numel()
         self._structs = {}
 
@@ -382,6 +384,7 @@ class Rope:
     interleaved = property(lambda self: self._interleaved)
     magnitude = property(lambda self: self._magnitude)
     positions = property(lambda self: self._positions)
+    device = property(lambda self: self._device)
 
     def struct(self, rows: int, strides) -> sw_rope:
         if self._num_positions is not None and self._num_positions < rows:
@@ -393,11 +396,13 @@ class Rope:
         return s
 
 
-def _check_devices(ctx: Context, **tensors) -> None:
+def _check_devices(ctx: Context, names: str, *tensors) -> None:
     # addresses of the host or of another device would go to the kernel
-    for name, t in tensors.items():
-        if t is not None and t.device != ctx.device:
-            raise ValueError(f"{name} must be on {ctx.device}, not {t.device}")
+    device = ctx.device
+    for t in tensors:
+        if t is not None and t.device != device:
+            name = names.split()[[x is t for x in tensors].index(True)]
+            raise ValueError(f"{name} must be on {device}, not {t.device}")
 
 
 def _row_stride(name: str, t, rows: int, heads: int, head_dim: int, bf16, dense: bool = False) -> int:
@@ -413,7 +418,7 @@ def _row_stride(name: str, t, rows: int, heads: int, head_dim: int, bf16, dense:
     return stride[0] if rows > 1 else width
 
 
-def _rope_rows(ctx: Context, batch: DeviceBatch, rope: Rope, q, k, v, q_out, k_out) -> sw_rope:
+def _rope_rows(ctx: Context, batch: DeviceBatch, rope: Rope, q, k, v, q_out, k_out, kv_pool) -> sw_rope:
     import torch
 
     sh, rows, bf16 = ctx.shape, batch.rows, torch.bfloat16
@@ -422,21 +427,20 @@ def _rope_rows(ctx: Context, batch: DeviceBatch, rope: Rope, q, k, v, q_out, k_o
     _row_stride("q_out", q_out, rows, hq, d, bf16, True)
     if k_out is not None:
         _row_stride("k_out", k_out, rows, hkv, d, bf16, True)
-    _check_devices(ctx, batch=batch.decode_kv_len, rope=rope.turns, q=q, k=k, v=v, q_out=q_out, k_out=k_out)
+    _check_devices(ctx, "batch rope q k v q_out k_out kv_pool", batch, rope, q, k, v, q_out, k_out, kv_pool)
     return rope.struct(rows, strides)
 
 
 def sw_rope_append(ctx: Context, kv_pool, batch: DeviceBatch, rope: Rope, q, k_new, v_new, q_out, stream=None) -> None:
     """Rotated queries to ``q_out``, rotated keys and the values to their pages.  ``q``, ``k_new``, ``v_new`` may be slices of one projection's rows."""
-    s = _rope_rows(ctx, batch, rope, q, k_new, v_new, q_out, None)
-    _check_devices(ctx, kv_pool=kv_pool)
+    s = _rope_rows(ctx, batch, rope, q, k_new, v_new, q_out, None, kv_pool)
     _check(_lib.sw_rope_append(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), C.byref(s), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(q_out),
                                _stream_handle(stream)), "sw_rope_append")
 
 
 def sw_rope_run(ctx: Context, batch: DeviceBatch, rope: Rope, q, k, q_out, k_out, stream=None) -> None:
     """Rotated queries and keys, for the calls that append by themselves; ``q_out`` may be ``q`` and ``k_out`` ``k``."""
-    s = _rope_rows(ctx, batch, rope, q, k, None, q_out, k_out)
+    s = _rope_rows(ctx, batch, rope, q, k, None, q_out, k_out, None)
     _check(_lib.sw_rope_run(ctx.handle, C.byref(batch.struct), C.byref(s), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _stream_handle(stream)),
            "sw_rope_run")
 
@@ -456,7 +460,7 @@ def sw_cross_attn_run(ctx: Context, kv_pool, batch: DeviceBatch, q, out, lse=Non
     _check_dense("q", q, torch.bfloat16, rows, sh.num_q_heads, sh.head_dim)
     _check_dense("out", out, torch.bfloat16, rows, sh.num_q_heads, sh.head_dim)
     _check_dense("lse", lse, torch.float32, rows, sh.num_q_heads)
-    _check_devices(ctx, kv_pool=kv_pool, batch=batch.decode_kv_len, q=q, out=out, lse=lse)
+    _check_devices(ctx, "kv_pool batch q out lse", kv_pool, batch, q, out, lse)
     _check(_lib.sw_cross_attn_run(ctx.handle, _ptr(kv_pool), C.byref(batch.struct), _ptr(q), _ptr(out), _ptr(lse), _stream_handle(stream)),
            "sw_cross_attn_run")
 
@@ -473,7 +477,7 @@ def sw_sample_run(ctx: Context, logits, uniform, tokens, log_probs=None, tempera
     for t, kind in ((uniform, f32), (tokens, i32), (log_probs, f32), (temperature, f32), (top_k, i32), (top_p, f32), (min_p, f32)):
         if t is not None and (t.dtype is not kind or t.numel() < rows or not t.is_contiguous()):
             raise ValueError("uniform, log_probs, temperature, top_p, min_p (fp32), tokens and top_k (int32) must be contiguous, one value per row")
-    _check_devices(ctx, logits=logits, uniform=uniform, tokens=tokens, log_probs=log_probs, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+    _check_devices(ctx, "logits uniform tokens log_probs temperature top_k top_p min_p", logits, uniform, tokens, log_probs, temperature, top_k, top_p, min_p)
     s = sw_sampling(logits.data_ptr(), dtype, rows, vocab, logits.stride(0) if rows > 1 else vocab, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
                     _ptr(uniform))
     _check(_lib.sw_sample_run(ctx.handle, C.byref(s), _ptr(tokens), _ptr(log_probs), _stream_handle(stream)), "sw_sample_run")

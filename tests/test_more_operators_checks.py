@@ -17,7 +17,7 @@ def context(device=torch.device("cpu")):
 
 
 def batch(device="cpu"):
-    return SimpleNamespace(rows=ROWS, struct=B.sw_batch(), decode_kv_len=torch.zeros(2, dtype=torch.int32, device=device))
+    return SimpleNamespace(rows=ROWS, struct=B.sw_batch(), device=torch.device(device))
 
 
 def rows(heads=8, count=ROWS, dtype=BF16, d=64):
