@@ -227,7 +227,8 @@ sw_status sw_kv_evict(sw_ctx* ctx, void* kv_pool, const sw_batch* batch, const s
 
 /* Rotary positions.  Pair i (of rotary_dim / 2) of every query and key head is turned by t = position * turns[i] turns: its elements (a, b) become
  * m (a cos t - b sin t) and m (b cos t + a sin t), m = magnitude.  The pair's elements are i and i + rotary_dim / 2, or, interleaved, 2i and 2i + 1; those
- * from rotary_dim on are left as they are.  rotary_dim: a multiple of 16, the head size at most.  Angles are worked out in 64 bits, rotations in 32.
+ * from rotary_dim on are left as they are.  rotary_dim: a multiple of 16, the head size at most.  Turns are worked out in 64 bits; what is left of one, its
+ * sine and cosine, and the rotation in 32.
  * positions: NULL for the batch's own (P + j for chunk row j, decode_kv_len[i] - 1 for request i), or one int32 per row, where a row's place in the
  * cache is not its position (after an eviction, say).
  * Strides: elements between rows, multiples of 8; 0 for dense rows.  So q, k and v can be slices of one projection's rows; what is written is dense. */
@@ -266,9 +267,12 @@ sw_status sw_rope_run(sw_ctx* ctx, const sw_batch* batch, const sw_rope* rope, c
 
 /* Cross attention: sw_mixed_attn_run over the cached states of an encoder, whose number has nothing to do with the rows'.  prefix_len (or
  * chunk_prefix_lens[j]) is the number of keys of a chunk's source, 0 or more, and every row of the chunk attends all of them; its page list needs
- * ceil(P / 16) entries.  decode_kv_len[i], 0 or more, likewise (where no list has an entry the lists may be NULL).  Rows without keys are zero, with a log-sum-exp of minus infinity.  The keys and values are
- * written once, by sw_kv_append with a batch of their own (prefix_len 0, chunk_len the number of states).  List the chunk with the longest items
- * (keys) first.  One launch, and one more for each chunk without keys.  Asynchronous. */
+ * ceil(P / 16) entries.  decode_kv_len[i], 0 or more, likewise (where no list has an entry the lists may be NULL).  Rows without keys are zero,
+ * with a log-sum-exp of minus infinity.  The keys and values are written once, by sw_kv_append with a batch of their own (prefix_len 0, chunk_len the
+ * number of states).  List the chunk with the longest items (keys) first.
+ * What is rounded beside the output is what sw_mixed_attn_run rounds: softmax weights to bf16, the values' type, where they meet the values (their sum is kept
+ * in 32 bits), and 2^x to 7.5e-5.
+ * One launch, and one more for each chunk without keys.  Asynchronous. */
 sw_status sw_cross_attn_run(sw_ctx* ctx, const void* kv_pool, const sw_batch* batch, const void* q, void* out, float* lse, void* stream);
 
 /* The next tokens: one draw a row from device logits [rows][vocab], row_stride elements apart.  Arrays are device memory, one value per row;
@@ -282,7 +286,7 @@ sw_status sw_cross_attn_run(sw_ctx* ctx, const void* kv_pool, const sw_batch* ba
  *   tokens[r] is the first index up to which the kept weights sum to more than uniform[r] (in [0, 1); others count as the nearest such) times their total;
  *   log_probs[r] (NULL: not asked for) the logarithm of its share of that total, 0 at temperature 0.
  * A row without any weight gets token -1 and minus infinity.  Sums are exact: the result depends on no order, and is the same in every batch.
- * vocab: at most 393216.  One launch, asynchronous; it uses nothing of the context but its device, so calls on several streams may overlap. */
+ * tokens and log_probs overlap none of the other arrays.  vocab: at most 393216.  One launch, asynchronous; it uses nothing of the context but its device, so calls on several streams may overlap. */
 typedef enum { SW_DTYPE_F32 = 0, SW_DTYPE_BF16 = 1, SW_DTYPE_F16 = 2 } sw_dtype;
 #define SW_SAMPLE_MAX_ROWS 65536
 typedef struct {

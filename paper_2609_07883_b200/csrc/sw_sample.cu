@@ -21,9 +21,14 @@
 //   - otherwise (a large k, more than hundreds of equal logits at the threshold) all CTAs search their stretches by bins, and read one another's.
 // Bound by the logits' bytes, by the instructions of a weight where all are needed (some 20 a logit, nine of them in 64 bits, and a conversion), and for a
 // few rows by the chain of two cluster barriers and the passes.
-// Measured, launches in a graph: one row of 128256 fp32 logits 8.5 us, the largest alone 3.9, with top-k 50 and top-p 13.4, 0.95 of an open row 37; 256 such rows (131 MB, 20 us
-// at a copy's rate) 71, 30, 68 and 342; 128 rows of 32003 without limits 14.1.  The weights of 256 rows take 27 us of the 64-bit pipes and the conversions alone
+// Measured, launches in a graph: one row of 128256 fp32 logits 8.5 us, the largest alone 3.9, top-k 50 12.2, with top-p too 13.4, min-p 7.8, 0.95 of an open row 37; 256 such
+// rows (131 MB, 20 us at a copy's rate) 71, 29, 64, 68, 64 and 342; 128 rows of 32003 without limits 14.1.  256 rows of 16 bits (10 us of bytes) 71, 27, 64, 69 and 66.
+// So bytes bound none of them.  The largest alone: a CTA loads, then compares, then ends, and three an SM overlap that in part (issue slots 37 %).  Top-k: one CTA of the row has the
+// searches, a chain of barriers, and its third of the SM's shared memory meanwhile (issue slots 36 %).  Min-p: few weights (64-bit pipes 4 %),
+// but a second sweep that looks block by block whether there are any (49 %).  Without limits: the weights take 27 us of the 64-bit pipes and the conversions alone
 // (30 cycles for 32 logits and scheduler); the rest of the 71 is loads, sums and the waits for both, as a third CTA an SM hides a part of them only.
+// With three CTAs an SM a thread has 80 registers and spills (68 bytes in fp32, 116 and 128 with 16-bit logits); the other kernels, with 120 to
+// 128 registers, do not.
 #include <cfloat>
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
